@@ -318,6 +318,184 @@ rag_status rag_kv_cache_write(const void *k, const void *v, void *k_cache,
                               int32_t head_dim, int32_t block_size,
                               int32_t num_blocks, hipStream_t stream);
 
+/*
+ * Pages of a batch of requests whose lengths change, kept on the GPU: the
+ * block-table entries, the slot mapping of the new tokens and the stack of free
+ * pages, all from the lengths alone.  It is the step before rag_kv_cache_write
+ * (and the paged attention calls) in the serving engine's iteration (Sec.
+ * "Implementation": a paged KV cache), with no length on the host, so that an
+ * iteration can be captured in a HIP graph.
+ *
+ *   block_tables  device int32 [num_seqs, max_blocks_per_seq], in and out: row s
+ *            holds the pages of old_lens[s] tokens in its first
+ *            ceil(old_lens[s] / 16) entries; the entries of the pages that it
+ *            gains are written, all others left as they are.
+ *   free_pages  device int32 [num_blocks], in and out: a stack of the pages
+ *            that no row holds, its top at entry num_free - 1.
+ *   num_free  device int32 [1].
+ *   old_lens, new_lens  device int32 [num_seqs]: tokens that row s holds, and is
+ *            to hold (0 gives all its pages back).
+ *   max_new_tokens  capacity of slot_mapping.
+ *   num_free_out  device int32 [1]: the free pages after the call.
+ *   lens_out  device int32 [num_seqs]: the tokens that row s then holds:
+ *            new_lens[s], or old_lens[s] where it could not grow.
+ *   cu_new   device int32 [num_seqs + 1]: prefix offsets of the tokens added.
+ *   slot_mapping  device int32 [max_new_tokens]: slots (page * 16 + offset) of
+ *            the tokens old_lens[s] .. lens_out[s] - 1 of every row in turn; -1
+ *            (not written, for rag_kv_cache_write) behind the last.
+ *   num_granted  device int32 [1]: num_seqs, or the first row that could not
+ *            grow.
+ *
+ * Rows that shrink give back the pages behind ceil(new_lens[s] / 16): rows in
+ * order, pages in order, onto the stack.  Rows that grow then take pages off its
+ * top, rows in order, pages in order.  A row fits while there are pages on the
+ * stack for it, its pages fit the table and its tokens slot_mapping; from the
+ * first row that does not fit on no row grows (shrinking rows shrink all the
+ * same).  num_free_out, num_granted and lens_out must not be num_free, old_lens
+ * or new_lens: every workgroup reads those.
+ * Preconditions (checked when RAG_ATTN_CHECK=1): 0 <= old_lens[s] <=
+ * max_blocks_per_seq * 16, new_lens[s] >= 0, 0 <= num_free <= num_blocks, every
+ * page at most once on the stack or in a row.
+ *
+ * Returns RAG_OK, RAG_ERR_INVALID_ARG (null pointer, negative size, an output
+ * that is an input, violated precondition in debug mode), RAG_ERR_UNSUPPORTED
+ * (block_size not 16, num_seqs over 4096, num_blocks over 2^27,
+ * max_blocks_per_seq from 2^27 on, max_new_tokens from 2^30 on) or RAG_ERR_HIP.
+ */
+rag_status rag_kv_pages_update(int32_t *block_tables, int32_t *free_pages,
+                               const int32_t *num_free, const int32_t *old_lens,
+                               const int32_t *new_lens, int32_t num_seqs,
+                               int32_t max_blocks_per_seq, int32_t num_blocks,
+                               int32_t block_size, int32_t max_new_tokens,
+                               int32_t *num_free_out, int32_t *lens_out,
+                               int32_t *cu_new, int32_t *slot_mapping,
+                               int32_t *num_granted, hipStream_t stream);
+
+/*
+ * Bytes of workspace that rag_attn_decode_paged_tree needs (0 where it does not
+ * cut its sequences, and for invalid sizes).  Library-internal layout: fp32
+ * partial outputs [num_seqs * max_nodes, num_q_heads, splits, head_dim], then fp32
+ * partial log-sum-exp values.
+ */
+size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
+                                           int32_t num_q_heads,
+                                           int32_t num_kv_heads, int32_t head_dim,
+                                           int32_t max_blocks_per_seq,
+                                           int32_t block_size, int32_t num_splits);
+
+/*
+ * Attention of trees of drafted tokens against a paged KV cache: one step of
+ * speculative decoding, which has the model judge several continuations of every
+ * sequence at once.  The n drafted tokens (nodes) of a sequence are the last n
+ * of its kv_lens[s] keys, their K/V already in the cache (rag_kv_cache_write);
+ * node i sees every key before the nodes, and node j where bit j % 64 of word
+ * j / 64 of its mask is set (for a tree: itself and its ancestors; no bit is
+ * implied).
+ *
+ *   q        device [Tq, num_q_heads, head_dim]   Tq = cu_seqlens_q[num_seqs]
+ *   k_cache, v_cache, block_tables, block_size, num_blocks  as in
+ *            rag_attn_decode_paged
+ *   o        device [Tq, num_q_heads, head_dim]; output, written in full.  A node
+ *            that sees no key (no key before the nodes and no bit) gives 0.
+ *            Values of keys that a node does not see never reach its row,
+ *            whatever they are (NaN in a slot not written yet).
+ *   tree_mask  device uint64 [Tq, mask_words], mask_words >= ceil(max_nodes / 64);
+ *            8-byte aligned.  Bits from the sequence's n on are ignored.
+ *   kv_lens  device int32 [num_seqs]: keys of sequence s, its nodes counted.
+ *   cu_seqlens_q  device int32 [num_seqs + 1]: sequence s has n = cu[s+1] - cu[s]
+ *            nodes, 0 <= n <= max_nodes and n <= kv_lens[s] <=
+ *            max_blocks_per_seq * 16 (checked when RAG_ATTN_CHECK=1, and the ids
+ *            of the pages read).  A sequence without nodes may hold no key.
+ *   max_nodes  host upper bound of n (sizes the grid).
+ *   num_splits  0 = automatic; else the most pieces (at most 64) that a
+ *            sequence's pages are cut into.
+ *   workspace, workspace_bytes  device scratch of at least
+ *            rag_attn_decode_tree_workspace_size(...) bytes for the same
+ *            arguments (NULL when that is 0); 256-byte aligned, of any contents.
+ *            Calls that may overlap, and graphs that may be replayed at once,
+ *            must not share it.
+ *
+ * Any num_q_heads / num_kv_heads.  Returns RAG_OK (num_seqs == 0 or max_nodes == 0
+ * is a no-op), RAG_ERR_INVALID_ARG (null or misaligned pointer, negative size,
+ * heads, scale, too few mask words), RAG_ERR_UNSUPPORTED (head_dim not 64 or 128,
+ * block_size not 16, max_nodes * num_q_heads from 2^24 on),
+ * RAG_ERR_WORKSPACE or RAG_ERR_HIP.
+ */
+rag_status rag_attn_decode_paged_tree(
+    const void *q, const void *k_cache, const void *v_cache, void *o,
+    const uint64_t *tree_mask, const int32_t *block_tables,
+    const int32_t *kv_lens, const int32_t *cu_seqlens_q, int32_t num_seqs,
+    int32_t max_nodes, int32_t mask_words, int32_t max_blocks_per_seq,
+    int32_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads,
+    int32_t head_dim, int32_t block_size, float softmax_scale,
+    int32_t num_splits, void *workspace, size_t workspace_bytes,
+    hipStream_t stream);
+
+/*
+ * Keep the accepted nodes of drafted trees: after a sequence's nodes (keys
+ * base_lens[s], base_lens[s] + 1, ... of its pages) are judged, the K/V rows of
+ * the accepted ones move to the places behind its base_lens[s] keys, in order:
+ * key base_lens[s] + i becomes what key base_lens[s] + kept[s][i] was.  The
+ * sequence then holds base_lens[s] + num_kept[s] keys; rag_kv_pages_update with
+ * that length gives the other pages back.
+ *
+ *   k_cache, v_cache  device [num_blocks, num_kv_heads, block_size, head_dim], in
+ *            and out
+ *   block_tables  device int32 [num_seqs, max_blocks_per_seq]
+ *   base_lens  device int32 [num_seqs]
+ *   kept     device int32 [num_seqs, max_kept]: the first num_kept[s] entries of
+ *            row s are its accepted nodes, strictly increasing (a path from the
+ *            root of a tree whose nodes come after their parents)
+ *   num_kept device int32 [num_seqs], 0 <= num_kept[s] <= max_kept
+ * Preconditions (checked when RAG_ATTN_CHECK=1): the above, keys inside the
+ * table, pages inside the pool; the pages from key base_lens[s] on belong to row
+ * s alone.  Nothing else of the cache changes.
+ *
+ * Returns RAG_OK (num_seqs, max_kept or max_blocks_per_seq 0 is a no-op),
+ * RAG_ERR_INVALID_ARG, RAG_ERR_UNSUPPORTED (head_dim, block_size, sizes) or
+ * RAG_ERR_HIP.
+ */
+rag_status rag_kv_cache_keep(void *k_cache, void *v_cache,
+                             const int32_t *block_tables,
+                             const int32_t *base_lens, const int32_t *kept,
+                             const int32_t *num_kept, int32_t num_seqs,
+                             int32_t max_blocks_per_seq, int32_t max_kept,
+                             int32_t num_blocks, int32_t num_kv_heads,
+                             int32_t head_dim, int32_t block_size,
+                             hipStream_t stream);
+
+/*
+ * Packed variable-length attention with a range of keys per query row, for
+ * stuffed prompts whose documents must not see one another, prefixes seen by
+ * every row and windows: query row i of a sequence with nq rows and nk keys stands
+ * at position p = nk - nq + i and sees key j < nk where
+ *   j < shared, or start <= j <= p,      (shared, start) = key_ranges[row].
+ *
+ *   documents  (system prompt of S tokens, documents, query): (0, 0) for the
+ *              system prompt's rows, (S, first key) for a document's rows, (0, 0)
+ *              for the query's, which see everything before them.  Their K/V
+ *              then depend on the document and the system prompt alone.
+ *   prefix     (P, 0): every row sees the first P keys, and those up to itself.
+ *   window     (F, p - w + 1): the last w keys and the first F.
+ *
+ *   q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k  as in
+ *            rag_attn_prefill_varlen; nq may exceed nk (rows with p < 0 see keys
+ *            below `shared` only).  A row that sees no key gives 0 (lse -inf).
+ *            Values of keys that a row does not see never reach it.
+ *   key_ranges  device int32 [Tq, 2], 8-byte aligned; any values (shared beyond
+ *            nk is nk, a negative one 0; start beyond p: no key of its own).
+ * Key tiles that no row of a query tile sees are not read.  A token generated
+ * behind such a prompt sees all its keys: rag_attn_decode_paged.
+ *
+ * Returns the statuses of rag_attn_prefill_varlen.
+ */
+rag_status rag_attn_prefill_varlen_ranges(
+    const void *q, const void *k, const void *v, void *o, float *lse,
+    const int32_t *cu_seqlens_q, const int32_t *cu_seqlens_k,
+    const int32_t *key_ranges, int32_t num_seqs, int32_t max_seqlen_q,
+    int32_t max_seqlen_k, int32_t num_q_heads, int32_t num_kv_heads,
+    int32_t head_dim, float softmax_scale, hipStream_t stream);
+
 /* Synthesis methods (Sec. "RAG systems and configurations"). */
 typedef enum {
   RAG_STUFF = 0,             /* one prompt: all chunks, then the query       */

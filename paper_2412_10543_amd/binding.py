@@ -51,7 +51,9 @@ def exported_symbols():
             "rag_attn_decode_paged", "rag_attn_decode_paged_noalloc", "rag_kv_cache_write", "rag_plan_prompts",
             "rag_prune_config_space", "rag_config_kv_bytes", "rag_choose_config",
             "rag_device_free_memory", "rag_awq_pack_weights", "rag_awq_workspace_size",
-            "rag_awq_gemm"]
+            "rag_awq_gemm", "rag_kv_pages_update", "rag_kv_cache_keep",
+            "rag_attn_decode_tree_workspace_size", "rag_attn_decode_paged_tree",
+            "rag_attn_prefill_varlen_ranges"]
 
 
 class QueryProfile(ctypes.Structure):
@@ -130,6 +132,21 @@ def lib():
     L.rag_awq_gemm.restype = ctypes.c_int
     L.rag_awq_gemm.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp,
                                ctypes.c_size_t, _vp]
+    L.rag_kv_pages_update.restype = ctypes.c_int
+    L.rag_kv_pages_update.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp,
+                                      _vp, _vp, _vp, _vp, _vp]
+    L.rag_kv_cache_keep.restype = ctypes.c_int
+    L.rag_kv_cache_keep.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32,
+                                    _i32, _i32, _vp]
+    L.rag_attn_decode_tree_workspace_size.restype = ctypes.c_size_t
+    L.rag_attn_decode_tree_workspace_size.argtypes = [_i32] * 8
+    L.rag_attn_decode_paged_tree.restype = ctypes.c_int
+    L.rag_attn_decode_paged_tree.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32,
+                                             _i32, _i32, _i32, _i32, _i32, _i32, _i32,
+                                             ctypes.c_float, _i32, _vp, ctypes.c_size_t, _vp]
+    L.rag_attn_prefill_varlen_ranges.restype = ctypes.c_int
+    L.rag_attn_prefill_varlen_ranges.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32,
+                                                 _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp]
     L.rag_plan_prompts.restype = ctypes.c_int
     L.rag_plan_prompts.argtypes = [ctypes.c_int, _i32, _i32p, _i32p, _i32, _i32, _i32, _i32p,
                                    _i32, _i32p, _i32p]
@@ -319,6 +336,136 @@ def rag_kv_cache_write(k, v, k_cache, v_cache, slot_mapping, stream=None) -> Non
     _check(lib().rag_kv_cache_write(
         _ptr(k), _ptr(v), _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), k.shape[0],
         k.shape[1], k.shape[2], k_cache.shape[2], k_cache.shape[0], _stream(stream)))
+
+
+def _here(*tensors):
+    """The tensors are on the current device, where the call is enqueued."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current device cuda:{dev}, got {t.device}")
+
+
+def _shape_is(t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def rag_kv_pages_update(block_tables, free_pages, num_free, old_lens, new_lens, num_free_out,
+                        lens_out, cu_new, slot_mapping, num_granted, stream=None) -> None:
+    """Pages of S rows that hold old_lens tokens and are to hold new_lens: all
+    int32 on the GPU; block_tables [S, max_blocks] and free_pages [num_blocks]
+    in and out; num_free, num_free_out and num_granted [1]; lens_out [S],
+    cu_new [S+1] and slot_mapping [max_new_tokens] outputs."""
+    for t, n in ((free_pages, "free_pages"), (num_free, "num_free"), (old_lens, "old_lens"),
+                 (new_lens, "new_lens"), (num_free_out, "num_free_out"), (lens_out, "lens_out"),
+                 (cu_new, "cu_new"), (slot_mapping, "slot_mapping"), (num_granted, "num_granted")):
+        _need(t, torch.int32, n, 1)
+    _need(block_tables, torch.int32, "block_tables", 2)
+    S, width = block_tables.shape
+    if not (old_lens.shape[0] == new_lens.shape[0] == lens_out.shape[0] == S and
+            cu_new.shape[0] == S + 1 and
+            num_free.shape[0] == num_free_out.shape[0] == num_granted.shape[0] == 1):
+        raise ValueError("kv pages: inconsistent shapes")
+    _here(block_tables, free_pages, num_free, old_lens, new_lens, num_free_out, lens_out, cu_new,
+          slot_mapping, num_granted)
+    _check(lib().rag_kv_pages_update(
+        _ptr(block_tables), _ptr(free_pages), _ptr(num_free), _ptr(old_lens), _ptr(new_lens), S,
+        width, free_pages.shape[0], 16, slot_mapping.shape[0], _ptr(num_free_out), _ptr(lens_out),
+        _ptr(cu_new), _ptr(slot_mapping), _ptr(num_granted), _stream(stream)))
+
+
+def rag_kv_cache_keep(k_cache, v_cache, block_tables, base_lens, kept, num_kept,
+                      stream=None) -> None:
+    """Moves the K/V rows of the accepted drafted nodes behind their sequence's
+    base_lens keys.  Caches [num_blocks, Hkv, 16, d] bf16; block_tables int32
+    [S, max_blocks]; base_lens and num_kept int32 [S]; kept int32 [S, max_kept]."""
+    for t, n in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _need(t, torch.bfloat16, n, 4)
+    _need(block_tables, torch.int32, "block_tables", 2)
+    _need(kept, torch.int32, "kept", 2)
+    _need(base_lens, torch.int32, "base_lens", 1)
+    _need(num_kept, torch.int32, "num_kept", 1)
+    S = block_tables.shape[0]
+    if not (kept.shape[0] == base_lens.shape[0] == num_kept.shape[0] == S) or \
+            v_cache.shape != k_cache.shape:
+        raise ValueError("kv keep: inconsistent shapes")
+    _here(k_cache, v_cache, block_tables, base_lens, kept, num_kept)
+    blocks, hkv, block, d = k_cache.shape
+    _check(lib().rag_kv_cache_keep(
+        _ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(base_lens), _ptr(kept),
+        _ptr(num_kept), S, block_tables.shape[1], kept.shape[1], blocks, hkv, d, block,
+        _stream(stream)))
+
+
+def rag_attn_decode_tree_workspace_size(num_seqs, max_nodes, num_q_heads, num_kv_heads, head_dim,
+                                        max_blocks_per_seq, block_size=16, num_splits=0) -> int:
+    return lib().rag_attn_decode_tree_workspace_size(num_seqs, max_nodes, num_q_heads,
+                                                     num_kv_heads, head_dim, max_blocks_per_seq,
+                                                     block_size, num_splits)
+
+
+def rag_attn_decode_paged_tree(q, k_cache, v_cache, o, tree_mask, block_tables, kv_lens,
+                               cu_seqlens_q, max_nodes, softmax_scale, num_splits=0,
+                               workspace=None, stream=None) -> None:
+    """q, o [Tq, Hq, d]; caches [num_blocks, Hkv, 16, d] bf16; tree_mask int64
+    [Tq, words]: bit j of row i's words set where node i sees node j; block_tables
+    int32 [S, max_blocks]; kv_lens int32 [S], the nodes counted; cu_seqlens_q int32
+    [S+1] offsets of the nodes; workspace a GPU tensor (torch.empty, uint8) of
+    rag_attn_decode_tree_workspace_size bytes, or None when that size is 0."""
+    _need(q, torch.bfloat16, "q", 3)
+    _need(o, torch.bfloat16, "o", 3)
+    _need(k_cache, torch.bfloat16, "k_cache", 4)
+    _need(v_cache, torch.bfloat16, "v_cache", 4)
+    _need(tree_mask, torch.int64, "tree_mask", 2)
+    _need(block_tables, torch.int32, "block_tables", 2)
+    _need(kv_lens, torch.int32, "kv_lens", 1)
+    _need(cu_seqlens_q, torch.int32, "cu_seqlens_q", 1)
+    S = block_tables.shape[0]
+    blocks, hkv, block, d = k_cache.shape
+    if o.shape != q.shape or v_cache.shape != k_cache.shape or q.shape[2] != d or \
+            tree_mask.shape[0] != q.shape[0] or kv_lens.shape[0] != S or \
+            cu_seqlens_q.shape[0] != S + 1:
+        raise ValueError("decode tree: inconsistent shapes")
+    ws_bytes = 0
+    if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous GPU tensor")
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _here(q, k_cache, v_cache, o, tree_mask, block_tables, kv_lens, cu_seqlens_q, workspace)
+    if q.shape[0] == 0:
+        return
+    _check(lib().rag_attn_decode_paged_tree(
+        _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(o), _ptr(tree_mask), _ptr(block_tables),
+        _ptr(kv_lens), _ptr(cu_seqlens_q), S, int(max_nodes), tree_mask.shape[1],
+        block_tables.shape[1], blocks, q.shape[1], hkv, d, block, float(softmax_scale),
+        int(num_splits), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, key_ranges,
+                                   max_seqlen_q, max_seqlen_k, softmax_scale, stream=None) -> None:
+    """q, o [Tq, Hq, d]; k, v [Tk, Hkv, d] bf16; lse fp32 [Hq, Tq] or None;
+    cu_seqlens_* int32 [S+1]; key_ranges int32 [Tq, 2]: the (shared, start) of each
+    row, which sees the keys j < shared and start <= j <= its position."""
+    for t, n in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
+        _need(t, torch.bfloat16, n, 3)
+    _need(cu_seqlens_q, torch.int32, "cu_seqlens_q", 1)
+    _need(cu_seqlens_k, torch.int32, "cu_seqlens_k", 1)
+    _need(key_ranges, torch.int32, "key_ranges", 2)
+    if o.shape != q.shape or v.shape != k.shape or k.shape[2] != q.shape[2] or \
+            cu_seqlens_k.shape != cu_seqlens_q.shape:
+        raise ValueError("prefill ranges: inconsistent shapes")
+    _shape_is(key_ranges, (q.shape[0], 2), "key_ranges")
+    if lse is not None:
+        _need(lse, torch.float32, "lse", 2)
+        _shape_is(lse, (q.shape[1], q.shape[0]), "lse")
+    _here(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, key_ranges)
+    if q.shape[0] == 0:
+        return
+    _check(lib().rag_attn_prefill_varlen_ranges(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(cu_seqlens_q), _ptr(cu_seqlens_k),
+        _ptr(key_ranges), cu_seqlens_q.shape[0] - 1, int(max_seqlen_q), int(max_seqlen_k),
+        q.shape[1], k.shape[1], q.shape[2], float(softmax_scale), _stream(stream)))
 
 
 def rag_plan_prompts(method, query_len, num_chunks, chunk_len, intermediate_length=0,

@@ -10,6 +10,7 @@
 #include <string>
 #include <vector>
 
+#include "checks.h"
 #include "common.h"
 #include "errors.h"
 #include "launch.h"
@@ -40,42 +41,14 @@ rag_status ok() {
 
 namespace {
 
+using rag::aligned16;
+using rag::check_cu;
+using rag::check_mode;
 using rag::fail;
+using rag::fetch;
+using rag::kBlock;
 using rag::ok;
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-bool check_mode() {
-  static const bool on = [] {
-    const char* e = std::getenv("RAG_ATTN_CHECK");
-    return e != nullptr && e[0] == '1';
-  }();
-  return on;
-}
-
-// Copies n int32 values from device memory (stream-ordered, synchronous).
-bool fetch(std::vector<int32_t>& dst, const int32_t* src, size_t n, hipStream_t stream) {
-  dst.resize(n);
-  if (n == 0) return true;
-  if (hipMemcpyAsync(dst.data(), src, n * sizeof(int32_t), hipMemcpyDeviceToHost, stream) !=
-      hipSuccess)
-    return false;
-  return hipStreamSynchronize(stream) == hipSuccess;
-}
-
-rag_status check_cu(const std::vector<int32_t>& cu, const char* name, int32_t max_len) {
-  if (cu[0] != 0) return fail(RAG_ERR_INVALID_ARG, "%s[0] = %d, expected 0", name, cu[0]);
-  for (size_t s = 0; s + 1 < cu.size(); ++s) {
-    const int64_t n = (int64_t)cu[s + 1] - cu[s];
-    if (n < 0) return fail(RAG_ERR_INVALID_ARG, "%s decreases at %zu", name, s);
-    if (n > max_len)
-      return fail(RAG_ERR_INVALID_ARG, "%s: sequence %zu has %lld > max %d rows", name, s,
-                  (long long)n, max_len);
-  }
-  return RAG_OK;
-}
-
-constexpr int32_t kBlock = 16;
 constexpr int32_t kMaxGroupDecode = 16;
 // Decode units are workgroups of four waves.  Each unit pays a fixed cost
 // (first page latency, merge of its split), so auto splits aim at about one

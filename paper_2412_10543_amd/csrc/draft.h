@@ -1,0 +1,79 @@
+// Host-side launch descriptors of the page tables, the drafted-token and the
+// key-range kernels (internal; the public ABI is include/rag_attn.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace rag {
+
+struct PagesArgs {
+  int32_t* tables;              // [num_seqs, max_blocks]
+  int32_t* stack;               // [num_blocks], num_free of them used
+  const int32_t* num_free;
+  const int32_t* old_lens;      // [num_seqs]
+  const int32_t* new_lens;
+  int32_t* num_free_out;
+  int32_t* lens_out;
+  int32_t* cu_new;              // [num_seqs + 1]
+  int32_t* slots;               // [max_new_tokens]
+  int32_t* num_granted;
+  int num_seqs, max_blocks, num_blocks, max_new_tokens;
+};
+
+struct KeepArgs {
+  void* k_cache;                // [num_blocks, hkv, 16, d]
+  void* v_cache;
+  const int32_t* tables;
+  const int32_t* base_lens;     // [num_seqs]
+  const int32_t* kept;          // [num_seqs, max_kept]
+  const int32_t* num_kept;      // [num_seqs]
+  int num_seqs, max_blocks, max_kept, hkv, d;
+};
+
+struct TreeArgs {
+  const void* q;                // [Tq, hq, d]
+  const void* k_cache;
+  const void* v_cache;
+  void* o;
+  const uint64_t* mask;         // [Tq, mask_words]
+  const int32_t* tables;
+  const int32_t* kv_lens;
+  const int32_t* cu_q;
+  int num_seqs, max_nodes, mask_words, max_blocks, hq, hkv, d;
+  float scale;
+  int num_splits;               // pieces that a sequence's pages are cut into, at most
+  float* part_o;                // [query row, head][split][d] (num_splits > 1)
+  float* part_lse;              // [query row, head][split]
+};
+
+struct RangesArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  const int32_t* ranges;        // [Tq, 2]
+  int num_seqs, max_seqlen_q, hq, hkv, d;
+  float scale;
+};
+
+constexpr int kPagesMaxSeqs = 4096;        // rows of one rag_kv_pages_update call (LDS)
+constexpr int kTreeMaxSplits = 64;
+
+int64_t pages_grid(const PagesArgs& a);
+hipError_t launch_pages(const PagesArgs& a, hipStream_t stream);
+int64_t keep_grid(const KeepArgs& a);
+hipError_t launch_keep(const KeepArgs& a, hipStream_t stream);
+// Pieces that a tree launch cuts a sequence's pages into (requested 0: chosen).
+int tree_splits(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks, int requested);
+int64_t tree_grid(const TreeArgs& a);
+hipError_t launch_tree(const TreeArgs& a, hipStream_t stream);
+int64_t ranges_grid(const RangesArgs& a);
+hipError_t launch_ranges(const RangesArgs& a, hipStream_t stream);
+
+}  // namespace rag

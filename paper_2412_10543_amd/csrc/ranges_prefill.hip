@@ -1,0 +1,129 @@
+// Packed variable-length attention with a key range per query row (gfx950): the
+// row at position p of its sequence sees the keys j < shared and the keys
+// start <= j <= p.  Documents that do not see one another, prefixes seen by
+// every row, windows with a few first keys.
+//
+// A workgroup is one tile of query rows of up to four heads of a GQA group, as
+// in the causal prefill; it visits the key tiles of two spans only: up to its
+// rows' largest `shared`, and from their smallest `start` to their last
+// position.
+#include "common.h"
+#include "draft.h"
+#include "masked_tile.h"
+
+namespace rag {
+
+namespace {
+
+constexpr int kRgWaves = 8;
+
+// The lane's row, and for the wave what makes a block full.
+struct RangeRows {
+  const bf16_t* qrow;
+  int shared, start, last;      // keys below shared, and start..last
+  int shared_min, start_max, last_min;           // of the wave's rows
+  __device__ __forceinline__ const bf16_t* q() const { return qrow; }
+  __device__ __forceinline__ bool full(int k0) const {
+    return k0 + 32 <= shared_min || (k0 >= start_max && k0 + 31 <= last_min);
+  }
+  __device__ __forceinline__ uint32_t seen(int k0) const {
+    return low_bits(shared - k0) | (low_bits(last + 1 - k0) & ~low_bits(start - k0));
+  }
+};
+
+template <class F>
+__device__ __forceinline__ int wave_reduce(int x, const F& f) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x = f(x, __shfl_xor(x, m, kWave));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+}  // namespace
+
+template <int D>
+__global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, int n_qt) {
+  __shared__ __attribute__((aligned(16))) bf16_t stage[ChunkLayout<D>::kElemsTile];
+  __shared__ int span[3][kRgWaves];
+  const int group = a.hq / a.hkv, hw = pf_heads_per_wg(group), ng = group / hw;
+  int xcd, local;
+  xcd_slot(blockIdx.x, xcd, local);
+  const int hg = local % ng, j = local / ng % n_qt;
+  const int stream = xcd + kNumXcd * (local / ng / n_qt);
+  if (stream >= a.num_seqs * a.hkv) return;
+  const int s = stream / a.hkv, kvh = stream % a.hkv, h0 = kvh * group + hg * hw;
+  const int qb = a.cu_q[s], nq = a.cu_q[s + 1] - qb;
+  const int kb = a.cu_k[s], nk = a.cu_k[s + 1] - kb;
+  const int rows = pf_rows_per_tile(group, kRgWaves);
+  const int q0 = (n_qt - 1 - j) * rows;          // tiles with the most keys first
+  if (q0 >= nq) return;
+  const int wave = wave_id(), lane = threadIdx.x & 63, half = lane >> 5;
+  const int r = q0 + 32 * (wave / hw) + (lane & 31);
+  const int rc = min(r, nq - 1), head = h0 + wave % hw;
+  RangeRows rr;
+  rr.qrow = (const bf16_t*)a.q + ((size_t)(qb + rc) * a.hq + head) * D;
+  const int2 rg = reinterpret_cast<const int2*>(a.ranges)[qb + rc];
+  rr.last = min(nk - nq + rc, nk - 1);
+  rr.shared = min(max(rg.x, 0), nk);
+  rr.start = max(rg.y, 0);
+  if (rr.start > rr.last) {                      // nothing of its own
+    rr.start = nk;
+    rr.last = -1;
+  }
+  auto lo = [](int x, int y) { return min(x, y); };
+  auto hi = [](int x, int y) { return max(x, y); };
+  rr.shared_min = wave_reduce(rr.shared, lo);
+  rr.start_max = wave_reduce(rr.start, hi);
+  rr.last_min = wave_reduce(rr.last, lo);
+  const int shared_max = wave_reduce(rr.shared, hi), start_min = wave_reduce(rr.start, lo);
+  const int last_max = wave_reduce(rr.last, hi);
+  if (lane == 0) {
+    span[0][wave] = shared_max;
+    span[1][wave] = start_min;
+    span[2][wave] = last_max;
+  }
+  __syncthreads();
+  int a1 = 0, b0 = nk, b1 = 0;
+#pragma unroll
+  for (int w = 0; w < kRgWaves; ++w) {
+    a1 = max(a1, span[0][w]);
+    b0 = min(b0, span[1][w]);
+    b1 = max(b1, span[2][w] + 1);
+  }
+  const DenseKV kv{(const bf16_t*)a.k + ((size_t)kb * a.hkv + kvh) * D,
+                   (const bf16_t*)a.v + ((size_t)kb * a.hkv + kvh) * D, (size_t)a.hkv * D};
+  const KeySpans sp = key_spans(a1, b0, b1);
+  PfState<D> st;
+  masked_tile<D, kRgWaves>(rr, kv, sp, 0, sp.tiles(), nk, a.scale, stage, st);
+  const float lse = mt_finish<D>(st, a.scale);
+  if (r >= nq) return;
+  bf16_t* o = (bf16_t*)a.o + ((size_t)(qb + r) * a.hq + head) * D + 4 * half;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<bf16x4*>(o + 32 * dt + 8 * g) =
+          to_bf16x4(st.oacc[dt][4 * g], st.oacc[dt][4 * g + 1], st.oacc[dt][4 * g + 2],
+                    st.oacc[dt][4 * g + 3]);
+  if (a.lse != nullptr && half == 0) a.lse[(size_t)head * a.cu_q[a.num_seqs] + qb + r] = lse;
+}
+
+int64_t ranges_grid(const RangesArgs& a) {
+  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kRgWaves);
+  const int64_t n_qt = (a.max_seqlen_q + (int64_t)rows - 1) / rows;
+  const int64_t streams = (int64_t)a.num_seqs * a.hkv;
+  return (streams + kNumXcd - 1) / kNumXcd * kNumXcd * n_qt * (group / pf_heads_per_wg(group));
+}
+
+hipError_t launch_ranges(const RangesArgs& a, hipStream_t stream) {
+  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kRgWaves);
+  const int n_qt = (a.max_seqlen_q + rows - 1) / rows;
+  const int64_t grid = ranges_grid(a);
+  if (grid == 0) return hipSuccess;
+  if (a.d == 64)
+    hipLaunchKernelGGL(ranges_kernel<64>, dim3((unsigned)grid), dim3(64 * kRgWaves), 0, stream, a, n_qt);
+  else
+    hipLaunchKernelGGL(ranges_kernel<128>, dim3((unsigned)grid), dim3(64 * kRgWaves), 0, stream, a, n_qt);
+  return hipGetLastError();
+}
+
+}  // namespace rag
