@@ -86,6 +86,7 @@ template <int D>
 struct ChunkLayout {
   static constexpr int kCh = D / 8;                  // 16-byte chunks per row
   static constexpr int kElemsTile = 2 * kPfBN * D;   // K then V
+  static constexpr int kVBase = kPfBN * D;           // V in a stage
   int k_lane, v_lane;                                // in bf16 elements
   __device__ __forceinline__ ChunkLayout() {
     const int lane = threadIdx.x & 63;
@@ -271,8 +272,8 @@ __device__ __forceinline__ void pf_barrier() {
 
 // S^T of the 32 keys [32*H, 32*H + 32) of a staged tile against this wave's
 // rows; element j of the result is key 8*(j/4) + 4*half + j%4 of the block.
-template <int D, int H>
-__device__ __forceinline__ f32x16 pf_qk(const PfState<D>& st, const ChunkLayout<D>& lay,
+template <int D, int H, class Lay>
+__device__ __forceinline__ f32x16 pf_qk(const PfState<D>& st, const Lay& lay,
                                         const bf16_t* __restrict__ kst) {
   f32x16 s = {};
 #pragma unroll
@@ -286,10 +287,10 @@ __device__ __forceinline__ f32x16 pf_qk(const PfState<D>& st, const ChunkLayout<
 // O^T += V^T P^T over the keys [32*H, 32*H + 32) of a staged tile (stage =
 // the tile's K then V); p[s2] is
 // the B operand of keys 16*s2 .. +16 of the block (see pf_tile for the order).
-template <int D, int H>
-__device__ __forceinline__ void pf_pv(PfState<D>& st, const ChunkLayout<D>& lay,
+template <int D, int H, class Lay>
+__device__ __forceinline__ void pf_pv(PfState<D>& st, const Lay& lay,
                                       const bf16_t* __restrict__ stage, const bf16x8 (&p)[2]) {
-  const bf16_t* vst = stage + kPfBN * D;   // V follows K in a stage
+  const bf16_t* vst = stage + Lay::kVBase;
 #pragma unroll
   for (int s2 = 0; s2 < 2; ++s2) {
     const int rw = 32 * H + 16 * s2;
@@ -378,14 +379,14 @@ struct PfPipeCtx {
 struct PfNoHook {
   __device__ __forceinline__ void operator()(int) const {}
 };
-template <int D, int HK, int HV, class Hook = PfNoHook>
-__device__ __forceinline__ float pf_full_slot(PfState<D>& st, const ChunkLayout<D>& lay,
+template <int D, int HK, int HV, class Lay, class Hook = PfNoHook>
+__device__ __forceinline__ float pf_full_slot(PfState<D>& st, const Lay& lay,
                                               const bf16_t* __restrict__ kst,
                                               const bf16_t* __restrict__ vstage,
                                               const f32x16& s_cur, f32x16& s_next,
                                               bf16x8 (&p_cur)[2], const bf16x8 (&p_prev)[2],
                                               float c, float nm, const Hook& hook = Hook()) {
-  const bf16_t* vst = vstage + kPfBN * D;   // V follows K in a stage
+  const bf16_t* vst = vstage + Lay::kVBase;
   constexpr int kSteps = D / 16;          // QK MFMAs = PV MFMAs = steps
   constexpr int kDt = D / 32;
   constexpr int kPer = 16 / kSteps;       // scores (per lane) per step

@@ -42,7 +42,10 @@ __device__ __forceinline__ int wave_reduce(int x, const F& f) {
 
 template <int D>
 __global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, int n_qt) {
-  __shared__ __attribute__((aligned(16))) bf16_t stage[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st0[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st1[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st2[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st3[ChunkLayout<D>::kElemsTile];
   __shared__ int span[3][kRgWaves];
   const int group = a.hq / a.hkv, hw = pf_heads_per_wg(group), ng = group / hw;
   int xcd, local;
@@ -93,7 +96,7 @@ __global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, 
                    (const bf16_t*)a.v + ((size_t)kb * a.hkv + kvh) * D, (size_t)a.hkv * D};
   const KeySpans sp = key_spans(a1, b0, b1);
   PfState<D> st;
-  masked_tile<D, kRgWaves>(rr, kv, sp, 0, sp.tiles(), nk, a.scale, stage, st);
+  masked_tile<D, kRgWaves>(rr, kv, sp, 0, sp.tiles(), nk, a.scale, st0, st1, st2, st3, st);
   const float lse = mt_finish<D>(st, a.scale);
   if (r >= nq) return;
   bf16_t* o = (bf16_t*)a.o + ((size_t)(qb + r) * a.hq + head) * D + 4 * half;

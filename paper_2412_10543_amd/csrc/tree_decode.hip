@@ -17,19 +17,6 @@ namespace {
 constexpr int kTrWaves = 8;
 constexpr int kTrRows = 32 * kTrWaves;
 
-template <int D>
-struct PagedKV {
-  const bf16_t* k;              // this kv head in block 0
-  const bf16_t* v;
-  const int32_t* table;
-  size_t block_stride;
-  __device__ __forceinline__ size_t at(int j) const {
-    return (size_t)table[j >> 4] * block_stride + (size_t)(j & 15) * D;
-  }
-  __device__ __forceinline__ const bf16_t* krow(int j) const { return k + at(j); }
-  __device__ __forceinline__ const bf16_t* vrow(int j) const { return v + at(j); }
-};
-
 // The lane's row: node and head of the group.
 struct TreeRows {
   const bf16_t* qrow;
@@ -81,7 +68,10 @@ __device__ __forceinline__ int tree_pieces(const TreeArgs& a, int kv_len, int& p
 
 template <int D>
 __global__ __launch_bounds__(64 * kTrWaves, 2) void tree_kernel(TreeArgs a) {
-  __shared__ __attribute__((aligned(16))) bf16_t stage[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st0[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st1[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st2[ChunkLayout<D>::kElemsTile];
+  __shared__ __attribute__((aligned(16))) bf16_t st3[ChunkLayout<D>::kElemsTile];
   const int group = a.hq / a.hkv;
   TreeCoord t;
   if (!tree_coord(a, (a.max_nodes * group + kTrRows - 1) / kTrRows, t)) return;
@@ -102,13 +92,13 @@ __global__ __launch_bounds__(64 * kTrWaves, 2) void tree_kernel(TreeArgs a) {
   tr.prior = nk - n;
   tr.n = n;
   tr.words = a.mask_words;
-  const PagedKV<D> kv{(const bf16_t*)a.k_cache + (size_t)t.kvh * 16 * D,
+  const PagedDmaKV<D> kv{(const bf16_t*)a.k_cache + (size_t)t.kvh * 16 * D,
                       (const bf16_t*)a.v_cache + (size_t)t.kvh * 16 * D,
                       a.tables + (size_t)t.s * a.max_blocks, (size_t)a.hkv * 16 * D};
   const KeySpans sp = key_spans(nk, 0, 0);
   PfState<D> st;
   masked_tile<D, kTrWaves>(tr, kv, sp, t.sp * pps / 4, min(sp.tiles(), (t.sp + 1) * pps / 4), nk,
-                           a.scale, stage, st);
+                           a.scale, st0, st1, st2, st3, st);
   const float lse = mt_finish<D>(st, a.scale);
   if (r >= rows) return;
   if (n_sp == 1) {
