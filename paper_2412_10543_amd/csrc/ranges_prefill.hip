@@ -7,6 +7,8 @@
 // in the causal prefill; it visits the key tiles of two spans only: up to its
 // rows' largest `shared`, and from their smallest `start` to their last
 // position.
+#include <climits>
+
 #include "common.h"
 #include "draft.h"
 #include "masked_tile.h"
@@ -14,8 +16,6 @@
 namespace rag {
 
 namespace {
-
-constexpr int kRgWaves = 8;
 
 // The lane's row, and for the wave what makes a block full.
 struct RangeRows {
@@ -31,22 +31,25 @@ struct RangeRows {
   }
 };
 
-template <class F>
-__device__ __forceinline__ int wave_reduce(int x, const F& f) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x = f(x, __shfl_xor(x, m, kWave));
-  return __builtin_amdgcn_readfirstlane(x);
+// Maximum over the wave of values from 0 on.
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));   // row_shr:1
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));   // row_shr:2
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));   // row_shr:4
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));   // row_shr:8
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));   // row_bcast:15
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));   // row_bcast:31
+  return __builtin_amdgcn_readlane(x, 63);
 }
+__device__ __forceinline__ int wave_min(int x) { return INT_MAX - wave_max(INT_MAX - x); }
 
 }  // namespace
 
 template <int D>
-__global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, int n_qt) {
-  __shared__ __attribute__((aligned(16))) bf16_t st0[ChunkLayout<D>::kElemsTile];
-  __shared__ __attribute__((aligned(16))) bf16_t st1[ChunkLayout<D>::kElemsTile];
-  __shared__ __attribute__((aligned(16))) bf16_t st2[ChunkLayout<D>::kElemsTile];
-  __shared__ __attribute__((aligned(16))) bf16_t st3[ChunkLayout<D>::kElemsTile];
-  __shared__ int span[3][kRgWaves];
+__global__ __launch_bounds__(64 * kMtWaves, 2) void ranges_kernel(RangesArgs a, int n_qt) {
+  __shared__ __attribute__((aligned(16))) bf16_t kring[kMtRing * BlockLayout<D>::kElems];
+  __shared__ __attribute__((aligned(16))) bf16_t vring[kMtRing * BlockLayout<D>::kElems];
+  __shared__ int span[3][kMtWaves];
   const int group = a.hq / a.hkv, hw = pf_heads_per_wg(group), ng = group / hw;
   int xcd, local;
   xcd_slot(blockIdx.x, xcd, local);
@@ -56,7 +59,7 @@ __global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, 
   const int s = stream / a.hkv, kvh = stream % a.hkv, h0 = kvh * group + hg * hw;
   const int qb = a.cu_q[s], nq = a.cu_q[s + 1] - qb;
   const int kb = a.cu_k[s], nk = a.cu_k[s + 1] - kb;
-  const int rows = pf_rows_per_tile(group, kRgWaves);
+  const int rows = pf_rows_per_tile(group, kMtWaves);
   const int q0 = (n_qt - 1 - j) * rows;          // tiles with the most keys first
   if (q0 >= nq) return;
   const int wave = wave_id(), lane = threadIdx.x & 63, half = lane >> 5;
@@ -72,13 +75,11 @@ __global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, 
     rr.start = nk;
     rr.last = -1;
   }
-  auto lo = [](int x, int y) { return min(x, y); };
-  auto hi = [](int x, int y) { return max(x, y); };
-  rr.shared_min = wave_reduce(rr.shared, lo);
-  rr.start_max = wave_reduce(rr.start, hi);
-  rr.last_min = wave_reduce(rr.last, lo);
-  const int shared_max = wave_reduce(rr.shared, hi), start_min = wave_reduce(rr.start, lo);
-  const int last_max = wave_reduce(rr.last, hi);
+  rr.shared_min = wave_min(rr.shared);
+  rr.start_max = wave_max(rr.start);
+  rr.last_min = wave_min(rr.last + 1) - 1;
+  const int shared_max = wave_max(rr.shared), start_min = wave_min(rr.start);
+  const int last_max = wave_max(rr.last + 1) - 1;
   if (lane == 0) {
     span[0][wave] = shared_max;
     span[1][wave] = start_min;
@@ -87,16 +88,18 @@ __global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, 
   __syncthreads();
   int a1 = 0, b0 = nk, b1 = 0;
 #pragma unroll
-  for (int w = 0; w < kRgWaves; ++w) {
+  for (int w = 0; w < kMtWaves; ++w) {
     a1 = max(a1, span[0][w]);
     b0 = min(b0, span[1][w]);
     b1 = max(b1, span[2][w] + 1);
   }
   const DenseKV kv{(const bf16_t*)a.k + ((size_t)kb * a.hkv + kvh) * D,
                    (const bf16_t*)a.v + ((size_t)kb * a.hkv + kvh) * D, (size_t)a.hkv * D};
-  const KeySpans sp = key_spans(a1, b0, b1);
+  const KeySpans sp = key_spans(__builtin_amdgcn_readfirstlane(a1),
+                                __builtin_amdgcn_readfirstlane(b0),
+                                __builtin_amdgcn_readfirstlane(b1));
   PfState<D> st;
-  masked_tile<D, kRgWaves>(rr, kv, sp, 0, sp.tiles(), nk, a.scale, st0, st1, st2, st3, st);
+  masked_tile<D>(rr, kv, sp, 0, sp.blocks(), nk, a.scale, kring, vring, st);
   const float lse = mt_finish<D>(st, a.scale);
   if (r >= nq) return;
   bf16_t* o = (bf16_t*)a.o + ((size_t)(qb + r) * a.hq + head) * D + 4 * half;
@@ -111,21 +114,21 @@ __global__ __launch_bounds__(64 * kRgWaves, 2) void ranges_kernel(RangesArgs a, 
 }
 
 int64_t ranges_grid(const RangesArgs& a) {
-  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kRgWaves);
+  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kMtWaves);
   const int64_t n_qt = (a.max_seqlen_q + (int64_t)rows - 1) / rows;
   const int64_t streams = (int64_t)a.num_seqs * a.hkv;
   return (streams + kNumXcd - 1) / kNumXcd * kNumXcd * n_qt * (group / pf_heads_per_wg(group));
 }
 
 hipError_t launch_ranges(const RangesArgs& a, hipStream_t stream) {
-  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kRgWaves);
+  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kMtWaves);
   const int n_qt = (a.max_seqlen_q + rows - 1) / rows;
   const int64_t grid = ranges_grid(a);
   if (grid == 0) return hipSuccess;
   if (a.d == 64)
-    hipLaunchKernelGGL(ranges_kernel<64>, dim3((unsigned)grid), dim3(64 * kRgWaves), 0, stream, a, n_qt);
+    hipLaunchKernelGGL(ranges_kernel<64>, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a, n_qt);
   else
-    hipLaunchKernelGGL(ranges_kernel<128>, dim3((unsigned)grid), dim3(64 * kRgWaves), 0, stream, a, n_qt);
+    hipLaunchKernelGGL(ranges_kernel<128>, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a, n_qt);
   return hipGetLastError();
 }
 

@@ -2,7 +2,7 @@
 // queries of a sequence's n drafted nodes, its last n keys, see every key
 // before them and the nodes that their mask names.
 //
-// A unit is (sequence, kv head, 256 rows, piece of the pages): its rows are the
+// A unit is (sequence, kv head, 128 rows, piece of the pages): its rows are the
 // (node, q head of the group) pairs, node by node, so that every K/V byte is
 // read once for all of them.  Pieces of one sequence write normalised partial
 // outputs and their log-sum-exp, which a second kernel joins.
@@ -14,8 +14,7 @@ namespace rag {
 
 namespace {
 
-constexpr int kTrWaves = 8;
-constexpr int kTrRows = 32 * kTrWaves;
+constexpr int kTrRows = 32 * kMtWaves;
 
 // The lane's row: node and head of the group.
 struct TreeRows {
@@ -62,16 +61,14 @@ __device__ __forceinline__ bool tree_coord(const TreeArgs& a, int row_blocks, Tr
 // Pieces that a sequence of kv_len keys is cut into, of pps pages each.
 __device__ __forceinline__ int tree_pieces(const TreeArgs& a, int kv_len, int& pps) {
   pps = max(1, (a.max_blocks + a.num_splits - 1) / a.num_splits);
-  pps = (pps + 3) & ~3;                          // whole 64-key tiles
+  pps = (pps + 1) & ~1;                          // whole blocks of 32 keys
   return max(1, ((kv_len + 15) / 16 + pps - 1) / pps);
 }
 
 template <int D>
-__global__ __launch_bounds__(64 * kTrWaves, 2) void tree_kernel(TreeArgs a) {
-  __shared__ __attribute__((aligned(16))) bf16_t st0[ChunkLayout<D>::kElemsTile];
-  __shared__ __attribute__((aligned(16))) bf16_t st1[ChunkLayout<D>::kElemsTile];
-  __shared__ __attribute__((aligned(16))) bf16_t st2[ChunkLayout<D>::kElemsTile];
-  __shared__ __attribute__((aligned(16))) bf16_t st3[ChunkLayout<D>::kElemsTile];
+__global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
+  __shared__ __attribute__((aligned(16))) bf16_t kring[kMtRing * BlockLayout<D>::kElems];
+  __shared__ __attribute__((aligned(16))) bf16_t vring[kMtRing * BlockLayout<D>::kElems];
   const int group = a.hq / a.hkv;
   TreeCoord t;
   if (!tree_coord(a, (a.max_nodes * group + kTrRows - 1) / kTrRows, t)) return;
@@ -97,8 +94,8 @@ __global__ __launch_bounds__(64 * kTrWaves, 2) void tree_kernel(TreeArgs a) {
                       a.tables + (size_t)t.s * a.max_blocks, (size_t)a.hkv * 16 * D};
   const KeySpans sp = key_spans(nk, 0, 0);
   PfState<D> st;
-  masked_tile<D, kTrWaves>(tr, kv, sp, t.sp * pps / 4, min(sp.tiles(), (t.sp + 1) * pps / 4), nk,
-                           a.scale, st0, st1, st2, st3, st);
+  masked_tile<D>(tr, kv, sp, t.sp * pps / 2, min(sp.blocks(), (t.sp + 1) * pps / 2), nk, a.scale,
+                 kring, vring, st);
   const float lse = mt_finish<D>(st, a.scale);
   if (r >= rows) return;
   if (n_sp == 1) {
@@ -171,7 +168,7 @@ int tree_splits(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blo
   const int64_t units = (int64_t)num_seqs * hkv * std::max(1, tree_row_blocks(max_nodes, hq / hkv));
   int64_t n = requested > 0 ? requested : (512 + units - 1) / units;
   if (requested <= 0) n = std::min<int64_t>(n, std::max(1, max_blocks / 16));
-  n = std::max<int64_t>(1, std::min<int64_t>({n, (int64_t)kTreeMaxSplits, (int64_t)(max_blocks + 3) / 4}));
+  n = std::max<int64_t>(1, std::min<int64_t>({n, (int64_t)kTreeMaxSplits, (int64_t)(max_blocks + 1) / 2}));
   return (int)n;
 }
 
@@ -191,7 +188,7 @@ static hipError_t launch_tree_d(const TreeArgs& a, hipStream_t stream) {
   const int64_t streams = (int64_t)a.num_seqs * a.hkv * a.num_splits;
   const int64_t grid =
       (streams + kNumXcd - 1) / kNumXcd * kNumXcd * tree_row_blocks(a.max_nodes, a.hq / a.hkv);
-  hipLaunchKernelGGL(tree_kernel<D>, dim3((unsigned)grid), dim3(64 * kTrWaves), 0, stream, a);
+  hipLaunchKernelGGL(tree_kernel<D>, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a);
   if (a.num_splits > 1)
     hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)tree_join_grid(a)), dim3(256), 0,
                        stream, a);
