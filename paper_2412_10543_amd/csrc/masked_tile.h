@@ -52,6 +52,13 @@ __device__ __forceinline__ KeySpans key_spans(int a1, int b0, int b1) {
   return k;
 }
 
+// Element i of an array that nothing in the launch writes, i the same for the
+// wave: a scalar load.
+__device__ __forceinline__ int uniform_load(const int32_t* p, int i) {
+  typedef __attribute__((address_space(4))) const int32_t const_i32;
+  return ((const_i32*)p)[i];
+}
+
 // Bits of a word for the keys below n of a block (n counts from its first).
 __device__ __forceinline__ uint32_t low_bits(int n) {
   return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
@@ -263,9 +270,10 @@ struct BlockCopy {
   }
 };
 
-template <int D, class Rows>
-__device__ __forceinline__ void mt_load_q(PfState<D>& st, const Rows& rows) {
-  const bf16_t* q = rows.q() + 8 * (opaque_lane() >> 5);
+// The lane's query row.
+template <int D>
+__device__ __forceinline__ void mt_load_q(PfState<D>& st, const bf16_t* row) {
+  const bf16_t* q = row + 8 * (opaque_lane() >> 5);
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) st.qf[ks] = as_bf16x8(load16(q + 16 * ks));
 }
@@ -280,7 +288,6 @@ __device__ __forceinline__ void masked_tile_odd(const Rows& rows, const KV& kv, 
   const BlockLayout<D> lay;
   const float c = scale * kLog2e;
   BlockCopy<D, KV> copy(kv, sp, nk, b1);
-  mt_load_q(st, rows);
   pf_reset(st);
 #pragma unroll 1
   for (int b = b0; b < b1; ++b) {
@@ -303,7 +310,7 @@ __device__ __forceinline__ void masked_tile_odd(const Rows& rows, const KV& kv, 
 }
 
 // The rows of one wave against the blocks [b0, b1) of the spans.  Rows gives
-// the lane's query row (q) and what it sees (full, seen); KV the key rows (nk of
+// what the lane's row sees (full, seen), st.qf its query; KV the key rows (nk of
 // them).  As in prefill_items, slot b forms QK(b + 1) and PV(b - 1) on the matrix
 // cores beside the weights of block b.  K(b + 4) and V(b + 2) are requested in
 // slot b, into the places of K(b) and V(b - 2), which slot b - 1 was the last to
@@ -333,7 +340,6 @@ __device__ __forceinline__ bool masked_tile_fast(const Rows& rows, const KV& kv,
   copy.both(kat(1), b0 + 1, vat(1), b0 + 1);
   copy.both(kat(2), b0 + 2, vat(2), b1);
   copy.both(kat(3), b0 + 3, vat(3), b1);
-  mt_load_q(st, rows);
   pf_reset(st);
   if (n <= 0) return false;
   copy.ids(b0 + 4, b0 + 2);
@@ -425,6 +431,29 @@ __device__ __forceinline__ float mt_finish(PfState<D>& st, float scale) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) st.oacc[dt][j] *= inv;
   return l == 0.f ? -INFINITY : st.m_used * scale + logf(l);
+}
+
+// Stores the lane's row (of the two lanes that hold a row, each the half of every
+// 16 values): the halves trade four values for four, and each then stores 16
+// bytes at a time.
+template <int D>
+__device__ __forceinline__ void mt_store(const PfState<D>& st, bf16_t* row, bool valid) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+      const f32x16& o = st.oacc[dt];
+      const bf16x4 a = to_bf16x4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+      const bf16x4 b = to_bf16x4(o[4 * g + 4], o[4 * g + 5], o[4 * g + 6], o[4 * g + 7]);
+      const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
+      // lane 0..31: a's first half from itself, its second from lane + 32; the
+      // other lanes the same of b
+      const auto s0 = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+      const u32x4 w = {s0[0], s1[0], s0[1], s1[1]};
+      if (valid) *reinterpret_cast<u32x4*>(row + 32 * dt + 8 * (g + half)) = w;
+    }
 }
 
 }  // namespace rag

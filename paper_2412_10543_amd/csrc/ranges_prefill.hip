@@ -17,12 +17,12 @@ namespace rag {
 
 namespace {
 
+constexpr int kRgLast = 4;       // tiles of every sequence that are dispatched first
+
 // The lane's row, and for the wave what makes a block full.
 struct RangeRows {
-  const bf16_t* qrow;
   int shared, start, last;      // keys below shared, and start..last
   int shared_min, start_max, last_min;           // of the wave's rows
-  __device__ __forceinline__ const bf16_t* q() const { return qrow; }
   __device__ __forceinline__ bool full(int k0) const {
     return k0 + 32 <= shared_min || (k0 >= start_max && k0 + 31 <= last_min);
   }
@@ -51,23 +51,36 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void ranges_kernel(RangesArgs a, 
   __shared__ __attribute__((aligned(16))) bf16_t vring[kMtRing * BlockLayout<D>::kElems];
   __shared__ int span[3][kMtWaves];
   const int group = a.hq / a.hkv, hw = pf_heads_per_wg(group), ng = group / hw;
+  // The last kRgLast tiles of every sequence first: a prompt's query sees all its
+  // documents, and nothing else would even out a launch that ends with it.
   int xcd, local;
   xcd_slot(blockIdx.x, xcd, local);
-  const int hg = local % ng, j = local / ng % n_qt;
-  const int stream = xcd + kNumXcd * (local / ng / n_qt);
+  const int streams = (a.num_seqs * a.hkv + kNumXcd - 1) / kNumXcd;   // per XCD
+  const int hg = local % ng;
+  local /= ng;
+  const int head_n = min(n_qt, kRgLast) * streams;
+  int j, stream;
+  if (local < head_n) {
+    j = local / streams;
+    stream = xcd + kNumXcd * (local % streams);
+  } else {
+    j = kRgLast + (local - head_n) % (n_qt - kRgLast);
+    stream = xcd + kNumXcd * ((local - head_n) / (n_qt - kRgLast));
+  }
   if (stream >= a.num_seqs * a.hkv) return;
   const int s = stream / a.hkv, kvh = stream % a.hkv, h0 = kvh * group + hg * hw;
-  const int qb = a.cu_q[s], nq = a.cu_q[s + 1] - qb;
-  const int kb = a.cu_k[s], nk = a.cu_k[s + 1] - kb;
+  const int qb = uniform_load(a.cu_q, s), kb = uniform_load(a.cu_k, s);
+  const int nq = uniform_load(a.cu_q, s + 1) - qb, nk = uniform_load(a.cu_k, s + 1) - kb;
   const int rows = pf_rows_per_tile(group, kMtWaves);
-  const int q0 = (n_qt - 1 - j) * rows;          // tiles with the most keys first
-  if (q0 >= nq) return;
+  const int q0 = ((nq + rows - 1) / rows - 1 - j) * rows;
+  if (q0 < 0) return;
   const int wave = wave_id(), lane = threadIdx.x & 63, half = lane >> 5;
   const int r = q0 + 32 * (wave / hw) + (lane & 31);
   const int rc = min(r, nq - 1), head = h0 + wave % hw;
-  RangeRows rr;
-  rr.qrow = (const bf16_t*)a.q + ((size_t)(qb + rc) * a.hq + head) * D;
   const int2 rg = reinterpret_cast<const int2*>(a.ranges)[qb + rc];
+  PfState<D> st;
+  mt_load_q<D>(st, (const bf16_t*)a.q + ((size_t)(qb + rc) * a.hq + head) * D);
+  RangeRows rr;
   rr.last = min(nk - nq + rc, nk - 1);
   rr.shared = min(max(rg.x, 0), nk);
   rr.start = max(rg.y, 0);
@@ -98,19 +111,11 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void ranges_kernel(RangesArgs a, 
   const KeySpans sp = key_spans(__builtin_amdgcn_readfirstlane(a1),
                                 __builtin_amdgcn_readfirstlane(b0),
                                 __builtin_amdgcn_readfirstlane(b1));
-  PfState<D> st;
   masked_tile<D>(rr, kv, sp, 0, sp.blocks(), nk, a.scale, kring, vring, st);
   const float lse = mt_finish<D>(st, a.scale);
-  if (r >= nq) return;
-  bf16_t* o = (bf16_t*)a.o + ((size_t)(qb + r) * a.hq + head) * D + 4 * half;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<bf16x4*>(o + 32 * dt + 8 * g) =
-          to_bf16x4(st.oacc[dt][4 * g], st.oacc[dt][4 * g + 1], st.oacc[dt][4 * g + 2],
-                    st.oacc[dt][4 * g + 3]);
-  if (a.lse != nullptr && half == 0) a.lse[(size_t)head * a.cu_q[a.num_seqs] + qb + r] = lse;
+  mt_store<D>(st, (bf16_t*)a.o + ((size_t)(qb + r) * a.hq + head) * D, r < nq);
+  if (a.lse != nullptr && half == 0 && r < nq)
+    a.lse[(size_t)head * uniform_load(a.cu_q, a.num_seqs) + qb + r] = lse;
 }
 
 int64_t ranges_grid(const RangesArgs& a) {

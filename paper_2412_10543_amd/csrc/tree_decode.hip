@@ -18,10 +18,8 @@ constexpr int kTrRows = 32 * kMtWaves;
 
 // The lane's row: node and head of the group.
 struct TreeRows {
-  const bf16_t* qrow;
   const uint64_t* mask;         // the node's words
   int prior, n, words;          // keys before the nodes; nodes; words per node
-  __device__ __forceinline__ const bf16_t* q() const { return qrow; }
   __device__ __forceinline__ bool full(int k0) const { return k0 + 32 <= prior; }
   __device__ __forceinline__ uint64_t word(int w) const {
     return w >= 0 && w < words ? mask[w] : 0;
@@ -72,10 +70,10 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
   const int group = a.hq / a.hkv;
   TreeCoord t;
   if (!tree_coord(a, (a.max_nodes * group + kTrRows - 1) / kTrRows, t)) return;
-  const int qb = a.cu_q[t.s], n = a.cu_q[t.s + 1] - qb;
+  const int qb = uniform_load(a.cu_q, t.s), n = uniform_load(a.cu_q, t.s + 1) - qb;
   const int rows = n * group;
   if (t.rb * kTrRows >= rows) return;
-  const int nk = min(a.kv_lens[t.s], a.max_blocks * 16);
+  const int nk = min(uniform_load(a.kv_lens, t.s), a.max_blocks * 16);
   int pps;
   const int n_sp = tree_pieces(a, nk, pps);
   if (t.sp >= n_sp) return;
@@ -83,8 +81,9 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
   const int r = t.rb * kTrRows + 32 * wave + (lane & 31);
   const int rc = min(r, rows - 1);
   const size_t row = (size_t)(qb + rc / group) * a.hq + t.kvh * group + rc % group;
+  PfState<D> st;
+  mt_load_q<D>(st, (const bf16_t*)a.q + row * D);
   TreeRows tr;
-  tr.qrow = (const bf16_t*)a.q + row * D;
   tr.mask = a.mask + (size_t)(qb + rc / group) * a.mask_words;
   tr.prior = nk - n;
   tr.n = n;
@@ -93,22 +92,14 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
                       (const bf16_t*)a.v_cache + (size_t)t.kvh * 16 * D,
                       a.tables + (size_t)t.s * a.max_blocks, (size_t)a.hkv * 16 * D};
   const KeySpans sp = key_spans(nk, 0, 0);
-  PfState<D> st;
   masked_tile<D>(tr, kv, sp, t.sp * pps / 2, min(sp.blocks(), (t.sp + 1) * pps / 2), nk, a.scale,
                  kring, vring, st);
   const float lse = mt_finish<D>(st, a.scale);
-  if (r >= rows) return;
   if (n_sp == 1) {
-    bf16_t* o = (bf16_t*)a.o + row * D + 4 * half;
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<bf16x4*>(o + 32 * dt + 8 * g) =
-            to_bf16x4(st.oacc[dt][4 * g], st.oacc[dt][4 * g + 1], st.oacc[dt][4 * g + 2],
-                      st.oacc[dt][4 * g + 3]);
+    mt_store<D>(st, (bf16_t*)a.o + row * D, r < rows);
     return;
   }
+  if (r >= rows) return;
   float* o = a.part_o + (row * a.num_splits + t.sp) * D + 4 * half;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
