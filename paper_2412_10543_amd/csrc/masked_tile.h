@@ -15,8 +15,6 @@
 //     short list of keys does not hide, run beside the products of the other.
 #pragma once
 
-#include <type_traits>
-
 #include "common.h"
 #include "prefill_tile.h"
 
@@ -25,6 +23,10 @@ namespace rag {
 constexpr int kMtWaves = 4;
 constexpr int kMtKeys = 32;      // keys of a block
 constexpr int kMtRing = 4;       // blocks of K, and of V, in LDS
+#ifndef RAG_MT_AHEAD
+#define RAG_MT_AHEAD 3
+#endif
+constexpr int kMtAhead = RAG_MT_AHEAD;   // steps of a slot that LDS reads run ahead
 
 // Keys [0, a1) and [b0, b1) in blocks; b0 is a multiple of 32 with b0 >= a1, or
 // the second span is empty.
@@ -51,6 +53,13 @@ __device__ __forceinline__ KeySpans key_spans(int a1, int b0, int b1) {
   k.na = a1 > 0 ? (a1 + kMtKeys - 1) / kMtKeys : 0;
   return k;
 }
+
+// The full blocks of a wave: [0, a) and [lo, lo + n) of the list.
+struct FullBlocks {
+  int a, lo;
+  uint32_t n;
+  __device__ __forceinline__ bool at(int b) const { return b < a || (uint32_t)(b - lo) < n; }
+};
 
 // Element i of an array that nothing in the launch writes, i the same for the
 // wave: a scalar load.
@@ -167,106 +176,114 @@ __device__ __forceinline__ void mt_pv_odd(PfState<D>& st, const BlockLayout<D>& 
   }
 }
 
-// Copies of K and V blocks from HBM to LDS by all four waves, each kInstr
-// instructions of K and as many of V: a block inside the sequence with a scalar
-// base and per-lane 32-bit offsets, one that reaches past the last key row by
-// row, from the last (those keys are masked).  A wave's K instructions copy rows
-// of one page; the page ids that the next copies need are read beforehand (ids).
-template <int D, class KV>
+// dma16_s with the LDS address as a byte offset.
+__device__ __forceinline__ void dma16_at(const void* sbase, uint32_t voff, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(voff), "s"(sbase), "s"(lds)
+      : "memory", "m0");
+}
+
+__device__ __forceinline__ uint32_t lds_offset(const bf16_t* p) {
+  typedef __attribute__((address_space(3))) char lds_char;
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char*)p);
+}
+
+// One side (K or V) of the copies of blocks from HBM to LDS by all four waves,
+// kInstr instructions a wave and block, each with a scalar base and per-lane 32-bit
+// offsets.  Blocks are requested in the order of the spans.  What a slot copies
+// is prepared before the slot (ids, then next), as scalar instructions between the
+// products of a wave cost as much as vector ones.  Only the last block can reach
+// past the sequence's last key: its offsets then repeat that key's row (those keys
+// are masked).  Behind the last block copies go on, of one 16-byte piece of it for
+// all lanes, into places that nobody reads: the slots stay one code, and the number
+// of copies in flight one number.
+template <int D, class KV, bool kIsK>
 struct BlockCopy {
   using Lay = BlockLayout<D>;
   static constexpr int kInstr = kMtKeys * Lay::kCh / (64 * kMtWaves);
   static_assert(kInstr == 1 || kInstr == 2, "block staging layout");
+  static constexpr uint32_t kPlace = Lay::kElems * sizeof(bf16_t);
   const KV& kv;
-  const KeySpans& sp;
-  int nk, end, wave;            // keys of the sequence; blocks end here
-  int k_page, v_page;           // page in the block of the wave's first K, V instruction
-  uint32_t k_off, v_off;
-  int kid, vid[kInstr];
-  __device__ __forceinline__ BlockCopy(const KV& kv_, const KeySpans& sp_, int nk_, int end_)
-      : kv(kv_), sp(sp_), nk(nk_), end(end_), wave(wave_id()) {
-    int kr, kc, vr, vc;
-    Lay::k_src(64 * wave * kInstr, kr, kc);
-    Lay::v_src(64 * wave * kInstr, vr, vc);
-    k_page = kr >> 4;
-    v_page = vr >> 4;
-    Lay::k_src(64 * wave * kInstr + (threadIdx.x & 63), kr, kc);
-    Lay::v_src(64 * wave * kInstr + (threadIdx.x & 63), vr, vc);
-    if constexpr (KV::kPaged) {
-      k_off = (uint32_t)(((kr & 15) * D + kc * 8) * sizeof(bf16_t));
-      v_off = (uint32_t)(((vr & 15) * D + vc * 8) * sizeof(bf16_t));
-    } else {
-      k_off = (uint32_t)((kr * kv.stride + kc * 8) * sizeof(bf16_t));
-      v_off = (uint32_t)((vr * kv.stride + vc * 8) * sizeof(bf16_t));
-    }
-    kid = 0;
+  int nk, last;                 // keys of the sequence; last block
+  int page;                     // page in the block of the wave's first instruction
+  int b, na, k0, k0b;           // next block and its first key; the spans' border
+  int id[kInstr];               // its page ids (K: all of a wave's rows are in one page)
+  uint32_t off[kInstr], ring;
+  const bf16_t* base[kInstr];
+  __device__ __forceinline__ BlockCopy(const KV& kv_, const KeySpans& sp, int nk_, int b0, int b1,
+                                       const bf16_t* ring_)
+      : kv(kv_), nk(nk_), last(b1 - 1), b(b0), na(sp.na), k0(sp.key0(b0)), k0b(sp.b0) {
+    const int wave = wave_id();
+    ring = lds_offset(ring_) + 1024 * wave * kInstr;
+    int r, c;
+    src(64 * wave * kInstr, r, c);
+    page = r >> 4;
+    offsets(0, 1 << 30);
 #pragma unroll
-    for (int i = 0; i < kInstr; ++i) vid[i] = 0;
+    for (int i = 0; i < kInstr; ++i) id[i] = 0;
   }
-  // Page ids for the copies of K block bk and V block bv.
-  __device__ __forceinline__ void ids(int bk, int bv) {
-    if constexpr (KV::kPaged) {
-      const int last = (nk - 1) >> 4;
-      if (bk < end) kid = kv.page(min((sp.key0(bk) >> 4) + k_page, last));
-      if (bv < end) {
+  __device__ __forceinline__ static void src(int p, int& r, int& c) {
+    if constexpr (kIsK) Lay::k_src(p, r, c); else Lay::v_src(p, r, c);
+  }
+  // Offsets of the lane's chunks for a block that starts at key k0 of n.
+  __device__ __forceinline__ void offsets(int first, int n) {
 #pragma unroll
-        for (int i = 0; i < kInstr; ++i)
-          vid[i] = kv.page(min((sp.key0(bv) >> 4) + v_page + i, last));
+    for (int i = 0; i < kInstr; ++i) {
+      int r, c;
+      src(64 * (wave_id() * kInstr + i) + opaque_lane(), r, c);
+      r = min(r, n - 1 - first);
+      if constexpr (KV::kPaged)
+        off[i] = (uint32_t)((((first + r) & 15) * D + c * 8) * sizeof(bf16_t));
+      else
+        off[i] = (uint32_t)((r * kv.stride + c * 8) * sizeof(bf16_t));
+    }
+  }
+  // Page ids of the next block (pages past the last are the last: see offsets).
+  __device__ __forceinline__ void ids() {
+    if constexpr (KV::kPaged) {
+      const int p = (k0 >> 4) + page, lp = (nk - 1) >> 4;
+      id[0] = kv.page(min(p, lp));
+      if constexpr (kInstr == 2) id[1] = kIsK ? id[0] : kv.page(min(p + 1, lp));
+    }
+  }
+  // The next block's copies from here on.
+  __device__ __forceinline__ void next() {
+#pragma unroll
+    for (int i = 0; i < kInstr; ++i) {
+      if constexpr (KV::kPaged) {
+        asm volatile("" : "+s"(id[i]));
+        base[i] = (kIsK ? kv.k : kv.v) + kv.at(id[i], 0);
+      } else {
+        base[i] = kIsK ? kv.krow(k0) : kv.vrow(k0);
       }
     }
+    if (b >= last) end_of_list();
+    const bool more = b < last;                  // (stays at the last block)
+    const int after = b + 1 == na ? k0b : k0 + kMtKeys;
+    k0 = more ? after : k0;
+    b = more ? b + 1 : last + 1;
   }
-  // Have the ids in scalar registers here, and not where the copies are.
-  __device__ __forceinline__ void settle() {
-    if constexpr (KV::kPaged) {
-      asm volatile("" : "+s"(kid));
+  __device__ __forceinline__ void end_of_list() {
+    asm volatile("");
+    if (b > last) {
 #pragma unroll
-      for (int i = 0; i < kInstr; ++i) asm volatile("" : "+s"(vid[i]));
+      for (int i = 0; i < kInstr; ++i) off[i] = 0;
+    } else if (k0 + kMtKeys > nk) {
+      offsets(k0, nk);
     }
   }
-  __device__ __forceinline__ void k(bf16_t* place, int b, int i) const {
-    if (b >= end) return;
-    const int k0 = sp.key0(b), g = wave * kInstr + i;
-    bf16_t* dst = place + 512 * g;
-    if (k0 + kMtKeys <= nk) {
-      if constexpr (KV::kPaged)
-        dma16_s(kv.k + kv.at(kid, 0) + 32 * i, k_off, dst);
-      else
-        dma16_s(kv.krow(k0) + 32 * i, k_off, dst);
-    } else {
-      int r, c;
-      Lay::k_src(64 * g + opaque_lane(), r, c);
-      const int j = min(k0 + r, nk - 1);         // (its page: see ids)
-      if constexpr (KV::kPaged)
-        dma16(kv.k + kv.at(kid, j & 15) + 8 * c, dst);
-      else
-        dma16(kv.krow(j) + 8 * c, dst);
-    }
+  __device__ __forceinline__ void copy(int place, int i) const {
+    dma16_at(base[i], off[i], ring + place * kPlace + 1024 * i);
   }
-  __device__ __forceinline__ void v(bf16_t* place, int b, int i) const {
-    if (b >= end) return;
-    const int k0 = sp.key0(b), g = wave * kInstr + i;
-    bf16_t* dst = place + 512 * g;
-    if (k0 + kMtKeys <= nk) {
-      if constexpr (KV::kPaged)
-        dma16_s(kv.v + kv.at(vid[i], 0), v_off, dst);
-      else
-        dma16_s(kv.vrow(k0 + 16 * i), v_off, dst);
-    } else {
-      int r, c;
-      Lay::v_src(64 * g + opaque_lane(), r, c);
-      const int j = min(k0 + r, nk - 1);
-      if constexpr (KV::kPaged)
-        dma16(kv.v + kv.at(vid[i], j & 15) + 8 * c, dst);
-      else
-        dma16(kv.vrow(j) + 8 * c, dst);
-    }
-  }
-  __device__ __forceinline__ void both(bf16_t* kp, int bk, bf16_t* vp, int bv) {
-    ids(bk, bv);
+  __device__ __forceinline__ void all(int place) {
+    ids();
+    next();
 #pragma unroll
-    for (int i = 0; i < kInstr; ++i) v(vp, bv, i);
-#pragma unroll
-    for (int i = 0; i < kInstr; ++i) k(kp, bk, i);
+    for (int i = 0; i < kInstr; ++i) copy(place, i);
   }
 };
 
@@ -287,15 +304,17 @@ __device__ __forceinline__ void masked_tile_odd(const Rows& rows, const KV& kv, 
                                                 PfState<D>& st) {
   const BlockLayout<D> lay;
   const float c = scale * kLog2e;
-  BlockCopy<D, KV> copy(kv, sp, nk, b1);
+  BlockCopy<D, KV, true> kc(kv, sp, nk, b0, b1, kst);
+  BlockCopy<D, KV, false> vc(kv, sp, nk, b0, b1, vst);
   pf_reset(st);
 #pragma unroll 1
   for (int b = b0; b < b1; ++b) {
-    copy.both(kst, b, vst, b);
+    kc.all(0);
+    vc.all(0);
     __builtin_amdgcn_s_waitcnt(0x0F70);
     pf_barrier();
     const int k0 = sp.key0(b);
-    const uint32_t seen = rows.full(k0) ? 0xffffffffu : rows.seen(k0);
+    const uint32_t seen = rows.seen(k0);
     if (wave_any(seen != 0)) {
       f32x16 s = pf_qk<D, 0>(st, lay, kst);
       mt_mask(s, seen);
@@ -310,8 +329,8 @@ __device__ __forceinline__ void masked_tile_odd(const Rows& rows, const KV& kv, 
 }
 
 // The rows of one wave against the blocks [b0, b1) of the spans.  Rows gives
-// what the lane's row sees (full, seen), st.qf its query; KV the key rows (nk of
-// them).  As in prefill_items, slot b forms QK(b + 1) and PV(b - 1) on the matrix
+// what the lane's row sees (full_blocks, seen), st.qf its query; KV the key rows
+// (nk of them).  As in prefill_items, slot b forms QK(b + 1) and PV(b - 1) on the matrix
 // cores beside the weights of block b.  K(b + 4) and V(b + 2) are requested in
 // slot b, into the places of K(b) and V(b - 2), which slot b - 1 was the last to
 // read; a barrier before every slot.  Every slot is the same code, the first with
@@ -332,17 +351,21 @@ __device__ __forceinline__ bool masked_tile_fast(const Rows& rows, const KV& kv,
   const Lay lay;
   const float c = scale * kLog2e;
   const int n = b1 - b0;
-  BlockCopy<D, KV> copy(kv, sp, nk, b1);
-  constexpr int kInstr = BlockCopy<D, KV>::kInstr;
-  auto kat = [&](int i) { return kring + (i & (kMtRing - 1)) * Lay::kElems; };
-  auto vat = [&](int i) { return vring + (i & (kMtRing - 1)) * Lay::kElems; };
-  copy.both(kat(0), b0, vat(0), b0);
-  copy.both(kat(1), b0 + 1, vat(1), b0 + 1);
-  copy.both(kat(2), b0 + 2, vat(2), b1);
-  copy.both(kat(3), b0 + 3, vat(3), b1);
   pf_reset(st);
   if (n <= 0) return false;
-  copy.ids(b0 + 4, b0 + 2);
+  BlockCopy<D, KV, true> kc(kv, sp, nk, b0, b1, kring);
+  BlockCopy<D, KV, false> vc(kv, sp, nk, b0, b1, vring);
+  constexpr int kInstr = BlockCopy<D, KV, true>::kInstr;
+  auto kat = [&](int i) { return kring + (i & (kMtRing - 1)) * Lay::kElems; };
+  auto vat = [&](int i) { return vring + (i & (kMtRing - 1)) * Lay::kElems; };
+  kc.all(0);
+  vc.all(0);
+  kc.all(1);
+  vc.all(1);
+  kc.all(2);
+  kc.all(3);
+  kc.ids();
+  vc.ids();
   for (int i = threadIdx.x; i < Lay::kElems / 8; i += 64 * kMtWaves)
     *reinterpret_cast<u32x4*>(vat(3) + 8 * i) = u32x4{0, 0, 0, 0};
   // (the first product waits for Q, and with it for the copies before it)
@@ -350,13 +373,15 @@ __device__ __forceinline__ bool masked_tile_fast(const Rows& rows, const KV& kv,
   for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(st.qf[ks]));
   __builtin_amdgcn_s_waitcnt(0x0070);            // the copies and the zeros
   pf_barrier();
-  copy.settle();
+  kc.next();
+  vc.next();
 
   f32x16 sE = pf_qk<D, 0>(st, lay, kat(0)), sO = {};
   bf16x8 pE[2] = {}, pO[2] = {};
   uint32_t odd = 0;
   bool partial = false;                          // the block before was not full
-  if (!rows.full(sp.key0(b0))) mt_mask(sE, rows.seen(sp.key0(b0)));
+  const FullBlocks fb = rows.full_blocks(sp);
+  if (!fb.at(b0)) mt_mask(sE, rows.seen(sp.key0(b0)));
   float tmax = sE[0];
 #pragma unroll
   for (int j = 1; j < 16; ++j) tmax = fmaxf(tmax, sE[j]);
@@ -365,47 +390,46 @@ __device__ __forceinline__ bool masked_tile_fast(const Rows& rows, const KV& kv,
   auto slot = [&](int i, f32x16& s_cur, f32x16& s_next, bf16x8 (&p_cur)[2],
                   const bf16x8 (&p_prev)[2]) {
     if (partial) odd |= mt_look<D>(lay, vat(i - 1));
-    const int k0 = sp.key0(b0 + i);
-    partial = !rows.full(k0) || i >= n;
-    if (partial) mt_mask(s_cur, i < n ? rows.seen(k0) : 0u);
-    float sum = pf_full_slot<D, 0, 0>(
+    partial = !fb.at(b0 + i) || i >= n;
+    if (partial) mt_mask(s_cur, i < n ? rows.seen(sp.key0(b0 + i)) : 0u);
+    float sum = pf_full_slot<D, 0, 0, Lay, kMtAhead>(
         st, lay, kat(i + 1), vat(i - 1), s_cur, s_next, p_cur, p_prev, c, -st.m_used * c,
         [&](int step) {                          // V and K of later blocks, spread over the slot
           constexpr int kStep = D / 16 / (2 * kInstr);
           if (step % kStep == 0) {
             const int x = step / kStep;
             if (x < kInstr)
-              copy.v(vat(i + 2), b0 + i + 2, x);
+              vc.copy((i + 2) & (kMtRing - 1), x);
             else
-              copy.k(kat(i), b0 + i + 4, x - kInstr);
+              kc.copy(i & (kMtRing - 1), x - kInstr);
           }
         });
     if (__builtin_expect(wave_any(!(sum <= kPfSumBound)), 0)) sum = pf_reref(st, s_cur, c, p_cur);
     st.l += sum;
   };
   // Slot i + 1 needs K(i + 2) and V(i), requested in slot i - 2 at the latest.
-  auto turn = [&](int i) {
+  auto turn = [&]() {
     __builtin_amdgcn_sched_barrier(0);
-    copy.ids(b0 + i + 5, b0 + i + 3);
-    constexpr int k2 = 4 * kInstr;               // the copies of two slots
-    if (i + 4 < n)
-      __builtin_amdgcn_s_waitcnt(0x0F70 | k2);
-    else
-      __builtin_amdgcn_s_waitcnt(0x0F70);
+    kc.ids();
+    vc.ids();
+    __builtin_amdgcn_s_waitcnt(0x0F70 | 4 * kInstr);   // the copies of two slots
     pf_barrier();
-    copy.settle();
+    kc.next();
+    vc.next();
   };
   int i = 0;
   for (; i < n; i += 2) {
     slot(i, sE, sO, pE, pO);
-    turn(i);
+    turn();
     slot(i + 1, sO, sE, pO, pE);
-    turn(i + 1);
+    turn();
   }
   if (i == n) {                                  // (else the empty block was the last)
     if (partial) odd |= mt_look<D>(lay, vat(n - 1));
     pf_pv<D, 0>(st, lay, vat(n - 1), pO);
   }
+  // (no copy into LDS outlives the workgroup, or meets its next use of the rings)
+  __builtin_amdgcn_s_waitcnt(0x0F70);
   return wave_any(odd != 0);
 }
 

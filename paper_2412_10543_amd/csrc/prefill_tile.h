@@ -379,7 +379,7 @@ struct PfPipeCtx {
 struct PfNoHook {
   __device__ __forceinline__ void operator()(int) const {}
 };
-template <int D, int HK, int HV, class Lay, class Hook = PfNoHook>
+template <int D, int HK, int HV, class Lay, int kAhead = 2, class Hook = PfNoHook>
 __device__ __forceinline__ float pf_full_slot(PfState<D>& st, const Lay& lay,
                                               const bf16_t* __restrict__ kst,
                                               const bf16_t* __restrict__ vstage,
@@ -427,13 +427,13 @@ __device__ __forceinline__ float pf_full_slot(PfState<D>& st, const Lay& lay,
     }
     asm volatile("" : "+v"(sum));
   };
-  load(0);
-  if (kSteps > 1) load(1);
+#pragma unroll
+  for (int i = 0; i < kAhead && i < kSteps; ++i) load(i);
   arg(0);
   f32x16 acc = {};
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    if (i + 2 < kSteps) load(i + 2);
+    if (i + kAhead < kSteps) load(i + kAhead);
     hook(i);
     __builtin_amdgcn_sched_barrier(0);
     acc = mfma32(ka[i], st.qf[i], acc);

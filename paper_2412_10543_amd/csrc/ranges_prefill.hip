@@ -23,8 +23,10 @@ constexpr int kRgLast = 4;       // tiles of every sequence that are dispatched 
 struct RangeRows {
   int shared, start, last;      // keys below shared, and start..last
   int shared_min, start_max, last_min;           // of the wave's rows
-  __device__ __forceinline__ bool full(int k0) const {
-    return k0 + 32 <= shared_min || (k0 >= start_max && k0 + 31 <= last_min);
+  __device__ __forceinline__ FullBlocks full_blocks(const KeySpans& sp) const {
+    const int lo = (start_max + kMtKeys - 1) / kMtKeys, hi = (last_min + 1) / kMtKeys;
+    return {min(shared_min / kMtKeys, sp.na), sp.nb > 0 ? lo + sp.na - sp.b0 / kMtKeys : lo,
+            (uint32_t)max(hi - lo, 0)};
   }
   __device__ __forceinline__ uint32_t seen(int k0) const {
     return low_bits(shared - k0) | (low_bits(last + 1 - k0) & ~low_bits(start - k0));

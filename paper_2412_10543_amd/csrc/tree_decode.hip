@@ -20,7 +20,9 @@ constexpr int kTrRows = 32 * kMtWaves;
 struct TreeRows {
   const uint64_t* mask;         // the node's words
   int prior, n, words;          // keys before the nodes; nodes; words per node
-  __device__ __forceinline__ bool full(int k0) const { return k0 + 32 <= prior; }
+  __device__ __forceinline__ FullBlocks full_blocks(const KeySpans&) const {
+    return {max(prior, 0) / kMtKeys, 0, 0u};
+  }
   __device__ __forceinline__ uint64_t word(int w) const {
     return w >= 0 && w < words ? mask[w] : 0;
   }
