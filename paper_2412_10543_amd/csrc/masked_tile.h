@@ -89,13 +89,14 @@ struct BlockLayout {
   }
   __device__ __forceinline__ int k_off(int, int ks) const { return k_lane + 256 * ks; }
   __device__ __forceinline__ int v_off(int r, int dt) const { return v_lane + 1024 * dt + 32 * r; }
-  __device__ __forceinline__ static void k_src(int p, int& r, int& c) {
-    r = (p / (16 * kCh)) * 16 + (p & 15);
-    c = (p >> 4) % kCh;
+  // (row, chunk) of the block held by staged chunk p
+  __device__ __forceinline__ static void k_src(uint32_t p, int& r, int& c) {
+    r = (int)(p / (16 * kCh) * 16 + (p & 15));
+    c = (int)((p >> 4) % kCh);
   }
-  __device__ __forceinline__ static void v_src(int p, int& r, int& c) {
-    r = (p & 127) >> 2;
-    c = 4 * (p >> 7) + (p & 3);
+  __device__ __forceinline__ static void v_src(uint32_t p, int& r, int& c) {
+    r = (int)((p & 127) >> 2);
+    c = (int)(4 * (p >> 7) + (p & 3));
   }
 };
 
@@ -106,7 +107,9 @@ __device__ __forceinline__ void mt_mask(f32x16& s, uint32_t seen) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     const int key = 8 * (j >> 2) + (j & 3);      // + 4 * half
-    if (!((mine >> key) & 1)) s[j] = -INFINITY;
+    const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)mine, key, 1);   // all ones or 0
+    const uint32_t x = __float_as_uint(s[j]);
+    s[j] = __uint_as_float((x & keep) | (0xff800000u & ~keep));
   }
 }
 
@@ -258,7 +261,7 @@ struct BlockCopy {
         asm volatile("" : "+s"(id[i]));
         base[i] = (kIsK ? kv.k : kv.v) + kv.at(id[i], 0);
       } else {
-        base[i] = kIsK ? kv.krow(k0) : kv.vrow(k0);
+        base[i] = (kIsK ? kv.k : kv.v) + (size_t)((uint64_t)(uint32_t)k0 * (uint32_t)kv.stride);
       }
     }
     if (b >= last) end_of_list();
