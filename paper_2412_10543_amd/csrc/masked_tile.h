@@ -20,29 +20,29 @@
 
 namespace rag {
 
+template <int kN>
+struct MtInt {
+  static constexpr int value = kN;
+};
+
 constexpr int kMtWaves = 4;
 constexpr int kMtKeys = 32;      // keys of a block
 constexpr int kMtRing = 4;       // blocks of K, and of V, in LDS
-#ifndef RAG_MT_AHEAD
-#define RAG_MT_AHEAD 3
-#endif
-constexpr int kMtAhead = RAG_MT_AHEAD;   // steps of a slot that LDS reads run ahead
+constexpr int kMtAhead = 3;      // steps of a slot that LDS reads run ahead
 
-// Keys [0, a1) and [b0, b1) in blocks; b0 is a multiple of 32 with b0 >= a1, or
-// the second span is empty.
+// The blocks of an item: na from key a0 on, then nb from key b0 on (both multiples
+// of 32).
 struct KeySpans {
-  int na, nb;                   // blocks of each
-  int b0;
+  int a0, na, b0, nb;
   __device__ __forceinline__ int blocks() const { return na + nb; }
   __device__ __forceinline__ int key0(int b) const {
-    return b < na ? b * kMtKeys : b0 + (b - na) * kMtKeys;
+    return b < na ? a0 + b * kMtKeys : b0 + (b - na) * kMtKeys;
   }
 };
 
+// Keys [0, a1) and [b0, b1).
 __device__ __forceinline__ KeySpans key_spans(int a1, int b0, int b1) {
-  KeySpans k;
-  k.b0 = 0;
-  k.nb = 0;
+  KeySpans k{0, 0, 0, 0};
   const int b0t = b0 & ~(kMtKeys - 1);
   if (b1 > b0 && b0t <= a1) {                    // one span
     a1 = max(a1, b1);
@@ -54,11 +54,14 @@ __device__ __forceinline__ KeySpans key_spans(int a1, int b0, int b1) {
   return k;
 }
 
-// The full blocks of a wave: [0, a) and [lo, lo + n) of the list.
+// The blocks of an item that all its rows see whole: [0, a) and [lo, hi) of its
+// list.
 struct FullBlocks {
-  int a, lo;
-  uint32_t n;
-  __device__ __forceinline__ bool at(int b) const { return b < a || (uint32_t)(b - lo) < n; }
+  int a, lo, hi;
+  // How many from block b on.
+  __device__ __forceinline__ int run(int b) const {
+    return b < a ? a - b : b >= lo && b < hi ? hi - b : 0;
+  }
 };
 
 // Element i of an array that nothing in the launch writes, i the same for the
@@ -125,17 +128,17 @@ __device__ __forceinline__ uint32_t mt_odd(uint32_t x) {
   return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
 
-// Whether the wave's part of a staged V block holds an infinite or NaN value.
+// Whether the wave's quarter of a staged V block holds an infinite or NaN value
+// (a block is partial for all four waves or for none).
 template <int D>
-__device__ __forceinline__ uint32_t mt_look(const BlockLayout<D>& lay, const bf16_t* v) {
+__device__ __forceinline__ uint32_t mt_look(const bf16_t* v) {
   uint32_t odd = 0;
 #pragma unroll
-  for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) {
-      const u32x4 x = mt_v<D>(lay, v, 16 * s2, dt);
-      odd |= mt_odd(x[0]) | mt_odd(x[1]) | mt_odd(x[2]) | mt_odd(x[3]);
-    }
+  for (int i = 0; i < D / 64; ++i) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(
+        v + ((wave_id() * (D / 64) + i) * kWave + opaque_lane()) * 8);
+    odd |= mt_odd(x[0]) | mt_odd(x[1]) | mt_odd(x[2]) | mt_odd(x[3]);
+  }
   return odd;
 }
 
@@ -179,15 +182,16 @@ __device__ __forceinline__ void mt_pv_odd(PfState<D>& st, const BlockLayout<D>& 
   }
 }
 
-// dma16_s with the LDS address as a byte offset.
+// dma16_s with the LDS address as a byte offset, kPlus bytes behind lds.
+template <int kPlus>
 __device__ __forceinline__ void dma16_at(const void* sbase, uint32_t voff, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %2\n\t"
+      "s_add_u32 m0, %2, %3\n\t"
       "s_nop 0\n\t"
       "global_load_lds_dwordx4 %0, %1"
       :
-      : "v"(voff), "s"(sbase), "s"(lds)
-      : "memory", "m0");
+      : "v"(voff), "s"(sbase), "s"(lds), "n"(kPlus)
+      : "memory", "m0", "scc");
 }
 
 __device__ __forceinline__ uint32_t lds_offset(const bf16_t* p) {
@@ -195,98 +199,144 @@ __device__ __forceinline__ uint32_t lds_offset(const bf16_t* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char*)p);
 }
 
+// Slots of an item of n blocks: an even number, and at least four where another
+// item follows, whose first four K blocks are requested in the last four slots.
+__device__ __forceinline__ int mt_slots(int n, bool more) {
+  const int even = (n + 1) & ~1;
+  return more ? max(even, kMtRing) : even;
+}
+
 // One side (K or V) of the copies of blocks from HBM to LDS by all four waves,
 // kInstr instructions a wave and block, each with a scalar base and per-lane 32-bit
-// offsets.  Blocks are requested in the order of the spans.  What a slot copies
-// is prepared before the slot (ids, then next), as scalar instructions between the
-// products of a wave cost as much as vector ones.  Only the last block can reach
-// past the sequence's last key: its offsets then repeat that key's row (those keys
-// are masked).  Behind the last block copies go on, of one 16-byte piece of it for
-// all lanes, into places that nobody reads: the slots stay one code, and the number
-// of copies in flight one number.
+// offsets.  The blocks of an item are requested in the order of its spans, those
+// of the next item behind them.  What a slot copies is prepared before the slot
+// (ready, then next), and counted in runs of blocks, as scalar instructions between
+// the products of a wave cost as much as vector ones.  A block that reaches past
+// the sequence's last key repeats that key's row (those keys are masked).  Slots
+// without a block copy one 16-byte piece for all lanes, into places that nobody
+// reads: the slots stay one code, and the number of copies in flight one number.
 template <int D, class KV, bool kIsK>
 struct BlockCopy {
   using Lay = BlockLayout<D>;
   static constexpr int kInstr = kMtKeys * Lay::kCh / (64 * kMtWaves);
   static_assert(kInstr == 1 || kInstr == 2, "block staging layout");
-  static constexpr uint32_t kPlace = Lay::kElems * sizeof(bf16_t);
   const KV& kv;
-  int nk, last;                 // keys of the sequence; last block
+  int nk;                       // keys of the sequence, at least one
   int page;                     // page in the block of the wave's first instruction
-  int b, na, k0, k0b;           // next block and its first key; the spans' border
-  int id[kInstr];               // its page ids (K: all of a wave's rows are in one page)
-  uint32_t off[kInstr], ring;
-  const bf16_t* base[kInstr];
-  __device__ __forceinline__ BlockCopy(const KV& kv_, const KeySpans& sp, int nk_, int b0, int b1,
-                                       const bf16_t* ring_)
-      : kv(kv_), nk(nk_), last(b1 - 1), b(b0), na(sp.na), k0(sp.key0(b0)), k0b(sp.b0) {
+  int run;                      // blocks left of the run at hand
+  int b, n, slots, na, a0, b0;  // the item: slots begun or in the run; blocks; spans
+  int p, dp;                    // paged: the next block's first page, pages per block
+  int id[kInstr];               //   and its page ids (K: all of a wave's rows in one page)
+  const bf16_t* at;             // dense: the next block's first row,
+  uint32_t step;                //   and elements to the one behind it
+  const bf16_t* base[kInstr];   // the copies of the slot
+  uint32_t off[kInstr], usual[kInstr], ring;
+  __device__ __forceinline__ BlockCopy(const KV& kv_, int nk_, const bf16_t* ring_)
+      : kv(kv_), nk(nk_) {
     const int wave = wave_id();
     ring = lds_offset(ring_) + 1024 * wave * kInstr;
     int r, c;
     src(64 * wave * kInstr, r, c);
     page = r >> 4;
-    offsets(0, 1 << 30);
+    offsets(usual, 0, 1 << 30);
 #pragma unroll
-    for (int i = 0; i < kInstr; ++i) id[i] = 0;
+    for (int i = 0; i < kInstr; ++i) {
+      off[i] = usual[i];
+      id[i] = 0;
+    }
+    run = 0;
+    p = dp = 0;
+    at = kIsK ? kv.k : kv.v;
+    step = 0;
   }
-  __device__ __forceinline__ static void src(int p, int& r, int& c) {
-    if constexpr (kIsK) Lay::k_src(p, r, c); else Lay::v_src(p, r, c);
+  __device__ __forceinline__ void item(const KeySpans& sp, int slots_) {
+    b = 0;
+    n = sp.blocks();
+    slots = slots_;
+    na = sp.na;
+    a0 = sp.a0;
+    b0 = sp.b0;
   }
-  // Offsets of the lane's chunks for a block that starts at key k0 of n.
-  __device__ __forceinline__ void offsets(int first, int n) {
+  __device__ __forceinline__ static void src(int q, int& r, int& c) {
+    if constexpr (kIsK) Lay::k_src(q, r, c); else Lay::v_src(q, r, c);
+  }
+  // Offsets of the lane's chunks for a block that starts at key `first` of n.
+  __device__ __forceinline__ void offsets(uint32_t (&o)[kInstr], int first, int n) {
 #pragma unroll
     for (int i = 0; i < kInstr; ++i) {
       int r, c;
       src(64 * (wave_id() * kInstr + i) + opaque_lane(), r, c);
       r = min(r, n - 1 - first);
       if constexpr (KV::kPaged)
-        off[i] = (uint32_t)((((first + r) & 15) * D + c * 8) * sizeof(bf16_t));
+        o[i] = (uint32_t)((((first + r) & 15) * D + c * 8) * sizeof(bf16_t));
       else
-        off[i] = (uint32_t)((r * kv.stride + c * 8) * sizeof(bf16_t));
+        o[i] = (uint32_t)((r * kv.stride + c * 8) * sizeof(bf16_t));
     }
   }
-  // Page ids of the next block (pages past the last are the last: see offsets).
-  __device__ __forceinline__ void ids() {
+  // The run from slot b of the item on; behind its last slot the next item's
+  // (after_slots 0: there is none).
+  __device__ __forceinline__ void refill(const KeySpans& after, int after_slots) {
+    asm volatile("");
+    if (b >= slots && after_slots > 0) item(after, after_slots);
+    if (b >= n) {                                // no block
+      run = max(slots - b, 1);
+      dp = 0;
+      at = kIsK ? kv.k : kv.v;                   // (at is behind the last block by now)
+      step = 0;
+#pragma unroll
+      for (int i = 0; i < kInstr; ++i) off[i] = 0;
+    } else {
+      const bool first = b < na;
+      const int k0 = first ? a0 + b * kMtKeys : b0 + (b - na) * kMtKeys;
+      const int inside = (nk - k0) / kMtKeys;    // whole blocks
+      run = min((first ? na : n) - b, max(inside, 1));
+      p = k0 >> 4;
+      dp = kMtKeys / 16;
+      if constexpr (!KV::kPaged) {
+        at = (kIsK ? kv.k : kv.v) + (size_t)k0 * kv.stride;
+        step = (uint32_t)(kMtKeys * kv.stride);
+      }
+#pragma unroll
+      for (int i = 0; i < kInstr; ++i) off[i] = usual[i];
+      if (inside < 1) offsets(off, k0, nk);
+    }
+    b += run;
+  }
+  // Before the slot's barrier: the next block's page ids (pages past the last are
+  // the last: see offsets).
+  __device__ __forceinline__ void ready(const KeySpans& after, int after_slots) {
+    if (run == 0) refill(after, after_slots);
     if constexpr (KV::kPaged) {
-      const int p = (k0 >> 4) + page, lp = (nk - 1) >> 4;
-      id[0] = kv.page(min(p, lp));
-      if constexpr (kInstr == 2) id[1] = kIsK ? id[0] : kv.page(min(p + 1, lp));
+      const int lp = (nk - 1) >> 4;
+      id[0] = kv.page(min(p + page, lp));
+      if constexpr (kInstr == 2) id[1] = kIsK ? id[0] : kv.page(min(p + page + 1, lp));
     }
   }
-  // The next block's copies from here on.
+  // And behind it: the slot's copies are the next block's.
   __device__ __forceinline__ void next() {
+    --run;
 #pragma unroll
     for (int i = 0; i < kInstr; ++i) {
       if constexpr (KV::kPaged) {
         asm volatile("" : "+s"(id[i]));
         base[i] = (kIsK ? kv.k : kv.v) + kv.at(id[i], 0);
       } else {
-        base[i] = (kIsK ? kv.k : kv.v) + (size_t)((uint64_t)(uint32_t)k0 * (uint32_t)kv.stride);
+        base[i] = at;
       }
     }
-    if (b >= last) end_of_list();
-    const bool more = b < last;                  // (stays at the last block)
-    const int after = b + 1 == na ? k0b : k0 + kMtKeys;
-    k0 = more ? after : k0;
-    b = more ? b + 1 : last + 1;
+    if constexpr (KV::kPaged) p += dp; else at += step;
   }
-  __device__ __forceinline__ void end_of_list() {
-    asm volatile("");
-    if (b > last) {
+  // Instruction i into the place at byte `place` + kPlus of the ring.
+  template <int kPlus>
+  __device__ __forceinline__ void copy(uint32_t place, int i) const {
+    if (i == 0)
+      dma16_at<kPlus>(base[0], off[0], ring + place);
+    else
+      dma16_at<kPlus + 1024>(base[kInstr - 1], off[kInstr - 1], ring + place);
+  }
+  __device__ __forceinline__ void all(int place) const {
 #pragma unroll
-      for (int i = 0; i < kInstr; ++i) off[i] = 0;
-    } else if (k0 + kMtKeys > nk) {
-      offsets(k0, nk);
-    }
-  }
-  __device__ __forceinline__ void copy(int place, int i) const {
-    dma16_at(base[i], off[i], ring + place * kPlace + 1024 * i);
-  }
-  __device__ __forceinline__ void all(int place) {
-    ids();
-    next();
-#pragma unroll
-    for (int i = 0; i < kInstr; ++i) copy(place, i);
+    for (int i = 0; i < kInstr; ++i) copy<0>(place * Lay::kElems * sizeof(bf16_t), i);
   }
 };
 
@@ -298,26 +348,31 @@ __device__ __forceinline__ void mt_load_q(PfState<D>& st, const bf16_t* row) {
   for (int ks = 0; ks < D / 16; ++ks) st.qf[ks] = as_bf16x8(load16(q + 16 * ks));
 }
 
-// The rows of one wave against the blocks [b0, b1) of the spans, where keys that
-// some row does not see have infinite or NaN values: one block at a time.
+// The rows of one wave against the blocks of an item, where keys that some row
+// does not see have infinite or NaN values: one block at a time.  st.qf is set.
 template <int D, class Rows, class KV>
-__device__ __forceinline__ void masked_tile_odd(const Rows& rows, const KV& kv, const KeySpans& sp,
-                                                int b0, int b1, int nk, float scale,
-                                                bf16_t* __restrict__ kst, bf16_t* __restrict__ vst,
-                                                PfState<D>& st) {
+__device__ __forceinline__ void masked_item_odd(const Rows& rows, const KV& kv, const KeySpans& sp,
+                                                int nk, float scale, bf16_t* __restrict__ kst,
+                                                bf16_t* __restrict__ vst, PfState<D>& st) {
   const BlockLayout<D> lay;
   const float c = scale * kLog2e;
-  BlockCopy<D, KV, true> kc(kv, sp, nk, b0, b1, kst);
-  BlockCopy<D, KV, false> vc(kv, sp, nk, b0, b1, vst);
+  const int n = sp.blocks();
+  BlockCopy<D, KV, true> kc(kv, nk, kst);
+  BlockCopy<D, KV, false> vc(kv, nk, vst);
+  kc.item(sp, n);
+  vc.item(sp, n);
   pf_reset(st);
 #pragma unroll 1
-  for (int b = b0; b < b1; ++b) {
+  for (int b = 0; b < n; ++b) {
+    kc.ready(sp, 0);
+    vc.ready(sp, 0);
+    kc.next();
+    vc.next();
     kc.all(0);
     vc.all(0);
     __builtin_amdgcn_s_waitcnt(0x0F70);
     pf_barrier();
-    const int k0 = sp.key0(b);
-    const uint32_t seen = rows.seen(k0);
+    const uint32_t seen = rows.seen(sp.key0(b));
     if (wave_any(seen != 0)) {
       f32x16 s = pf_qk<D, 0>(st, lay, kst);
       mt_mask(s, seen);
@@ -331,132 +386,227 @@ __device__ __forceinline__ void masked_tile_odd(const Rows& rows, const KV& kv, 
   }
 }
 
-// The rows of one wave against the blocks [b0, b1) of the spans.  Rows gives
-// what the lane's row sees (full_blocks, seen), st.qf its query; KV the key rows
-// (nk of them).  As in prefill_items, slot b forms QK(b + 1) and PV(b - 1) on the matrix
-// cores beside the weights of block b.  K(b + 4) and V(b + 2) are requested in
-// slot b, into the places of K(b) and V(b - 2), which slot b - 1 was the last to
-// read; a barrier before every slot.  Every slot is the same code, the first with
-// weights and values of 0 for the block before it, the last with a product that
-// nobody reads, and an odd number of blocks with an empty one behind: with slots
-// of several kinds the accumulators had other registers in each, and the spills
-// made every slot wait for the copies (docs of 512 keys in a 5800-token prompt,
-// 16 of them: 2273 us against 1441).
-// Returns whether a key that some row of the wave does not see has an infinite
-// or NaN value: its weight of 0 has then made NaN of rows that it should not
-// reach.
-template <int D, class Rows, class KV>
-__device__ __forceinline__ bool masked_tile_fast(const Rows& rows, const KV& kv, const KeySpans& sp,
-                                                 int b0, int b1, int nk, float scale,
-                                                 bf16_t* __restrict__ kring,
-                                                 bf16_t* __restrict__ vring, PfState<D>& st) {
+// LDS of a workgroup: rings of K and V blocks, and a block of zeros.
+template <int D>
+struct MtLds {
+  bf16_t k[kMtRing * BlockLayout<D>::kElems];
+  bf16_t v[kMtRing * BlockLayout<D>::kElems];
+  bf16_t zero[BlockLayout<D>::kElems];
+};
+
+// The items of a workgroup, one after another: 128 (row, head) pairs each, 32 of
+// them a wave's, against the blocks of the item's spans.  All items are of one
+// sequence and kv head (kv, of nk >= 1 keys).  Src:
+//   count               items
+//   Rows rows           of the item settled last: what the lane's row sees
+//   fetch(m)            requests what item m's rows and spans follow from
+//   settle(m)           the spans of item m, from what was fetched last, and rows
+//   q(m)                the lane's query row
+//   store(m, st, l, scale)   writes the lane's row, of sum of weights l
+// As in prefill_items, slot i of an item forms QK(i + 1) and PV(i - 1) on the
+// matrix cores beside the weights of block i.  K(i + 4) and V(i + 2) are requested
+// in slot i, into the places of K(i) and V(i - 2), which slot i - 1 was the last to
+// read; a barrier before every slot.  The last slots of an item request the first
+// blocks of the next, so that between items only its queries are waited for
+// (beside the other workgroup's products).  Every slot is the same code, the
+// first with zeros as the values of the block before it, and slots without a
+// block (their number is even) with weights of 0: with slots of several kinds the
+// accumulators had other registers in each, and the spills made every slot wait
+// for the copies (16 prompts of 5800 tokens in documents of 456: 2273 us against
+// 1441).
+// Returns the items (a bit each) where a key that some row of the wave does not
+// see has an infinite or NaN value: its weight of 0 has then made NaN of rows that
+// it should not reach.
+template <int D, class Src, class KV>
+__device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, int nk, float scale,
+                                                      MtLds<D>& lds) {
   using Lay = BlockLayout<D>;
   const Lay lay;
   const float c = scale * kLog2e;
-  const int n = b1 - b0;
-  pf_reset(st);
-  if (n <= 0) return false;
-  BlockCopy<D, KV, true> kc(kv, sp, nk, b0, b1, kring);
-  BlockCopy<D, KV, false> vc(kv, sp, nk, b0, b1, vring);
+  PfState<D> st;
+  src.fetch(0);
+  mt_load_q<D>(st, src.q(0));
+  KeySpans sp = src.settle(0), sp_next{0, 0, 0, 0};
+  auto rows = src.rows;
+  auto rows_next = rows;
+  int slots = mt_slots(sp.blocks(), src.count > 1), slots_next = 0;
+  BlockCopy<D, KV, true> kc(kv, nk, lds.k);
+  BlockCopy<D, KV, false> vc(kv, nk, lds.v);
+  kc.item(sp, slots);
+  vc.item(sp, slots);
   constexpr int kInstr = BlockCopy<D, KV, true>::kInstr;
-  auto kat = [&](int i) { return kring + (i & (kMtRing - 1)) * Lay::kElems; };
-  auto vat = [&](int i) { return vring + (i & (kMtRing - 1)) * Lay::kElems; };
-  kc.all(0);
-  vc.all(0);
-  kc.all(1);
-  vc.all(1);
-  kc.all(2);
-  kc.all(3);
-  kc.ids();
-  vc.ids();
+  if (src.count > 1) src.fetch(1);
+#pragma unroll
+  for (int i = 0; i < kMtRing; ++i) {
+    kc.ready(sp, 0);
+    kc.next();
+    kc.all(i);
+    if (i < 2) {
+      vc.ready(sp, 0);
+      vc.next();
+      vc.all(i);
+    }
+  }
   for (int i = threadIdx.x; i < Lay::kElems / 8; i += 64 * kMtWaves)
-    *reinterpret_cast<u32x4*>(vat(3) + 8 * i) = u32x4{0, 0, 0, 0};
+    *reinterpret_cast<u32x4*>(lds.zero + 8 * i) = u32x4{0, 0, 0, 0};
   // (the first product waits for Q, and with it for the copies before it)
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(st.qf[ks]));
+  if (src.count > 1) {
+    sp_next = src.settle(1);
+    rows_next = src.rows;
+    slots_next = mt_slots(sp_next.blocks(), src.count > 2);
+    if (src.count > 2) src.fetch(2);
+  }
+  kc.ready(sp_next, slots_next);
+  vc.ready(sp_next, slots_next);
   __builtin_amdgcn_s_waitcnt(0x0070);            // the copies and the zeros
   pf_barrier();
   kc.next();
   vc.next();
 
-  f32x16 sE = pf_qk<D, 0>(st, lay, kat(0)), sO = {};
-  bf16x8 pE[2] = {}, pO[2] = {};
-  uint32_t odd = 0;
-  bool partial = false;                          // the block before was not full
-  const FullBlocks fb = rows.full_blocks(sp);
-  if (!fb.at(b0)) mt_mask(sE, rows.seen(sp.key0(b0)));
-  float tmax = sE[0];
+  uint32_t odd_items = 0;
+  // Places r, r + 1 and r + 2, r + 3 (mod 4) of the rings, in elements: slot i of
+  // an even i has K(i) and V(i) in the first.
+  constexpr int kE = Lay::kElems;
+  int ra = 0, rb = 2 * kE;
+  f32x16 sE, sO = {};
+  bf16x8 pE[2] = {}, pO[2];
+#pragma unroll 1
+  for (int m = 0;; ++m) {
+    const int n = sp.blocks();
+    const FullBlocks fb = rows.full_blocks(sp);
+    int run = min(fb.run(0), n);                 // blocks from the slot's on that are full
+    uint32_t odd = 0;
+    bool partial = false;                        // the block before was not full, and was there
+    pf_reset(st);
+    pO[0] = pO[1] = bf16x8{};                    // (the last item's may be NaN, and times 0 stay so)
+    sE = pf_qk<D, 0>(st, lay, lds.k + ra);
+    if (run == 0) mt_mask(sE, n == 0 ? 0u : rows.seen(sp.key0(0)));
+    float tmax = sE[0];
 #pragma unroll
-  for (int j = 1; j < 16; ++j) tmax = fmaxf(tmax, sE[j]);
-  st.m_used = max_halves(tmax);
-  // Block b0 + i with scores s_cur.
-  auto slot = [&](int i, f32x16& s_cur, f32x16& s_next, bf16x8 (&p_cur)[2],
-                  const bf16x8 (&p_prev)[2]) {
-    if (partial) odd |= mt_look<D>(lay, vat(i - 1));
-    partial = !fb.at(b0 + i) || i >= n;
-    if (partial) mt_mask(s_cur, i < n ? rows.seen(sp.key0(b0 + i)) : 0u);
-    float sum = pf_full_slot<D, 0, 0, Lay, kMtAhead>(
-        st, lay, kat(i + 1), vat(i - 1), s_cur, s_next, p_cur, p_prev, c, -st.m_used * c,
-        [&](int step) {                          // V and K of later blocks, spread over the slot
-          constexpr int kStep = D / 16 / (2 * kInstr);
-          if (step % kStep == 0) {
-            const int x = step / kStep;
-            if (x < kInstr)
-              vc.copy((i + 2) & (kMtRing - 1), x);
-            else
-              kc.copy(i & (kMtRing - 1), x - kInstr);
-          }
-        });
-    if (__builtin_expect(wave_any(!(sum <= kPfSumBound)), 0)) sum = pf_reref(st, s_cur, c, p_cur);
-    st.l += sum;
-  };
-  // Slot i + 1 needs K(i + 2) and V(i), requested in slot i - 2 at the latest.
-  auto turn = [&]() {
-    __builtin_amdgcn_sched_barrier(0);
-    kc.ids();
-    vc.ids();
-    __builtin_amdgcn_s_waitcnt(0x0F70 | 4 * kInstr);   // the copies of two slots
-    pf_barrier();
-    kc.next();
-    vc.next();
-  };
-  int i = 0;
-  for (; i < n; i += 2) {
-    slot(i, sE, sO, pE, pO);
+    for (int j = 1; j < 16; ++j) tmax = fmaxf(tmax, sE[j]);
+    st.m_used = max_halves(tmax);
+    const bool more = m + 1 < src.count;
+    // Block i with scores s_cur; the next block's K, the last one's V.
+    auto slot = [&](int i, f32x16& s_cur, f32x16& s_next, bf16x8 (&p_cur)[2],
+                    const bf16x8 (&p_prev)[2], const bf16_t* kst, const bf16_t* vst,
+                    const auto& hook) {
+      if (partial) odd |= mt_look<D>(vst);
+      partial = false;
+      if (run > 0) {
+        --run;
+      } else {
+        asm volatile("");
+        partial = i < n;
+        mt_mask(s_cur, partial ? rows.seen(sp.key0(i)) : 0u);
+        run = max(min(fb.run(i + 1), n - i - 1), 0);
+      }
+      float sum = pf_full_slot<D, 0, 0, Lay, kMtAhead>(st, lay, kst, vst, s_cur, s_next, p_cur,
+                                                       p_prev, c, -st.m_used * c, hook);
+      if (__builtin_expect(wave_any(!(sum <= kPfSumBound)), 0)) sum = pf_reref(st, s_cur, c, p_cur);
+      st.l += sum;
+    };
+    // V(i + 2) and K(i + 4), spread over slot i.
+    auto copies = [&](auto plus, uint32_t kplace, uint32_t vplace) {
+      return [&kc, &vc, kplace, vplace](int step) {
+        constexpr int kPlus = decltype(plus)::value, kStep = D / 16 / (2 * kInstr);
+        if (step % kStep == 0) {
+          const int x = step / kStep;
+          if (x < kInstr)
+            vc.template copy<kPlus>(vplace, x);
+          else
+            kc.template copy<kPlus>(kplace, x - kInstr);
+        }
+      };
+    };
+    // Slot i + 1 needs K(i + 2) and V(i), requested in slot i - 2 at the latest.
+    auto turn = [&]() {
+      __builtin_amdgcn_sched_barrier(0);
+      kc.ready(sp_next, slots_next);
+      vc.ready(sp_next, slots_next);
+      __builtin_amdgcn_s_waitcnt(0x0F70 | 4 * kInstr);   // the copies of two slots
+      pf_barrier();
+      kc.next();
+      vc.next();
+    };
+    constexpr int kBytes = kE * sizeof(bf16_t);
+#pragma unroll 1
+    for (int i = 0; i < slots; i += 2) {
+      if (i > 0) turn();
+      slot(i, sE, sO, pE, pO, lds.k + ra + kE, i == 0 || i > n ? lds.zero : lds.v + rb + kE,
+           copies(MtInt<0>{}, ra * sizeof(bf16_t), rb * sizeof(bf16_t)));
+      turn();
+      slot(i + 1, sO, sE, pO, pE, lds.k + rb, i + 1 > n ? lds.zero : lds.v + ra,
+           copies(MtInt<kBytes>{}, ra * sizeof(bf16_t), rb * sizeof(bf16_t)));
+      const int t = ra;
+      ra = rb;
+      rb = t;
+    }
+    // The copies are in the next item by now (an item has four slots), and may go on
+    // to the one behind it.
+    const KeySpans sp1 = sp_next;
+    const auto rows1 = rows_next;
+    const int slots1 = slots_next;
+    slots_next = 0;
+    if (m + 2 < src.count) {
+      sp_next = src.settle(m + 2);
+      rows_next = src.rows;
+      slots_next = mt_slots(sp_next.blocks(), m + 3 < src.count);
+      if (m + 3 < src.count) src.fetch(m + 3);
+    }
     turn();
-    slot(i + 1, sO, sE, pO, pE);
-    turn();
-  }
-  if (i == n) {                                  // (else the empty block was the last)
-    if (partial) odd |= mt_look<D>(lay, vat(n - 1));
-    pf_pv<D, 0>(st, lay, vat(n - 1), pO);
+    if (n == slots && n > 0) {                   // (else the last block's was in a slot)
+      if (partial) odd |= mt_look<D>(lds.v + rb + kE);
+      pf_pv<D, 0>(st, lay, lds.v + rb + kE, pO);
+    }
+    if (wave_any(odd != 0)) odd_items |= 1u << m;
+    if (more) mt_load_q<D>(st, src.q(m + 1));
+    src.store(m, st, mt_finish<D>(st), scale);
+    if (!more) break;
+    sp = sp1;
+    rows = rows1;
+    slots = slots1;
   }
   // (no copy into LDS outlives the workgroup, or meets its next use of the rings)
   __builtin_amdgcn_s_waitcnt(0x0F70);
-  return wave_any(odd != 0);
+  return odd_items;
 }
 
-// masked_tile_fast, and masked_tile_odd for the workgroup where a wave needs it.
-template <int D, class Rows, class KV>
-__device__ __forceinline__ void masked_tile(const Rows& rows, const KV& kv, const KeySpans& sp,
-                                            int b0, int b1, int nk, float scale,
-                                            bf16_t* __restrict__ kring, bf16_t* __restrict__ vring,
-                                            PfState<D>& st) {
-  const bool odd = masked_tile_fast<D>(rows, kv, sp, b0, b1, nk, scale, kring, vring, st);
-  if (__builtin_expect(__syncthreads_or(odd), 0))
-    masked_tile_odd<D>(rows, kv, sp, b0, b1, nk, scale, kring, vring, st);
+// masked_items_fast, and the items again that need it (of any wave).
+template <int D, class Src, class KV>
+__device__ __forceinline__ void masked_items(Src& src, const KV& kv, int nk, float scale,
+                                             MtLds<D>& lds) {
+  const uint32_t odd = masked_items_fast<D>(src, kv, nk, scale, lds);
+  if (__builtin_expect(!__syncthreads_or(odd != 0), 1)) return;
+  asm volatile("");
+#pragma unroll 1
+  for (int m = 0; m < src.count; ++m) {
+    if (!__syncthreads_or(odd >> m & 1)) continue;
+    PfState<D> st;
+    src.fetch(m);
+    mt_load_q<D>(st, src.q(m));
+    const KeySpans sp = src.settle(m);
+    masked_item_odd<D>(src.rows, kv, sp, nk, scale, lds.k, lds.v, st);
+    src.store(m, st, mt_finish<D>(st), scale);
+  }
 }
 
 // A row's normalised output, element j of d tile dt at
-// d = 32 dt + 8 (j / 4) + 4 half + j % 4, and its log-sum-exp.
+// d = 32 dt + 8 (j / 4) + 4 half + j % 4; returns its sum of weights.
 template <int D>
-__device__ __forceinline__ float mt_finish(PfState<D>& st, float scale) {
+__device__ __forceinline__ float mt_finish(PfState<D>& st) {
   const float l = st.l + wave_xor(st.l, 32);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int j = 0; j < 16; ++j) st.oacc[dt][j] *= inv;
+  return l;
+}
+// And its log-sum-exp.
+template <int D>
+__device__ __forceinline__ float mt_lse(const PfState<D>& st, float l, float scale) {
   return l == 0.f ? -INFINITY : st.m_used * scale + logf(l);
 }
 

@@ -18,20 +18,11 @@ namespace rag {
 namespace {
 
 constexpr int kRgLast = 4;       // tiles of every sequence that are dispatched first
-
-// The lane's row, and for the wave what makes a block full.
-struct RangeRows {
-  int shared, start, last;      // keys below shared, and start..last
-  int shared_min, start_max, last_min;           // of the wave's rows
-  __device__ __forceinline__ FullBlocks full_blocks(const KeySpans& sp) const {
-    const int lo = (start_max + kMtKeys - 1) / kMtKeys, hi = (last_min + 1) / kMtKeys;
-    return {min(shared_min / kMtKeys, sp.na), sp.nb > 0 ? lo + sp.na - sp.b0 / kMtKeys : lo,
-            (uint32_t)max(hi - lo, 0)};
-  }
-  __device__ __forceinline__ uint32_t seen(int k0) const {
-    return low_bits(shared - k0) | (low_bits(last + 1 - k0) & ~low_bits(start - k0));
-  }
-};
+// Of the others a workgroup takes kRgItems where there are at least kRgMany (eight
+// for each place of the GPU): 21800 tiles of 14 blocks 955 us one by one, 912 by
+// twos, 914 by fours; but 1024 rows with 8192 keys 163 us one by one, 526 by fours.
+constexpr int kRgItems = 2;
+constexpr int64_t kRgMany = 4096;
 
 // Maximum over the wave of values from 0 on.
 __device__ __forceinline__ int wave_max(int x) {
@@ -43,99 +34,179 @@ __device__ __forceinline__ int wave_max(int x) {
   x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));   // row_bcast:31
   return __builtin_amdgcn_readlane(x, 63);
 }
-__device__ __forceinline__ int wave_min(int x) { return INT_MAX - wave_max(INT_MAX - x); }
+
+// What a row sees: keys below shared, and start..last (start kNoStart: none).
+constexpr int kNoStart = 1 << 30;
+struct RowRange {
+  int shared, start;
+};
+__device__ __forceinline__ RowRange row_range(int2 r, int last, int nk) {
+  return {min(max(r.x, 0), nk), r.y > last || last < 0 ? kNoStart : max(r.y, 0)};
+}
+
+// The lane's row, and for the tile's rows what makes a block full.
+struct RangeRows {
+  RowRange r;
+  int last;
+  int shared_min, start_max, last_min;
+  __device__ __forceinline__ FullBlocks full_blocks(const KeySpans& sp) const {
+    const int by = sp.nb > 0 ? sp.na - sp.b0 / kMtKeys : 0;
+    return {min(shared_min / kMtKeys, sp.na), (start_max + kMtKeys - 1) / kMtKeys + by,
+            (last_min + 1) / kMtKeys + by};
+  }
+  __device__ __forceinline__ uint32_t seen(int k0) const {
+    return low_bits(r.shared - k0) | (low_bits(last + 1 - k0) & ~low_bits(r.start - k0));
+  }
+};
+
+// Smallest and largest of a value from 0 on over the wave; mostly it is one.
+__device__ __forceinline__ void wave_bounds(int x, int y, int& lo, int& hi) {
+  lo = hi = __builtin_amdgcn_readfirstlane(x);
+  if (__builtin_amdgcn_ballot_w64(x != lo || y != lo) != 0) {
+    lo = INT_MAX - wave_max(INT_MAX - min(x, y));
+    hi = wave_max(max(x, y));
+  }
+}
+
+// Query tiles t0, t0 + 1, ... of one sequence and head group.
+template <int D>
+struct RangeSrc {
+  using Rows = RangeRows;
+  const RangesArgs& a;
+  int count, t0, qb, nq, nk, h0, hw, tile_rows;
+  Rows rows;
+  int2 own, some, more;         // ranges of the lane's row, and of the tile's rows
+  __device__ __forceinline__ int row(int m) const {
+    return (t0 + m) * tile_rows + 32 * (wave_id() / hw) + (opaque_lane() & 31);
+  }
+  __device__ __forceinline__ int2 range(int r) const {
+    return reinterpret_cast<const int2*>(a.ranges)[qb + min(r, nq - 1)];
+  }
+  __device__ __forceinline__ void fetch(int m) {
+    own = range(row(m));
+    if (tile_rows > 32) some = range((t0 + m) * tile_rows + opaque_lane());
+    if (tile_rows > 64) more = range((t0 + m) * tile_rows + 64 + opaque_lane());
+  }
+  __device__ __forceinline__ int last_key(int r) const {   // of row r's own range
+    return min(nk - nq + min(r, nq - 1), nk - 1);
+  }
+  __device__ __forceinline__ KeySpans settle(int m) {
+    const int r0 = (t0 + m) * tile_rows;
+    rows.last = last_key(row(m));
+    rows.r = row_range(own, rows.last, nk);
+    RowRange lo = rows.r, hi = rows.r;           // the tile's rows
+    auto join = [&](int2 r, int i) {
+      const RowRange x = row_range(r, last_key(r0 + i), nk);
+      lo = {min(lo.shared, x.shared), min(lo.start, x.start)};
+      hi = {max(hi.shared, x.shared), max(hi.start, x.start)};
+    };
+    if (tile_rows > 32) join(some, opaque_lane());
+    if (tile_rows > 64) join(more, 64 + opaque_lane());
+    int shared_max, start_min;
+    wave_bounds(lo.shared, hi.shared, rows.shared_min, shared_max);
+    wave_bounds(lo.start, hi.start, start_min, rows.start_max);
+    rows.last_min = last_key(r0);
+    return key_spans(shared_max, start_min, last_key(r0 + tile_rows - 1) + 1);
+  }
+  __device__ __forceinline__ size_t out(int m) const {
+    return (size_t)(qb + min(row(m), nq - 1)) * a.hq + h0 + wave_id() % hw;
+  }
+  __device__ __forceinline__ const bf16_t* q(int m) const { return (const bf16_t*)a.q + out(m) * D; }
+  __device__ __forceinline__ void store(int m, const PfState<D>& st, float l, float scale) const {
+    const int r = row(m);
+    mt_store<D>(st, (bf16_t*)a.o + out(m) * D, r < nq);
+    if (a.lse != nullptr) {
+      const float lse = mt_lse(st, l, scale);
+      if (opaque_lane() < 32 && r < nq)
+        a.lse[(size_t)(h0 + wave_id() % hw) * uniform_load(a.cu_q, a.num_seqs) + qb + r] = lse;
+    }
+  }
+};
 
 }  // namespace
 
+// Workgroups of a (sequence, kv head, head group): min(n_qt, kRgLast) for the last
+// tiles, one each, dispatched first for all of them (a prompt's query sees all its
+// documents, and nothing else would even out a launch that ends with it); then one
+// for every `items` others.
+__host__ __device__ constexpr int ranges_groups(int n_qt, int items) {
+  return n_qt <= kRgLast ? n_qt : kRgLast + (n_qt - kRgLast + items - 1) / items;
+}
+
 template <int D>
-__global__ __launch_bounds__(64 * kMtWaves, 2) void ranges_kernel(RangesArgs a, int n_qt) {
-  __shared__ __attribute__((aligned(16))) bf16_t kring[kMtRing * BlockLayout<D>::kElems];
-  __shared__ __attribute__((aligned(16))) bf16_t vring[kMtRing * BlockLayout<D>::kElems];
-  __shared__ int span[3][kMtWaves];
+__global__ __launch_bounds__(64 * kMtWaves, 2) void ranges_kernel(RangesArgs a, int n_qt, int items) {
+  __shared__ __attribute__((aligned(16))) MtLds<D> lds;
   const int group = a.hq / a.hkv, hw = pf_heads_per_wg(group), ng = group / hw;
-  // The last kRgLast tiles of every sequence first: a prompt's query sees all its
-  // documents, and nothing else would even out a launch that ends with it.
   int xcd, local;
   xcd_slot(blockIdx.x, xcd, local);
   const int streams = (a.num_seqs * a.hkv + kNumXcd - 1) / kNumXcd;   // per XCD
   const int hg = local % ng;
   local /= ng;
-  const int head_n = min(n_qt, kRgLast) * streams;
-  int j, stream;
-  if (local < head_n) {
+  const int first = min(n_qt, kRgLast) * streams;
+  int j, stream, count = 1;
+  if (local < first) {
     j = local / streams;
     stream = xcd + kNumXcd * (local % streams);
   } else {
-    j = kRgLast + (local - head_n) % (n_qt - kRgLast);
-    stream = xcd + kNumXcd * ((local - head_n) / (n_qt - kRgLast));
+    const int per = ranges_groups(n_qt, items) - kRgLast;
+    j = kRgLast + (local - first) % per * items;
+    count = items;
+    stream = xcd + kNumXcd * ((local - first) / per);
   }
   if (stream >= a.num_seqs * a.hkv) return;
-  const int s = stream / a.hkv, kvh = stream % a.hkv, h0 = kvh * group + hg * hw;
+  const int s = stream / a.hkv, kvh = stream % a.hkv;
   const int qb = uniform_load(a.cu_q, s), kb = uniform_load(a.cu_k, s);
   const int nq = uniform_load(a.cu_q, s + 1) - qb, nk = uniform_load(a.cu_k, s + 1) - kb;
   const int rows = pf_rows_per_tile(group, kMtWaves);
-  const int q0 = ((nq + rows - 1) / rows - 1 - j) * rows;
-  if (q0 < 0) return;
-  const int wave = wave_id(), lane = threadIdx.x & 63, half = lane >> 5;
-  const int r = q0 + 32 * (wave / hw) + (lane & 31);
-  const int rc = min(r, nq - 1), head = h0 + wave % hw;
-  const int2 rg = reinterpret_cast<const int2*>(a.ranges)[qb + rc];
-  PfState<D> st;
-  mt_load_q<D>(st, (const bf16_t*)a.q + ((size_t)(qb + rc) * a.hq + head) * D);
-  RangeRows rr;
-  rr.last = min(nk - nq + rc, nk - 1);
-  rr.shared = min(max(rg.x, 0), nk);
-  rr.start = max(rg.y, 0);
-  if (rr.start > rr.last) {                      // nothing of its own
-    rr.start = nk;
-    rr.last = -1;
-  }
-  rr.shared_min = wave_min(rr.shared);
-  rr.start_max = wave_max(rr.start);
-  rr.last_min = wave_min(rr.last + 1) - 1;
-  const int shared_max = wave_max(rr.shared), start_min = wave_min(rr.start);
-  const int last_max = wave_max(rr.last + 1) - 1;
-  if (lane == 0) {
-    span[0][wave] = shared_max;
-    span[1][wave] = start_min;
-    span[2][wave] = last_max;
-  }
-  __syncthreads();
-  int a1 = 0, b0 = nk, b1 = 0;
-#pragma unroll
-  for (int w = 0; w < kMtWaves; ++w) {
-    a1 = max(a1, span[0][w]);
-    b0 = min(b0, span[1][w]);
-    b1 = max(b1, span[2][w] + 1);
+  // tiles j .. j + count - 1 from the sequence's end, in ascending order
+  const int last = (nq + rows - 1) / rows - 1 - j;
+  if (last < 0) return;
+  RangeSrc<D> src{a};
+  src.count = min(count, last + 1);
+  src.t0 = last + 1 - src.count;
+  src.qb = qb;
+  src.nq = nq;
+  src.nk = nk;
+  src.h0 = kvh * group + hg * hw;
+  src.hw = hw;
+  src.tile_rows = rows;
+  if (nk <= 0) {                                 // no key: nothing to copy from
+    PfState<D> st;
+    pf_reset(st);
+    for (int m = 0; m < src.count; ++m) src.store(m, st, 0.f, a.scale);
+    return;
   }
   const DenseKV kv{(const bf16_t*)a.k + ((size_t)kb * a.hkv + kvh) * D,
                    (const bf16_t*)a.v + ((size_t)kb * a.hkv + kvh) * D, (size_t)a.hkv * D};
-  const KeySpans sp = key_spans(__builtin_amdgcn_readfirstlane(a1),
-                                __builtin_amdgcn_readfirstlane(b0),
-                                __builtin_amdgcn_readfirstlane(b1));
-  masked_tile<D>(rr, kv, sp, 0, sp.blocks(), nk, a.scale, kring, vring, st);
-  const float lse = mt_finish<D>(st, a.scale);
-  mt_store<D>(st, (bf16_t*)a.o + ((size_t)(qb + r) * a.hq + head) * D, r < nq);
-  if (a.lse != nullptr && half == 0 && r < nq)
-    a.lse[(size_t)head * uniform_load(a.cu_q, a.num_seqs) + qb + r] = lse;
+  masked_items<D>(src, kv, nk, a.scale, lds);
+}
+
+static int ranges_tiles(const RangesArgs& a) {
+  const int rows = pf_rows_per_tile(a.hq / a.hkv, kMtWaves);
+  return (int)((a.max_seqlen_q + (int64_t)rows - 1) / rows);
+}
+
+static int ranges_items(const RangesArgs& a) {
+  const int group = a.hq / a.hkv, ng = group / pf_heads_per_wg(group);
+  const int64_t tiles = (int64_t)(ranges_tiles(a) - kRgLast) * a.num_seqs * a.hkv * ng;
+  return tiles >= kRgMany ? kRgItems : 1;
 }
 
 int64_t ranges_grid(const RangesArgs& a) {
-  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kMtWaves);
-  const int64_t n_qt = (a.max_seqlen_q + (int64_t)rows - 1) / rows;
+  const int group = a.hq / a.hkv;
   const int64_t streams = (int64_t)a.num_seqs * a.hkv;
-  return (streams + kNumXcd - 1) / kNumXcd * kNumXcd * n_qt * (group / pf_heads_per_wg(group));
+  return (streams + kNumXcd - 1) / kNumXcd * kNumXcd *
+         ranges_groups(ranges_tiles(a), ranges_items(a)) * (group / pf_heads_per_wg(group));
 }
 
 hipError_t launch_ranges(const RangesArgs& a, hipStream_t stream) {
-  const int group = a.hq / a.hkv, rows = pf_rows_per_tile(group, kMtWaves);
-  const int n_qt = (a.max_seqlen_q + rows - 1) / rows;
   const int64_t grid = ranges_grid(a);
   if (grid == 0) return hipSuccess;
-  if (a.d == 64)
-    hipLaunchKernelGGL(ranges_kernel<64>, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a, n_qt);
-  else
-    hipLaunchKernelGGL(ranges_kernel<128>, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a, n_qt);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a,
+                       ranges_tiles(a), ranges_items(a));
+  };
+  a.d == 64 ? go(ranges_kernel<64>) : go(ranges_kernel<128>);
   return hipGetLastError();
 }
 

@@ -16,12 +16,12 @@ namespace {
 
 constexpr int kTrRows = 32 * kMtWaves;
 
-// The lane's row: node and head of the group.
+// What the lane's row sees.
 struct TreeRows {
-  const uint64_t* mask;         // the node's words
+  const uint64_t* mask;         // its node's words
   int prior, n, words;          // keys before the nodes; nodes; words per node
-  __device__ __forceinline__ FullBlocks full_blocks(const KeySpans&) const {
-    return {max(prior, 0) / kMtKeys, 0, 0u};
+  __device__ __forceinline__ FullBlocks full_blocks(const KeySpans& sp) const {
+    return {max(prior - sp.a0, 0) / kMtKeys, 0, 0};
   }
   __device__ __forceinline__ uint64_t word(int w) const {
     return w >= 0 && w < words ? mask[w] : 0;
@@ -33,6 +33,52 @@ struct TreeRows {
     if (b > 32) x |= word(w + 1) << (64 - b);
     const uint32_t nodes = (uint32_t)x & low_bits(n - j0);
     return low_bits(-j0) | (nodes & ~low_bits(-j0));
+  }
+};
+
+// The rows of a unit (one item): (node, q head of the group) pairs r0 + 32 wave on.
+template <int D>
+struct TreeSrc {
+  const TreeArgs& a;
+  static constexpr int count = 1;
+  int qb, n, group, h0, r0, kv_len, sp, n_sp;
+  KeySpans spans;
+  TreeRows rows;
+  __device__ __forceinline__ int row() const {
+    return r0 + 32 * wave_id() + (opaque_lane() & 31);
+  }
+  __device__ __forceinline__ size_t out() const {         // (query row, q head)
+    const int r = min(row(), n * group - 1);
+    return (size_t)(qb + r / group) * a.hq + h0 + r % group;
+  }
+  __device__ __forceinline__ void fetch(int) {}
+  __device__ __forceinline__ KeySpans settle(int) {
+    rows.mask = a.mask + (size_t)(qb + min(row(), n * group - 1) / group) * a.mask_words;
+    rows.prior = kv_len - n;
+    rows.n = n;
+    rows.words = a.mask_words;
+    return spans;
+  }
+  __device__ __forceinline__ const bf16_t* q(int) const { return (const bf16_t*)a.q + out() * D; }
+  __device__ __forceinline__ void store(int, const PfState<D>& st, float l, float scale) const {
+    const bool valid = row() < n * group;
+    const size_t x = out();
+    if (n_sp == 1) {
+      mt_store<D>(st, (bf16_t*)a.o + x * D, valid);
+      return;
+    }
+    const float lse = mt_lse(st, l, scale);
+    if (!valid) return;
+    const int half = opaque_lane() >> 5;
+    float* o = a.part_o + (x * a.num_splits + sp) * D + 4 * half;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(o + 32 * dt + 8 * g) =
+            f32x4{st.oacc[dt][4 * g], st.oacc[dt][4 * g + 1], st.oacc[dt][4 * g + 2],
+                  st.oacc[dt][4 * g + 3]};
+    if (half == 0) a.part_lse[x * a.num_splits + sp] = lse;
   }
 };
 
@@ -67,50 +113,29 @@ __device__ __forceinline__ int tree_pieces(const TreeArgs& a, int kv_len, int& p
 
 template <int D>
 __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
-  __shared__ __attribute__((aligned(16))) bf16_t kring[kMtRing * BlockLayout<D>::kElems];
-  __shared__ __attribute__((aligned(16))) bf16_t vring[kMtRing * BlockLayout<D>::kElems];
+  __shared__ __attribute__((aligned(16))) MtLds<D> lds;
   const int group = a.hq / a.hkv;
   TreeCoord t;
   if (!tree_coord(a, (a.max_nodes * group + kTrRows - 1) / kTrRows, t)) return;
-  const int qb = uniform_load(a.cu_q, t.s), n = uniform_load(a.cu_q, t.s + 1) - qb;
-  const int rows = n * group;
-  if (t.rb * kTrRows >= rows) return;
+  TreeSrc<D> src{a};
+  src.qb = uniform_load(a.cu_q, t.s);
+  src.n = uniform_load(a.cu_q, t.s + 1) - src.qb;
+  src.r0 = t.rb * kTrRows;
+  if (src.r0 >= src.n * group) return;
   const int nk = min(uniform_load(a.kv_lens, t.s), a.max_blocks * 16);
   int pps;
-  const int n_sp = tree_pieces(a, nk, pps);
-  if (t.sp >= n_sp) return;
-  const int wave = wave_id(), lane = threadIdx.x & 63, half = lane >> 5;
-  const int r = t.rb * kTrRows + 32 * wave + (lane & 31);
-  const int rc = min(r, rows - 1);
-  const size_t row = (size_t)(qb + rc / group) * a.hq + t.kvh * group + rc % group;
-  PfState<D> st;
-  mt_load_q<D>(st, (const bf16_t*)a.q + row * D);
-  TreeRows tr;
-  tr.mask = a.mask + (size_t)(qb + rc / group) * a.mask_words;
-  tr.prior = nk - n;
-  tr.n = n;
-  tr.words = a.mask_words;
+  src.n_sp = tree_pieces(a, nk, pps);
+  if (t.sp >= src.n_sp || nk <= 0) return;
+  src.sp = t.sp;
+  src.group = group;
+  src.h0 = t.kvh * group;
+  src.kv_len = nk;
+  const int k0 = t.sp * pps * 16, k1 = min(nk, k0 + pps * 16);
+  src.spans = KeySpans{k0, (k1 - k0 + kMtKeys - 1) / kMtKeys, 0, 0};
   const PagedDmaKV<D> kv{(const bf16_t*)a.k_cache + (size_t)t.kvh * 16 * D,
-                      (const bf16_t*)a.v_cache + (size_t)t.kvh * 16 * D,
-                      a.tables + (size_t)t.s * a.max_blocks, (size_t)a.hkv * 16 * D};
-  const KeySpans sp = key_spans(nk, 0, 0);
-  masked_tile<D>(tr, kv, sp, t.sp * pps / 2, min(sp.blocks(), (t.sp + 1) * pps / 2), nk, a.scale,
-                 kring, vring, st);
-  const float lse = mt_finish<D>(st, a.scale);
-  if (n_sp == 1) {
-    mt_store<D>(st, (bf16_t*)a.o + row * D, r < rows);
-    return;
-  }
-  if (r >= rows) return;
-  float* o = a.part_o + (row * a.num_splits + t.sp) * D + 4 * half;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<f32x4*>(o + 32 * dt + 8 * g) =
-          f32x4{st.oacc[dt][4 * g], st.oacc[dt][4 * g + 1], st.oacc[dt][4 * g + 2],
-                st.oacc[dt][4 * g + 3]};
-  if (half == 0) a.part_lse[row * a.num_splits + t.sp] = lse;
+                         (const bf16_t*)a.v_cache + (size_t)t.kvh * 16 * D,
+                         a.tables + (size_t)t.s * a.max_blocks, (size_t)a.hkv * 16 * D};
+  masked_items<D>(src, kv, nk, a.scale, lds);
 }
 
 // o = sum_i 2^(lse_i - m) o_i / sum_i 2^(lse_i - m): one wave per (node, q head).
