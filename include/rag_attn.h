@@ -374,8 +374,9 @@ rag_status rag_kv_pages_update(int32_t *block_tables, int32_t *free_pages,
 /*
  * Bytes of workspace that rag_attn_decode_paged_tree needs (0 where it does not
  * cut its sequences, and for invalid sizes).  Library-internal layout: fp32
- * partial outputs [num_seqs * max_nodes, num_q_heads, splits, head_dim], then fp32
- * partial log-sum-exp values.
+ * partial outputs (head_dim values for every piece and (node, q head) pair, in
+ * whole blocks of 128 pairs of a kv head above that number), their fp32
+ * log-sum-exp values, and two int32 for every sequence.
  */
 size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
                                            int32_t num_q_heads,
@@ -407,8 +408,11 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
  *            max_blocks_per_seq * 16 (checked when RAG_ATTN_CHECK=1, and the ids
  *            of the pages read).  A sequence without nodes may hold no key.
  *   max_nodes  host upper bound of n (sizes the grid).
- *   num_splits  0 = automatic; else the most pieces (at most 64) that a
- *            sequence's pages are cut into.
+ *   num_splits  0 = automatic; else the number of pieces (at most 64, and one for
+ *            each 32 keys) that every sequence's keys are cut into.  Automatic: with
+ *            at most 256 sequences the pieces are cut on the GPU from the
+ *            sequences' lengths, about equally long and about as many as the GPU
+ *            works on at a time; with more, none.
  *   workspace, workspace_bytes  device scratch of at least
  *            rag_attn_decode_tree_workspace_size(...) bytes for the same
  *            arguments (NULL when that is 0); 256-byte aligned, of any contents.

@@ -44,9 +44,21 @@ struct TreeArgs {
   const int32_t* cu_q;
   int num_seqs, max_nodes, mask_words, max_blocks, hq, hkv, d;
   float scale;
-  int num_splits;               // pieces that a sequence's pages are cut into, at most
-  float* part_o;                // [query row, head][split][d] (num_splits > 1)
-  float* part_lse;              // [query row, head][split]
+  int row_blocks = 1;           // blocks of 128 (node, q head of a group) rows, at most
+  int splits = 1;               // pieces of every sequence (0: cut from the lengths)
+  int pieces = 0;               // of all sequences, at most
+  int part_rows = 0;            // rows of a row block in the partials
+  // a launch that may cut: partial outputs [piece][kv head][row block][part_rows][d], their
+  // log-sum-exps, and each sequence's first piece and their number (else null)
+  float* part_o = nullptr;
+  float* part_lse = nullptr;
+  int32_t* part_of = nullptr;
+};
+
+// How a tree launch is cut (requested splits 0: chosen).
+struct TreeShape {
+  int row_blocks, splits, part_rows;
+  int64_t pieces;
 };
 
 struct RangesArgs {
@@ -69,9 +81,10 @@ int64_t pages_grid(const PagesArgs& a);
 hipError_t launch_pages(const PagesArgs& a, hipStream_t stream);
 int64_t keep_grid(const KeepArgs& a);
 hipError_t launch_keep(const KeepArgs& a, hipStream_t stream);
-// Pieces that a tree launch cuts a sequence's pages into (requested 0: chosen).
-int tree_splits(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks, int requested);
-int64_t tree_grid(const TreeArgs& a);
+TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
+                     int requested);
+size_t tree_partial_rows(const TreeShape& t, int hkv);
+int64_t tree_grid(const TreeShape& t, const TreeArgs& a);
 hipError_t launch_tree(const TreeArgs& a, hipStream_t stream);
 int64_t ranges_grid(const RangesArgs& a);
 hipError_t launch_ranges(const RangesArgs& a, hipStream_t stream);

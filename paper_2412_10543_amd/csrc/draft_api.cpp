@@ -135,17 +135,21 @@ rag_status check_tree(const rag::TreeArgs& a, int32_t num_blocks, hipStream_t st
   return RAG_OK;
 }
 
-// Partials of a tree launch: fp32 outputs, then fp32 log-sum-exps.
+// Workspace of a tree launch that may cut: fp32 partial outputs, fp32
+// log-sum-exps, int32 pairs per sequence.
 struct TreeWs {
-  size_t lse_off, bytes;
+  size_t lse_off, of_off, bytes;
 };
 
-TreeWs tree_workspace(int32_t num_seqs, int32_t max_nodes, int32_t hq, int32_t d, int32_t splits) {
-  if (splits <= 1) return {0, 0};
+TreeWs tree_workspace(const rag::TreeShape& t, int32_t num_seqs, int32_t hkv, int32_t d) {
+  const size_t rows = rag::tree_partial_rows(t, hkv);
+  if (rows == 0) return {0, 0, 0};
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  const size_t rows = (size_t)num_seqs * max_nodes * hq * splits;
-  const size_t o = up(rows * d * sizeof(float));
-  return {o, o + up(rows * sizeof(float))};
+  TreeWs w;
+  w.lse_off = up(rows * d * sizeof(float));
+  w.of_off = w.lse_off + up(rows * sizeof(float));
+  w.bytes = w.of_off + up((size_t)num_seqs * 2 * sizeof(int32_t));
+  return w;
 }
 
 }  // namespace
@@ -222,9 +226,9 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes, 
   if (num_seqs <= 0 || max_nodes <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 ||
       num_q_heads % num_kv_heads != 0 || head_dim <= 0 || max_blocks_per_seq <= 0 || num_splits < 0)
     return 0;
-  const int32_t n = rag::tree_splits(num_seqs, max_nodes, num_q_heads, num_kv_heads, head_dim,
-                                     max_blocks_per_seq, num_splits);
-  return tree_workspace(num_seqs, max_nodes, num_q_heads, head_dim, n).bytes;
+  const rag::TreeShape t = rag::tree_shape(num_seqs, max_nodes, num_q_heads, num_kv_heads,
+                                           head_dim, max_blocks_per_seq, num_splits);
+  return tree_workspace(t, num_seqs, num_kv_heads, head_dim).bytes;
 }
 
 rag_status rag_attn_decode_paged_tree(const void* q, const void* k_cache, const void* v_cache,
@@ -258,10 +262,16 @@ rag_status rag_attn_decode_paged_tree(const void* q, const void* k_cache, const 
     return fail(RAG_ERR_UNSUPPORTED, "%s: %d nodes of %d heads", who, max_nodes, num_q_heads);
   rag::TreeArgs a{q, k_cache, v_cache, o, tree_mask, block_tables, kv_lens, cu_seqlens_q, num_seqs,
                   max_nodes, mask_words, max_blocks_per_seq, num_q_heads, num_kv_heads, head_dim,
-                  softmax_scale, 1, nullptr, nullptr};
-  a.num_splits = rag::tree_splits(num_seqs, max_nodes, num_q_heads, num_kv_heads, head_dim,
-                                  max_blocks_per_seq, num_splits);
-  const TreeWs ws = tree_workspace(num_seqs, max_nodes, num_q_heads, head_dim, a.num_splits);
+                  softmax_scale};
+  const rag::TreeShape t = rag::tree_shape(num_seqs, max_nodes, num_q_heads, num_kv_heads,
+                                           head_dim, max_blocks_per_seq, num_splits);
+  if (rag::tree_grid(t, a) > INT_MAX)
+    return fail(RAG_ERR_UNSUPPORTED, "%s: batch too large for one grid", who);
+  a.row_blocks = t.row_blocks;
+  a.splits = t.splits;
+  a.pieces = (int)t.pieces;
+  a.part_rows = t.part_rows;
+  const TreeWs ws = tree_workspace(t, num_seqs, num_kv_heads, head_dim);
   if (ws.bytes > 0) {
     if (workspace == nullptr || workspace_bytes < ws.bytes)
       return fail(RAG_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, ws.bytes,
@@ -270,9 +280,8 @@ rag_status rag_attn_decode_paged_tree(const void* q, const void* k_cache, const 
       return fail(RAG_ERR_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
     a.part_o = static_cast<float*>(workspace);
     a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + ws.lse_off);
+    a.part_of = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ws.of_off);
   }
-  if (rag::tree_grid(a) > INT_MAX)
-    return fail(RAG_ERR_UNSUPPORTED, "%s: batch too large for one grid", who);
   if (check_mode()) {
     st = check_tree(a, num_blocks, stream);
     if (st != RAG_OK) return st;

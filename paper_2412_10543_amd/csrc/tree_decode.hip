@@ -2,10 +2,12 @@
 // queries of a sequence's n drafted nodes, its last n keys, see every key
 // before them and the nodes that their mask names.
 //
-// A unit is (sequence, kv head, 128 rows, piece of the pages): its rows are the
-// (node, q head of the group) pairs, node by node, so that every K/V byte is
-// read once for all of them.  Pieces of one sequence write normalised partial
-// outputs and their log-sum-exp, which a second kernel joins.
+// A unit is (piece of a sequence's keys, kv head, 128 rows): its rows are (node, q
+// head of the group) pairs, node by node, so that every K/V byte is read once for
+// 128 of them.  The pieces are cut on the GPU from the sequences' lengths, about
+// as many units as the chip takes at a time and about equally long (tree_plan);
+// where a sequence has several, they write normalised partial outputs and their
+// log-sum-exp, which a second kernel joins.
 #include "common.h"
 #include "draft.h"
 #include "masked_tile.h"
@@ -15,6 +17,15 @@ namespace rag {
 namespace {
 
 constexpr int kTrRows = 32 * kMtWaves;
+constexpr int kTrPlanSeqs = 256;     // sequences whose pieces are cut from their lengths
+#ifndef RAG_TR_MIN
+#define RAG_TR_MIN 8
+#endif
+#ifndef RAG_TR_ROUNDS
+#define RAG_TR_ROUNDS 1
+#endif
+constexpr int kTrMinBlocks = RAG_TR_MIN;    // blocks a piece is cut for, at least
+constexpr int kTrRounds = RAG_TR_ROUNDS;
 
 // What the lane's row sees.
 struct TreeRows {
@@ -41,7 +52,8 @@ template <int D>
 struct TreeSrc {
   const TreeArgs& a;
   static constexpr int count = 1;
-  int qb, n, group, h0, r0, kv_len, sp, n_sp;
+  int qb, n, group, h0, r0, kv_len, n_sp;
+  size_t unit;                  // of the partials
   KeySpans spans;
   TreeRows rows;
   __device__ __forceinline__ int row() const {
@@ -70,7 +82,8 @@ struct TreeSrc {
     const float lse = mt_lse(st, l, scale);
     if (!valid) return;
     const int half = opaque_lane() >> 5;
-    float* o = a.part_o + (x * a.num_splits + sp) * D + 4 * half;
+    const size_t pr = unit * a.part_rows + (row() - r0);
+    float* o = a.part_o + pr * D + 4 * half;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -78,63 +91,134 @@ struct TreeSrc {
         *reinterpret_cast<f32x4*>(o + 32 * dt + 8 * g) =
             f32x4{st.oacc[dt][4 * g], st.oacc[dt][4 * g + 1], st.oacc[dt][4 * g + 2],
                   st.oacc[dt][4 * g + 3]};
-    if (half == 0) a.part_lse[x * a.num_splits + sp] = lse;
+    if (half == 0) a.part_lse[pr] = lse;
   }
-};
-
-struct TreeCoord {
-  int s, kvh, rb, sp;
 };
 
 }  // namespace
 
-// Unit order: the row blocks of one (sequence, kv head, piece) follow each other
-// on one XCD, whose L2 then serves their K/V.
-__device__ __forceinline__ bool tree_coord(const TreeArgs& a, int row_blocks, TreeCoord& t) {
-  int xcd, local;
-  xcd_slot(blockIdx.x, xcd, local);
-  t.rb = local % row_blocks;
-  const int64_t stream = xcd + (int64_t)kNumXcd * (local / row_blocks);
-  const int64_t pairs = (int64_t)a.num_seqs * a.hkv;
-  if (stream >= pairs * a.num_splits) return false;
-  t.sp = (int)(stream / pairs);
-  const int pr = (int)(stream % pairs);
-  t.s = pr / a.hkv;
-  t.kvh = pr % a.hkv;
-  return true;
+__device__ __forceinline__ int tree_blocks(const TreeArgs& a, int s) {   // of sequence s
+  if (a.cu_q[s + 1] - a.cu_q[s] <= 0) return 0;
+  return (min(a.kv_lens[s], a.max_blocks * 16) + kMtKeys - 1) / kMtKeys;
 }
 
-// Pieces that a sequence of kv_len keys is cut into, of pps pages each.
-__device__ __forceinline__ int tree_pieces(const TreeArgs& a, int kv_len, int& pps) {
-  pps = max(1, (a.max_blocks + a.num_splits - 1) / a.num_splits);
-  pps = (pps + 1) & ~1;                          // whole blocks of 32 keys
-  return max(1, ((kv_len + 15) / 16 + pps - 1) / pps);
+// Piece `pi` of the launch: sequence s (-1: there is no such piece), the p-th of
+// its n pieces; `first` its first.
+struct TreePiece {
+  int s, p, n, first;
+};
+
+// With a number of splits given every sequence is cut into that many (or its
+// blocks), and piece s * splits + p is sequence s's p-th.
+__device__ __forceinline__ TreePiece tree_piece_even(const TreeArgs& a, int pi) {
+  TreePiece t;
+  t.s = pi / a.splits;
+  t.p = pi % a.splits;
+  t.first = pi - t.p;
+  t.n = t.s < a.num_seqs ? min(a.splits, max(tree_blocks(a, t.s), 1)) : 0;
+  if (t.p >= t.n) t.s = -1;
+  return t;
 }
 
-template <int D>
+// Otherwise (at most kTrPlanSeqs sequences) into pieces of at most a quota of blocks,
+// the smallest quota tried for which the pieces are at most a.pieces.  Wave-parallel,
+// one lane per sequence; every wave finds the same.
+template <int kChunks>
+__device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
+  const int lane = threadIdx.x & 63;
+  int bl[kChunks], np[kChunks], longest = 0;
+  float total = 0.f;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int s = c * kWave + lane;
+    bl[c] = tree_blocks(a, min(s, a.num_seqs - 1));
+    if (s >= a.num_seqs) bl[c] = 0;
+    longest = max(longest, bl[c]);
+  }
+  auto lanes_sum = [](auto x) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, kWave);
+    return x;
+  };
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) total += lanes_sum((float)bl[c]);
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) longest = max(longest, __shfl_xor(longest, m, kWave));
+  // (single precision: every wave forms the same numbers, and any cut is a valid one)
+  float q = fmaxf((float)kTrMinBlocks, fmaxf(total / (float)a.pieces,
+                                             (float)longest / (float)kTreeMaxSplits));
+  for (;;) {
+    const float rq = 1.f / q;
+    int count = 0;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      np[c] = bl[c] > 0 ? min(max((int)ceilf((float)bl[c] * rq - 1e-3f), 1), kTreeMaxSplits) : 0;
+      count += lanes_sum(np[c]);
+    }
+    // (from the longest on every sequence is one piece: at most num_seqs <= pieces)
+    if (count <= a.pieces || q > (float)longest) break;
+    q = fmaxf(q * 1.0625f, q + 1.f);
+  }
+  TreePiece t{-1, 0, 0, 0};
+  int before = 0;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    int incl = np[c];
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int y = __shfl_up(incl, d, kWave);
+      if (lane >= d) incl += y;
+    }
+    const int first = before + incl - np[c];
+    const uint64_t at = __builtin_amdgcn_ballot_w64(pi >= first && pi < first + np[c]);
+    if (at != 0) {
+      const int l = __builtin_ctzll(at);
+      t.s = c * kWave + l;
+      t.first = __builtin_amdgcn_readlane(first, l);
+      t.n = __builtin_amdgcn_readlane(np[c], l);
+      t.p = pi - t.first;
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return t;
+}
+
+// Unit order: the row blocks of one (piece, kv head) follow each other on one XCD,
+// whose L2 then serves their K/V.
+template <int D, int kChunks>
 __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
   __shared__ __attribute__((aligned(16))) MtLds<D> lds;
   const int group = a.hq / a.hkv;
-  TreeCoord t;
-  if (!tree_coord(a, (a.max_nodes * group + kTrRows - 1) / kTrRows, t)) return;
+  int xcd, local;
+  xcd_slot(blockIdx.x, xcd, local);
+  const int rb = local % a.row_blocks;
+  const int stream = xcd + kNumXcd * (local / a.row_blocks);
+  const int kvh = stream % a.hkv, pi = stream / a.hkv;
+  if (pi >= a.pieces) return;
+  TreePiece t;
+  if constexpr (kChunks == 0) t = tree_piece_even(a, pi); else t = tree_plan<kChunks>(a, pi);
+  const int s = __builtin_amdgcn_readfirstlane(t.s);
+  if (s < 0) return;
+  const int p = __builtin_amdgcn_readfirstlane(t.p), n_sp = __builtin_amdgcn_readfirstlane(t.n);
+  if (p == 0 && rb == 0 && kvh == 0 && threadIdx.x == 0 && a.part_of != nullptr)
+    reinterpret_cast<int2*>(a.part_of)[s] = int2{t.first, t.n};   // for the join
   TreeSrc<D> src{a};
-  src.qb = uniform_load(a.cu_q, t.s);
-  src.n = uniform_load(a.cu_q, t.s + 1) - src.qb;
-  src.r0 = t.rb * kTrRows;
-  if (src.r0 >= src.n * group) return;
-  const int nk = min(uniform_load(a.kv_lens, t.s), a.max_blocks * 16);
-  int pps;
-  src.n_sp = tree_pieces(a, nk, pps);
-  if (t.sp >= src.n_sp || nk <= 0) return;
-  src.sp = t.sp;
+  src.qb = uniform_load(a.cu_q, s);
+  src.n = uniform_load(a.cu_q, s + 1) - src.qb;
+  src.r0 = rb * kTrRows;
+  const int nk = min(uniform_load(a.kv_lens, s), a.max_blocks * 16);
+  if (src.r0 >= src.n * group || nk <= 0) return;
+  src.n_sp = n_sp;
+  src.unit = ((size_t)pi * a.hkv + kvh) * a.row_blocks + rb;
   src.group = group;
-  src.h0 = t.kvh * group;
+  src.h0 = kvh * group;
   src.kv_len = nk;
-  const int k0 = t.sp * pps * 16, k1 = min(nk, k0 + pps * 16);
-  src.spans = KeySpans{k0, (k1 - k0 + kMtKeys - 1) / kMtKeys, 0, 0};
-  const PagedDmaKV<D> kv{(const bf16_t*)a.k_cache + (size_t)t.kvh * 16 * D,
-                         (const bf16_t*)a.v_cache + (size_t)t.kvh * 16 * D,
-                         a.tables + (size_t)t.s * a.max_blocks, (size_t)a.hkv * 16 * D};
+  const int64_t blocks = (nk + kMtKeys - 1) / kMtKeys;
+  const int b0 = (int)(blocks * p / n_sp), b1 = (int)(blocks * (p + 1) / n_sp);
+  src.spans = KeySpans{b0 * kMtKeys, b1 - b0, 0, 0};
+  const PagedDmaKV<D> kv{(const bf16_t*)a.k_cache + (size_t)kvh * 16 * D,
+                         (const bf16_t*)a.v_cache + (size_t)kvh * 16 * D,
+                         a.tables + (size_t)s * a.max_blocks, (size_t)a.hkv * 16 * D};
   masked_items<D>(src, kv, nk, a.scale, lds);
 }
 
@@ -145,15 +229,18 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   const int wave = wave_id(), lane = threadIdx.x & 63;
   const int per = (a.max_nodes * a.hq + 3) / 4;  // workgroups of a sequence
   const int s = blockIdx.x / per;
-  const int qb = a.cu_q[s], n = a.cu_q[s + 1] - qb;
+  const int qb = uniform_load(a.cu_q, s), n = uniform_load(a.cu_q, s + 1) - qb;
   const int i = blockIdx.x % per * 4 + wave;     // (node, head) of the sequence
   if (i >= n * a.hq) return;
-  const int nk = min(a.kv_lens[s], a.max_blocks * 16);
-  int pps;
-  const int n_sp = tree_pieces(a, nk, pps);
-  if (n_sp == 1) return;
-  const size_t row = (size_t)qb * a.hq + i;
-  const float lse = lane < n_sp ? a.part_lse[row * a.num_splits + lane] : -INFINITY;
+  if (uniform_load(a.kv_lens, s) <= 0) return;
+  const int first = uniform_load(a.part_of, 2 * s), n_sp = uniform_load(a.part_of, 2 * s + 1);
+  if (n_sp <= 1) return;
+  const int group = a.hq / a.hkv, node = i / a.hq, head = i % a.hq, kvh = head / group;
+  const int r = node * group + head % group;     // row of the unit's row blocks
+  const size_t stride = (size_t)a.hkv * a.row_blocks * a.part_rows;     // rows between pieces
+  const size_t row = (((size_t)first * a.hkv + kvh) * a.row_blocks + r / kTrRows) * a.part_rows +
+                     r % kTrRows;
+  const float lse = lane < n_sp ? a.part_lse[row + lane * stride] : -INFINITY;
   float mx = lse;
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) mx = fmaxf(mx, wave_xor(mx, m));
@@ -164,50 +251,70 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   for (int m = 32; m >= 1; m >>= 1) den += wave_xor(den, m);
   const float inv = den == 0.f ? 0.f : 1.f / den;
   float acc[kPer] = {};
-  const float* po = a.part_o + row * a.num_splits * D + lane * kPer;
+  const float* po = a.part_o + row * D + lane * kPer;
   for (int k = 0; k < n_sp; ++k) {
     const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k));
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) acc[e] += wk * po[(size_t)k * D + e];
+    for (int e = 0; e < kPer; ++e) acc[e] += wk * po[(size_t)k * stride * D + e];
   }
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const __bf16 b = (__bf16)(acc[e] * inv);
-    ((bf16_t*)a.o)[row * D + lane * kPer + e] = __builtin_bit_cast(bf16_t, b);
+    ((bf16_t*)a.o)[((size_t)qb * a.hq + i) * D + lane * kPer + e] = __builtin_bit_cast(bf16_t, b);
   }
 }
 
-static int tree_row_blocks(int max_nodes, int group) {
-  return (int)(((int64_t)max_nodes * group + kTrRows - 1) / kTrRows);
+TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
+                     int requested) {
+  TreeShape t;
+  const int64_t rows = (int64_t)max_nodes * (hq / hkv);
+  t.row_blocks = (int)((rows + kTrRows - 1) / kTrRows);
+  t.part_rows = (int)std::min<int64_t>(rows, kTrRows);
+  const int64_t blocks = ((int64_t)max_blocks + 1) / 2;          // of the longest sequence
+  if (requested > 0 || num_seqs > kTrPlanSeqs) {
+    t.splits = (int)std::max<int64_t>(1, std::min<int64_t>({requested, kTreeMaxSplits, blocks}));
+    t.pieces = (int64_t)num_seqs * t.splits;
+    return t;
+  }
+  t.splits = 0;
+  const int64_t units = (int64_t)kTrRounds * (d == 64 ? 3 : 2) * 256;
+  int64_t n = units / ((int64_t)hkv * t.row_blocks);
+  n = std::min(n, num_seqs * std::max<int64_t>(1, blocks / kTrMinBlocks));
+  n = std::min<int64_t>(n, (int64_t)num_seqs * kTreeMaxSplits);
+  t.pieces = std::max<int64_t>(n, num_seqs);
+  if (t.pieces == num_seqs) t.splits = 1;                        // nothing to cut
+  return t;
 }
 
-int tree_splits(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks, int requested) {
-  (void)d;
-  const int64_t units = (int64_t)num_seqs * hkv * std::max(1, tree_row_blocks(max_nodes, hq / hkv));
-  int64_t n = requested > 0 ? requested : (512 + units - 1) / units;
-  if (requested <= 0) n = std::min<int64_t>(n, std::max(1, max_blocks / 16));
-  n = std::max<int64_t>(1, std::min<int64_t>({n, (int64_t)kTreeMaxSplits, (int64_t)(max_blocks + 1) / 2}));
-  return (int)n;
+size_t tree_partial_rows(const TreeShape& t, int hkv) {
+  return t.splits == 1 ? 0 : (size_t)t.pieces * hkv * t.row_blocks * t.part_rows;
 }
 
 static int64_t tree_join_grid(const TreeArgs& a) {
   return (int64_t)a.num_seqs * (((int64_t)a.max_nodes * a.hq + 3) / 4);
 }
+static int64_t tree_units_grid(int64_t pieces, int hkv, int row_blocks) {
+  return (pieces * hkv + kNumXcd - 1) / kNumXcd * kNumXcd * row_blocks;
+}
 
-int64_t tree_grid(const TreeArgs& a) {
-  const int64_t streams = (int64_t)a.num_seqs * a.hkv * a.num_splits;
-  const int64_t units =
-      (streams + kNumXcd - 1) / kNumXcd * kNumXcd * tree_row_blocks(a.max_nodes, a.hq / a.hkv);
-  return std::max(units, a.num_splits > 1 ? tree_join_grid(a) : 0);   // (the larger of the launches)
+int64_t tree_grid(const TreeShape& t, const TreeArgs& a) {
+  return std::max(tree_units_grid(t.pieces, a.hkv, t.row_blocks),
+                  t.splits == 1 ? 0 : tree_join_grid(a));        // (the larger of the launches)
 }
 
 template <int D>
 static hipError_t launch_tree_d(const TreeArgs& a, hipStream_t stream) {
-  const int64_t streams = (int64_t)a.num_seqs * a.hkv * a.num_splits;
-  const int64_t grid =
-      (streams + kNumXcd - 1) / kNumXcd * kNumXcd * tree_row_blocks(a.max_nodes, a.hq / a.hkv);
-  hipLaunchKernelGGL(tree_kernel<D>, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a);
-  if (a.num_splits > 1)
+  const int64_t grid = tree_units_grid(a.pieces, a.hkv, a.row_blocks);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a);
+  };
+  if (a.splits > 0)
+    go(tree_kernel<D, 0>);
+  else if (a.num_seqs <= kWave)
+    go(tree_kernel<D, 1>);
+  else
+    go(tree_kernel<D, kTrPlanSeqs / kWave>);
+  if (a.part_o != nullptr)
     hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)tree_join_grid(a)), dim3(256), 0,
                        stream, a);
   return hipGetLastError();
