@@ -340,12 +340,38 @@ struct BlockCopy {
   }
 };
 
-// The lane's query row.
-template <int D>
-__device__ __forceinline__ void mt_load_q(PfState<D>& st, const bf16_t* row) {
-  const bf16_t* q = row + 8 * (opaque_lane() >> 5);
+// Rows of a wave go to and from memory as 64-byte pieces, 16 rows an instruction,
+// through 2 KiB of LDS of the wave's own (io: 32 rows of 64 bytes, 16-byte chunk c
+// of row r at c ^ (r / 4) % 4), where a lane has its own row.  (A lane's row in
+// 16-byte pieces straight from memory is 64 pieces an instruction: queries and
+// outputs of 16 prompts of 6000 tokens took 160 us of 518.)
+__device__ __forceinline__ int io_at(int r, int c) { return 32 * r + 8 * (c ^ ((r >> 2) & 3)); }
+
+// The lane's query row: rows(r) is row r of the wave's 32.
+template <int D, class RowPtr>
+__device__ __forceinline__ void mt_request_q(PfState<D>& st, const RowPtr& rows) {
+  const int lane = opaque_lane(), c = lane & 3;
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) st.qf[ks] = as_bf16x8(load16(q + 16 * ks));
+  for (int i = 0; i < 2; ++i) {
+    const bf16_t* q = rows((lane >> 2) + 16 * i) + 8 * c;
+#pragma unroll
+    for (int p = 0; p < D / 32; ++p) st.qf[2 * p + i] = as_bf16x8(load16(q + 32 * p));
+  }
+}
+template <int D>
+__device__ __forceinline__ void mt_place_q(PfState<D>& st, bf16_t* io) {
+  const int lane = opaque_lane(), c = lane & 3, r = lane & 31, half = lane >> 5;
+#pragma unroll
+  for (int p = 0; p < D / 32; ++p) {             // columns 32 p on
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<bf16x8*>(io + io_at((lane >> 2) + 16 * i, c)) = st.qf[2 * p + i];
+    wave_lds_sync();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      st.qf[2 * p + i] = *reinterpret_cast<const bf16x8*>(io + io_at(r, 2 * i + half));
+    wave_lds_sync();
+  }
 }
 
 // The rows of one wave against the blocks of an item, where keys that some row
@@ -386,12 +412,14 @@ __device__ __forceinline__ void masked_item_odd(const Rows& rows, const KV& kv, 
   }
 }
 
-// LDS of a workgroup: rings of K and V blocks, and a block of zeros.
+// LDS of a workgroup: rings of K and V blocks, a block of zeros, and the waves'
+// 2 KiB for rows to and from memory (80 KiB at D = 128: two workgroups a CU).
 template <int D>
 struct MtLds {
   bf16_t k[kMtRing * BlockLayout<D>::kElems];
   bf16_t v[kMtRing * BlockLayout<D>::kElems];
   bf16_t zero[BlockLayout<D>::kElems];
+  bf16_t io[kMtWaves][1024];
 };
 
 // The items of a workgroup, one after another: 128 (row, head) pairs each, 32 of
@@ -401,8 +429,8 @@ struct MtLds {
 //   Rows rows           of the item settled last: what the lane's row sees
 //   fetch(m)            requests what item m's rows and spans follow from
 //   settle(m)           the spans of item m, from what was fetched last, and rows
-//   q(m)                the lane's query row
-//   store(m, st, l, scale)   writes the lane's row, of sum of weights l
+//   q(m, r)             row r of the wave's 32 query rows
+//   store(m, st, l, scale, io)   writes the wave's rows; l: the lane's row's sum of weights
 // As in prefill_items, slot i of an item forms QK(i + 1) and PV(i - 1) on the
 // matrix cores beside the weights of block i.  K(i + 4) and V(i + 2) are requested
 // in slot i, into the places of K(i) and V(i - 2), which slot i - 1 was the last to
@@ -424,8 +452,9 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
   const Lay lay;
   const float c = scale * kLog2e;
   PfState<D> st;
+  bf16_t* const io = lds.io[wave_id()];
   src.fetch(0);
-  mt_load_q<D>(st, src.q(0));
+  mt_request_q<D>(st, [&](int r) { return src.q(0, r); });
   KeySpans sp = src.settle(0), sp_next{0, 0, 0, 0};
   auto rows = src.rows;
   auto rows_next = rows;
@@ -450,8 +479,7 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
   for (int i = threadIdx.x; i < Lay::kElems / 8; i += 64 * kMtWaves)
     *reinterpret_cast<u32x4*>(lds.zero + 8 * i) = u32x4{0, 0, 0, 0};
   // (the first product waits for Q, and with it for the copies before it)
-#pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(st.qf[ks]));
+  mt_place_q<D>(st, io);
   if (src.count > 1) {
     sp_next = src.settle(1);
     rows_next = src.rows;
@@ -561,9 +589,10 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
       pf_pv<D, 0>(st, lay, lds.v + rb + kE, pO);
     }
     if (wave_any(odd != 0)) odd_items |= 1u << m;
-    if (more) mt_load_q<D>(st, src.q(m + 1));
-    src.store(m, st, mt_finish<D>(st), scale);
+    if (more) mt_request_q<D>(st, [&](int r) { return src.q(m + 1, r); });
+    src.store(m, st, mt_finish<D>(st), scale, io);
     if (!more) break;
+    mt_place_q<D>(st, io);
     sp = sp1;
     rows = rows1;
     slots = slots1;
@@ -577,18 +606,30 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
 template <int D, class Src, class KV>
 __device__ __forceinline__ void masked_items(Src& src, const KV& kv, int nk, float scale,
                                              MtLds<D>& lds) {
-  const uint32_t odd = masked_items_fast<D>(src, kv, nk, scale, lds);
-  if (__builtin_expect(!__syncthreads_or(odd != 0), 1)) return;
+  uint32_t odd = masked_items_fast<D>(src, kv, nk, scale, lds);
+  uint32_t* const all = reinterpret_cast<uint32_t*>(lds.zero);   // (nobody reads zeros any more)
+  __syncthreads();
+  if (threadIdx.x < kMtWaves) all[threadIdx.x] = 0;
+  __syncthreads();
+  if (odd != 0) all[wave_id()] = odd;
+  __syncthreads();
+  odd = 0;
+#pragma unroll
+  for (int w = 0; w < kMtWaves; ++w) odd |= all[w];
+  odd = __builtin_amdgcn_readfirstlane(odd);
+  if (__builtin_expect(odd == 0, 1)) return;
   asm volatile("");
+  bf16_t* const io = lds.io[wave_id()];
 #pragma unroll 1
   for (int m = 0; m < src.count; ++m) {
-    if (!__syncthreads_or(odd >> m & 1)) continue;
+    if (!(odd >> m & 1)) continue;
     PfState<D> st;
     src.fetch(m);
-    mt_load_q<D>(st, src.q(m));
+    mt_request_q<D>(st, [&](int r) { return src.q(m, r); });
     const KeySpans sp = src.settle(m);
+    mt_place_q<D>(st, io);
     masked_item_odd<D>(src.rows, kv, sp, nk, scale, lds.k, lds.v, st);
-    src.store(m, st, mt_finish<D>(st), scale);
+    src.store(m, st, mt_finish<D>(st), scale, io);
   }
 }
 
@@ -610,26 +651,50 @@ __device__ __forceinline__ float mt_lse(const PfState<D>& st, float l, float sca
   return l == 0.f ? -INFINITY : st.m_used * scale + logf(l);
 }
 
-// Stores the lane's row (of the two lanes that hold a row, each the half of every
-// 16 values): the halves trade four values for four, and each then stores 16
-// bytes at a time.
-template <int D>
-__device__ __forceinline__ void mt_store(const PfState<D>& st, bf16_t* row, bool valid) {
-  const int half = (threadIdx.x & 63) >> 5;
+// Stores the wave's rows: rows(r) is where row r goes, or null.
+template <int D, class RowPtr>
+__device__ __forceinline__ void mt_store(const PfState<D>& st, bf16_t* io, const RowPtr& rows) {
+  const int lane = opaque_lane(), c = lane & 3, r = lane & 31, half = lane >> 5;
+  bf16_t* const to[2] = {rows(lane >> 2), rows((lane >> 2) + 16)};
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) {
+    const f32x16& o = st.oacc[dt];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<bf16x4*>(io + io_at(r, g) + 4 * half) =
+          to_bf16x4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+    wave_lds_sync();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(io + io_at((lane >> 2) + 16 * i, c));
+      if (to[i] != nullptr) *reinterpret_cast<u32x4*>(to[i] + 32 * dt + 8 * c) = x;
+    }
+    wave_lds_sync();
+  }
+}
+
+// The same in fp32.
+template <int D, class RowPtr>
+__device__ __forceinline__ void mt_store_f32(const PfState<D>& st, bf16_t* io_, const RowPtr& rows) {
+  const int lane = opaque_lane(), c = lane & 3, r = lane & 31, half = lane >> 5;
+  float* const to[2] = {rows(lane >> 2), rows((lane >> 2) + 16)};
+  float* io = reinterpret_cast<float*>(io_);
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int g = 0; g < 4; g += 2) {
+    for (int h = 0; h < 2; ++h) {                // columns 32 dt + 16 h on
       const f32x16& o = st.oacc[dt];
-      const bf16x4 a = to_bf16x4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
-      const bf16x4 b = to_bf16x4(o[4 * g + 4], o[4 * g + 5], o[4 * g + 6], o[4 * g + 7]);
-      const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
-      // lane 0..31: a's first half from itself, its second from lane + 32; the
-      // other lanes the same of b
-      const auto s0 = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
-      const auto s1 = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
-      const u32x4 w = {s0[0], s1[0], s0[1], s1[1]};
-      if (valid) *reinterpret_cast<u32x4*>(row + 32 * dt + 8 * (g + half)) = w;
+#pragma unroll
+      for (int g = 2 * h; g < 2 * h + 2; ++g)
+        *reinterpret_cast<f32x4*>(io + io_at(r, 2 * (g & 1) + half) / 2) =
+            f32x4{o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]};
+      wave_lds_sync();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(io + io_at((lane >> 2) + 16 * i, c) / 2);
+        if (to[i] != nullptr) *reinterpret_cast<f32x4*>(to[i] + 32 * dt + 16 * h + 4 * c) = x;
+      }
+      wave_lds_sync();
     }
 }
 

@@ -108,15 +108,24 @@ struct RangeSrc {
     rows.last_min = last_key(r0);
     return key_spans(shared_max, start_min, last_key(r0 + tile_rows - 1) + 1);
   }
-  __device__ __forceinline__ size_t out(int m) const {
-    return (size_t)(qb + min(row(m), nq - 1)) * a.hq + h0 + wave_id() % hw;
+  // Element offset of row r of the wave's 32, of item m; its row of the sequence.
+  __device__ __forceinline__ int seq_row(int m, int r) const {
+    return (t0 + m) * tile_rows + 32 * (wave_id() / hw) + r;
   }
-  __device__ __forceinline__ const bf16_t* q(int m) const { return (const bf16_t*)a.q + out(m) * D; }
-  __device__ __forceinline__ void store(int m, const PfState<D>& st, float l, float scale) const {
-    const int r = row(m);
-    mt_store<D>(st, (bf16_t*)a.o + out(m) * D, r < nq);
+  __device__ __forceinline__ size_t at(int m, int r) const {
+    return ((size_t)(qb + min(seq_row(m, r), nq - 1)) * a.hq + h0 + wave_id() % hw) * D;
+  }
+  __device__ __forceinline__ const bf16_t* q(int m, int r) const {
+    return (const bf16_t*)a.q + at(m, r);
+  }
+  __device__ __forceinline__ void store(int m, const PfState<D>& st, float l, float scale,
+                                        bf16_t* io) const {
+    mt_store<D>(st, io, [&](int r) {
+      return seq_row(m, r) < nq ? (bf16_t*)a.o + at(m, r) : (bf16_t*)nullptr;
+    });
     if (a.lse != nullptr) {
       const float lse = mt_lse(st, l, scale);
+      const int r = row(m);
       if (opaque_lane() < 32 && r < nq)
         a.lse[(size_t)(h0 + wave_id() % hw) * uniform_load(a.cu_q, a.num_seqs) + qb + r] = lse;
     }
@@ -173,7 +182,7 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void ranges_kernel(RangesArgs a, 
   if (nk <= 0) {                                 // no key: nothing to copy from
     PfState<D> st;
     pf_reset(st);
-    for (int m = 0; m < src.count; ++m) src.store(m, st, 0.f, a.scale);
+    for (int m = 0; m < src.count; ++m) src.store(m, st, 0.f, a.scale, lds.io[wave_id()]);
     return;
   }
   const DenseKV kv{(const bf16_t*)a.k + ((size_t)kb * a.hkv + kvh) * D,

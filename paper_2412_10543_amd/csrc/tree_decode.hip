@@ -56,42 +56,37 @@ struct TreeSrc {
   size_t unit;                  // of the partials
   KeySpans spans;
   TreeRows rows;
-  __device__ __forceinline__ int row() const {
-    return r0 + 32 * wave_id() + (opaque_lane() & 31);
-  }
-  __device__ __forceinline__ size_t out() const {         // (query row, q head)
-    const int r = min(row(), n * group - 1);
-    return (size_t)(qb + r / group) * a.hq + h0 + r % group;
+  // Row r of the wave's 32 is pair `pair(r)` of the sequence and kv head.
+  __device__ __forceinline__ int pair(int r) const { return r0 + 32 * wave_id() + r; }
+  __device__ __forceinline__ size_t at(int r) const {     // its element offset in q and o
+    const int x = min(pair(r), n * group - 1);
+    return ((size_t)(qb + x / group) * a.hq + h0 + x % group) * D;
   }
   __device__ __forceinline__ void fetch(int) {}
   __device__ __forceinline__ KeySpans settle(int) {
-    rows.mask = a.mask + (size_t)(qb + min(row(), n * group - 1) / group) * a.mask_words;
+    const int x = min(pair(opaque_lane() & 31), n * group - 1);
+    rows.mask = a.mask + (size_t)(qb + x / group) * a.mask_words;
     rows.prior = kv_len - n;
     rows.n = n;
     rows.words = a.mask_words;
     return spans;
   }
-  __device__ __forceinline__ const bf16_t* q(int) const { return (const bf16_t*)a.q + out() * D; }
-  __device__ __forceinline__ void store(int, const PfState<D>& st, float l, float scale) const {
-    const bool valid = row() < n * group;
-    const size_t x = out();
+  __device__ __forceinline__ const bf16_t* q(int, int r) const { return (const bf16_t*)a.q + at(r); }
+  __device__ __forceinline__ void store(int, const PfState<D>& st, float l, float scale,
+                                        bf16_t* io) const {
     if (n_sp == 1) {
-      mt_store<D>(st, (bf16_t*)a.o + x * D, valid);
+      mt_store<D>(st, io, [&](int r) {
+        return pair(r) < n * group ? (bf16_t*)a.o + at(r) : (bf16_t*)nullptr;
+      });
       return;
     }
+    const size_t first = unit * a.part_rows + 32 * wave_id();
+    mt_store_f32<D>(st, io, [&](int r) {
+      return pair(r) < n * group ? a.part_o + (first + r) * D : (float*)nullptr;
+    });
     const float lse = mt_lse(st, l, scale);
-    if (!valid) return;
-    const int half = opaque_lane() >> 5;
-    const size_t pr = unit * a.part_rows + (row() - r0);
-    float* o = a.part_o + pr * D + 4 * half;
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(o + 32 * dt + 8 * g) =
-            f32x4{st.oacc[dt][4 * g], st.oacc[dt][4 * g + 1], st.oacc[dt][4 * g + 2],
-                  st.oacc[dt][4 * g + 3]};
-    if (half == 0) a.part_lse[pr] = lse;
+    const int r = opaque_lane();
+    if (r < 32 && pair(r) < n * group) a.part_lse[first + r] = lse;
   }
 };
 
@@ -120,13 +115,24 @@ __device__ __forceinline__ TreePiece tree_piece_even(const TreeArgs& a, int pi) 
   return t;
 }
 
+// Inclusive prefix sums over the wave's lanes.
+__device__ __forceinline__ int tree_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return x;
+}
+
 // Otherwise (at most kTrPlanSeqs sequences) into pieces of at most a quota of blocks,
 // the smallest quota tried for which the pieces are at most a.pieces.  Wave-parallel,
 // one lane per sequence; every wave finds the same.
 template <int kChunks>
 __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
   const int lane = threadIdx.x & 63;
-  int bl[kChunks], np[kChunks], longest = 0;
+  int bl[kChunks], np[kChunks], pf[kChunks], longest = 0;
   float total = 0.f;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
@@ -135,13 +141,9 @@ __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
     if (s >= a.num_seqs) bl[c] = 0;
     longest = max(longest, bl[c]);
   }
-  auto lanes_sum = [](auto x) {
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, kWave);
-    return x;
-  };
-#pragma unroll
-  for (int c = 0; c < kChunks; ++c) total += lanes_sum((float)bl[c]);
+  for (int c = 0; c < kChunks; ++c)
+    total += (float)(uint32_t)__builtin_amdgcn_readlane(tree_scan(bl[c]), 63);
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) longest = max(longest, __shfl_xor(longest, m, kWave));
   // (single precision: every wave forms the same numbers, and any cut is a valid one)
@@ -153,32 +155,25 @@ __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
       np[c] = bl[c] > 0 ? min(max((int)ceilf((float)bl[c] * rq - 1e-3f), 1), kTreeMaxSplits) : 0;
-      count += lanes_sum(np[c]);
+      const int incl = tree_scan(np[c]);
+      pf[c] = count + incl - np[c];
+      count += __builtin_amdgcn_readlane(incl, 63);
     }
     // (from the longest on every sequence is one piece: at most num_seqs <= pieces)
     if (count <= a.pieces || q > (float)longest) break;
     q = fmaxf(q * 1.0625f, q + 1.f);
   }
   TreePiece t{-1, 0, 0, 0};
-  int before = 0;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
-    int incl = np[c];
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int y = __shfl_up(incl, d, kWave);
-      if (lane >= d) incl += y;
-    }
-    const int first = before + incl - np[c];
-    const uint64_t at = __builtin_amdgcn_ballot_w64(pi >= first && pi < first + np[c]);
+    const uint64_t at = __builtin_amdgcn_ballot_w64(pi >= pf[c] && pi < pf[c] + np[c]);
     if (at != 0) {
       const int l = __builtin_ctzll(at);
       t.s = c * kWave + l;
-      t.first = __builtin_amdgcn_readlane(first, l);
+      t.first = __builtin_amdgcn_readlane(pf[c], l);
       t.n = __builtin_amdgcn_readlane(np[c], l);
       t.p = pi - t.first;
     }
-    before += __builtin_amdgcn_readlane(incl, 63);
   }
   return t;
 }
@@ -240,7 +235,18 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   const size_t stride = (size_t)a.hkv * a.row_blocks * a.part_rows;     // rows between pieces
   const size_t row = (((size_t)first * a.hkv + kvh) * a.row_blocks + r / kTrRows) * a.part_rows +
                      r % kTrRows;
+  // kBatch pieces requested at a time, the first beside the log-sum-exps.
+  constexpr int kBatch = 8;
   const float lse = lane < n_sp ? a.part_lse[row + lane * stride] : -INFINITY;
+  const float* po = a.part_o + row * D + lane * kPer;
+  float x[kBatch][kPer];
+  auto request = [&](int k0) {
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) x[b][e] = po[min(k0 + b, n_sp - 1) * stride * D + e];
+  };
+  request(0);
   float mx = lse;
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) mx = fmaxf(mx, wave_xor(mx, m));
@@ -251,16 +257,23 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   for (int m = 32; m >= 1; m >>= 1) den += wave_xor(den, m);
   const float inv = den == 0.f ? 0.f : 1.f / den;
   float acc[kPer] = {};
-  const float* po = a.part_o + row * D + lane * kPer;
-  for (int k = 0; k < n_sp; ++k) {
-    const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), k));
+  for (int k0 = 0; k0 < n_sp; k0 += kBatch) {
+    if (k0 > 0) request(k0);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) acc[e] += wk * po[(size_t)k * stride * D + e];
+    for (int b = 0; b < kBatch; ++b) {
+      const float wk = __uint_as_float(
+          __builtin_amdgcn_readlane(__float_as_uint(w), min(k0 + b, n_sp - 1)));
+      if (k0 + b < n_sp) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] += wk * x[b][e];
+      }
+    }
   }
+  bf16_t* o = (bf16_t*)a.o + ((size_t)qb * a.hq + i) * D + lane * kPer;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const __bf16 b = (__bf16)(acc[e] * inv);
-    ((bf16_t*)a.o)[((size_t)qb * a.hq + i) * D + lane * kPer + e] = __builtin_bit_cast(bf16_t, b);
+    o[e] = __builtin_bit_cast(bf16_t, b);
   }
 }
 
