@@ -338,17 +338,26 @@ def rag_kv_cache_write(k, v, k_cache, v_cache, slot_mapping, stream=None) -> Non
         k.shape[1], k.shape[2], k_cache.shape[2], k_cache.shape[0], _stream(stream)))
 
 
-def _here(*tensors):
-    """The tensors are on the current device, where the call is enqueued."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"tensors must be on the current device cuda:{dev}, got {t.device}")
+def _need_all(tensors) -> int:
+    """Each (tensor, dtype, name, rank) is a contiguous tensor of this dtype and
+    rank on the current device, where the call is enqueued; returns that device.
+    (One loop of plain tests: ten tensors cost as much as the launch otherwise.)"""
+    first = tensors[0][0]
+    dev = first.get_device() if isinstance(first, torch.Tensor) else -1
+    for t, dtype, name, ndim in tensors:
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or \
+                dev < 0 or not t.is_contiguous() or t.ndim != ndim:
+            _refuse(t, dtype, name, ndim)
+            raise ValueError(f"{name} is on {t.device}, not on {first.device}")
+    if torch.cuda.current_device() != dev:
+        raise ValueError(f"tensors on cuda:{dev}, not on the current device")
+    return dev
 
 
-def _shape_is(t, shape, name):
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+def _raw_stream(stream, dev):
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def rag_kv_pages_update(block_tables, free_pages, num_free, old_lens, new_lens, num_free_out,
@@ -357,22 +366,21 @@ def rag_kv_pages_update(block_tables, free_pages, num_free, old_lens, new_lens, 
     int32 on the GPU; block_tables [S, max_blocks] and free_pages [num_blocks]
     in and out; num_free, num_free_out and num_granted [1]; lens_out [S],
     cu_new [S+1] and slot_mapping [max_new_tokens] outputs."""
-    for t, n in ((free_pages, "free_pages"), (num_free, "num_free"), (old_lens, "old_lens"),
-                 (new_lens, "new_lens"), (num_free_out, "num_free_out"), (lens_out, "lens_out"),
-                 (cu_new, "cu_new"), (slot_mapping, "slot_mapping"), (num_granted, "num_granted")):
-        _need(t, torch.int32, n, 1)
-    _need(block_tables, torch.int32, "block_tables", 2)
+    i32 = torch.int32
+    dev = _need_all(((block_tables, i32, "block_tables", 2), (free_pages, i32, "free_pages", 1),
+                     (num_free, i32, "num_free", 1), (old_lens, i32, "old_lens", 1),
+                     (new_lens, i32, "new_lens", 1), (num_free_out, i32, "num_free_out", 1),
+                     (lens_out, i32, "lens_out", 1), (cu_new, i32, "cu_new", 1),
+                     (slot_mapping, i32, "slot_mapping", 1), (num_granted, i32, "num_granted", 1)))
     S, width = block_tables.shape
-    if not (old_lens.shape[0] == new_lens.shape[0] == lens_out.shape[0] == S and
-            cu_new.shape[0] == S + 1 and
-            num_free.shape[0] == num_free_out.shape[0] == num_granted.shape[0] == 1):
+    if not (len(old_lens) == len(new_lens) == len(lens_out) == len(cu_new) - 1 == S and
+            len(num_free) == len(num_free_out) == len(num_granted) == 1):
         raise ValueError("kv pages: inconsistent shapes")
-    _here(block_tables, free_pages, num_free, old_lens, new_lens, num_free_out, lens_out, cu_new,
-          slot_mapping, num_granted)
     _check(lib().rag_kv_pages_update(
-        _ptr(block_tables), _ptr(free_pages), _ptr(num_free), _ptr(old_lens), _ptr(new_lens), S,
-        width, free_pages.shape[0], 16, slot_mapping.shape[0], _ptr(num_free_out), _ptr(lens_out),
-        _ptr(cu_new), _ptr(slot_mapping), _ptr(num_granted), _stream(stream)))
+        block_tables.data_ptr(), free_pages.data_ptr(), num_free.data_ptr(), old_lens.data_ptr(),
+        new_lens.data_ptr(), S, width, len(free_pages), 16, len(slot_mapping),
+        num_free_out.data_ptr(), lens_out.data_ptr(), cu_new.data_ptr(), slot_mapping.data_ptr(),
+        num_granted.data_ptr(), _raw_stream(stream, dev)))
 
 
 def rag_kv_cache_keep(k_cache, v_cache, block_tables, base_lens, kept, num_kept,
@@ -380,22 +388,19 @@ def rag_kv_cache_keep(k_cache, v_cache, block_tables, base_lens, kept, num_kept,
     """Moves the K/V rows of the accepted drafted nodes behind their sequence's
     base_lens keys.  Caches [num_blocks, Hkv, 16, d] bf16; block_tables int32
     [S, max_blocks]; base_lens and num_kept int32 [S]; kept int32 [S, max_kept]."""
-    for t, n in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        _need(t, torch.bfloat16, n, 4)
-    _need(block_tables, torch.int32, "block_tables", 2)
-    _need(kept, torch.int32, "kept", 2)
-    _need(base_lens, torch.int32, "base_lens", 1)
-    _need(num_kept, torch.int32, "num_kept", 1)
-    S = block_tables.shape[0]
-    if not (kept.shape[0] == base_lens.shape[0] == num_kept.shape[0] == S) or \
-            v_cache.shape != k_cache.shape:
-        raise ValueError("kv keep: inconsistent shapes")
-    _here(k_cache, v_cache, block_tables, base_lens, kept, num_kept)
+    i32 = torch.int32
+    dev = _need_all(((k_cache, torch.bfloat16, "k_cache", 4), (v_cache, torch.bfloat16, "v_cache", 4),
+                     (block_tables, i32, "block_tables", 2), (kept, i32, "kept", 2),
+                     (base_lens, i32, "base_lens", 1), (num_kept, i32, "num_kept", 1)))
+    S, width = block_tables.shape
+    rows, max_kept = kept.shape
     blocks, hkv, block, d = k_cache.shape
+    if not (rows == len(base_lens) == len(num_kept) == S) or v_cache.shape != k_cache.shape:
+        raise ValueError("kv keep: inconsistent shapes")
     _check(lib().rag_kv_cache_keep(
-        _ptr(k_cache), _ptr(v_cache), _ptr(block_tables), _ptr(base_lens), _ptr(kept),
-        _ptr(num_kept), S, block_tables.shape[1], kept.shape[1], blocks, hkv, d, block,
-        _stream(stream)))
+        k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), base_lens.data_ptr(),
+        kept.data_ptr(), num_kept.data_ptr(), S, width, max_kept, blocks, hkv, d, block,
+        _raw_stream(stream, dev)))
 
 
 def rag_attn_decode_tree_workspace_size(num_seqs, max_nodes, num_q_heads, num_kv_heads, head_dim,
@@ -413,33 +418,30 @@ def rag_attn_decode_paged_tree(q, k_cache, v_cache, o, tree_mask, block_tables, 
     int32 [S, max_blocks]; kv_lens int32 [S], the nodes counted; cu_seqlens_q int32
     [S+1] offsets of the nodes; workspace a GPU tensor (torch.empty, uint8) of
     rag_attn_decode_tree_workspace_size bytes, or None when that size is 0."""
-    _need(q, torch.bfloat16, "q", 3)
-    _need(o, torch.bfloat16, "o", 3)
-    _need(k_cache, torch.bfloat16, "k_cache", 4)
-    _need(v_cache, torch.bfloat16, "v_cache", 4)
-    _need(tree_mask, torch.int64, "tree_mask", 2)
-    _need(block_tables, torch.int32, "block_tables", 2)
-    _need(kv_lens, torch.int32, "kv_lens", 1)
-    _need(cu_seqlens_q, torch.int32, "cu_seqlens_q", 1)
-    S = block_tables.shape[0]
+    i32, bf16 = torch.int32, torch.bfloat16
+    dev = _need_all(((q, bf16, "q", 3), (o, bf16, "o", 3), (k_cache, bf16, "k_cache", 4),
+                     (v_cache, bf16, "v_cache", 4), (tree_mask, torch.int64, "tree_mask", 2),
+                     (block_tables, i32, "block_tables", 2), (kv_lens, i32, "kv_lens", 1),
+                     (cu_seqlens_q, i32, "cu_seqlens_q", 1)))
+    S, width = block_tables.shape
+    rows, hq, dq = q.shape
+    mask_rows, words = tree_mask.shape
     blocks, hkv, block, d = k_cache.shape
-    if o.shape != q.shape or v_cache.shape != k_cache.shape or q.shape[2] != d or \
-            tree_mask.shape[0] != q.shape[0] or kv_lens.shape[0] != S or \
-            cu_seqlens_q.shape[0] != S + 1:
+    if o.shape != q.shape or v_cache.shape != k_cache.shape or dq != d or mask_rows != rows or \
+            not (len(kv_lens) == len(cu_seqlens_q) - 1 == S):
         raise ValueError("decode tree: inconsistent shapes")
-    ws_bytes = 0
+    ws_ptr, ws_bytes = None, 0
     if workspace is not None:
-        if not workspace.is_cuda or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous GPU tensor")
-        ws_bytes = workspace.numel() * workspace.element_size()
-    _here(q, k_cache, v_cache, o, tree_mask, block_tables, kv_lens, cu_seqlens_q, workspace)
-    if q.shape[0] == 0:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the current device")
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if rows == 0:
         return
     _check(lib().rag_attn_decode_paged_tree(
-        _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(o), _ptr(tree_mask), _ptr(block_tables),
-        _ptr(kv_lens), _ptr(cu_seqlens_q), S, int(max_nodes), tree_mask.shape[1],
-        block_tables.shape[1], blocks, q.shape[1], hkv, d, block, float(softmax_scale),
-        int(num_splits), _ptr(workspace), ws_bytes, _stream(stream)))
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), o.data_ptr(), tree_mask.data_ptr(),
+        block_tables.data_ptr(), kv_lens.data_ptr(), cu_seqlens_q.data_ptr(), S, int(max_nodes),
+        words, width, blocks, hq, hkv, d, block, float(softmax_scale), int(num_splits), ws_ptr,
+        ws_bytes, _raw_stream(stream, dev)))
 
 
 def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, key_ranges,
@@ -447,25 +449,23 @@ def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, 
     """q, o [Tq, Hq, d]; k, v [Tk, Hkv, d] bf16; lse fp32 [Hq, Tq] or None;
     cu_seqlens_* int32 [S+1]; key_ranges int32 [Tq, 2]: the (shared, start) of each
     row, which sees the keys j < shared and start <= j <= its position."""
-    for t, n in ((q, "q"), (k, "k"), (v, "v"), (o, "o")):
-        _need(t, torch.bfloat16, n, 3)
-    _need(cu_seqlens_q, torch.int32, "cu_seqlens_q", 1)
-    _need(cu_seqlens_k, torch.int32, "cu_seqlens_k", 1)
-    _need(key_ranges, torch.int32, "key_ranges", 2)
-    if o.shape != q.shape or v.shape != k.shape or k.shape[2] != q.shape[2] or \
-            cu_seqlens_k.shape != cu_seqlens_q.shape:
+    i32, bf16 = torch.int32, torch.bfloat16
+    tensors = ((q, bf16, "q", 3), (k, bf16, "k", 3), (v, bf16, "v", 3), (o, bf16, "o", 3),
+               (cu_seqlens_q, i32, "cu_seqlens_q", 1), (cu_seqlens_k, i32, "cu_seqlens_k", 1),
+               (key_ranges, i32, "key_ranges", 2))
+    dev = _need_all(tensors if lse is None else tensors + ((lse, torch.float32, "lse", 2),))
+    rows, hq, d = q.shape
+    _, hkv, dk = k.shape
+    if o.shape != q.shape or v.shape != k.shape or dk != d or \
+            len(cu_seqlens_k) != len(cu_seqlens_q) or tuple(key_ranges.shape) != (rows, 2) or \
+            (lse is not None and tuple(lse.shape) != (hq, rows)):
         raise ValueError("prefill ranges: inconsistent shapes")
-    _shape_is(key_ranges, (q.shape[0], 2), "key_ranges")
-    if lse is not None:
-        _need(lse, torch.float32, "lse", 2)
-        _shape_is(lse, (q.shape[1], q.shape[0]), "lse")
-    _here(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, key_ranges)
-    if q.shape[0] == 0:
+    if rows == 0:
         return
     _check(lib().rag_attn_prefill_varlen_ranges(
-        _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(cu_seqlens_q), _ptr(cu_seqlens_k),
-        _ptr(key_ranges), cu_seqlens_q.shape[0] - 1, int(max_seqlen_q), int(max_seqlen_k),
-        q.shape[1], k.shape[1], q.shape[2], float(softmax_scale), _stream(stream)))
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), cu_seqlens_q.data_ptr(),
+        cu_seqlens_k.data_ptr(), key_ranges.data_ptr(), len(cu_seqlens_q) - 1, int(max_seqlen_q),
+        int(max_seqlen_k), hq, hkv, d, float(softmax_scale), _raw_stream(stream, dev)))
 
 
 def rag_plan_prompts(method, query_len, num_chunks, chunk_len, intermediate_length=0,

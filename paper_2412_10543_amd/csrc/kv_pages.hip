@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kPgThreads = 256;
 constexpr int kPgWaves = kPgThreads / kWave;
+constexpr int kPgRows = 4;                       // consecutive rows of a thread, at a time
 constexpr int kPgSlots = 4 * kPgThreads;         // slots per workgroup, four a thread
 // Sums stop here: any count above what a call can grant is as good as another,
 // and two of them still fit 32 bits.
@@ -22,31 +23,13 @@ constexpr uint32_t kPgMany = 1u << 30;
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, kPgMany); }
 
 __device__ __forceinline__ uint32_t wave_scan_sat(uint32_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const uint32_t y = __shfl_up(x, d, kWave);
-    if (lane >= d) x = sat_add(x, y);
-  }
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));  // row_shr:1
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));  // row_shr:2
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));  // row_shr:4
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));  // row_shr:8
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));  // row_bcast:15
+  x = sat_add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));  // row_bcast:31
   return x;
-}
-
-// What row r is to gain or give back.
-struct RowChange {
-  uint32_t grow, give, tokens;  // pages taken, pages given back, tokens added
-  int want;                     // pages it is to hold
-};
-
-__device__ __forceinline__ RowChange row_change(const PagesArgs& a, int r) {
-  const int cap = a.max_blocks * 16;             // (max_blocks is below 2^27)
-  const int o = min(max(a.old_lens[r], 0), cap), n = max(a.new_lens[r], 0);
-  const int held = (o + 15) >> 4;
-  RowChange c;
-  c.want = (int)(((uint32_t)n + 15) >> 4);
-  c.grow = (uint32_t)max(c.want - held, 0);
-  c.give = (uint32_t)max(held - c.want, 0);
-  c.tokens = (uint32_t)max(n - o, 0);
-  return c;
 }
 
 }  // namespace
@@ -57,54 +40,86 @@ __device__ __forceinline__ RowChange row_change(const PagesArgs& a, int r) {
 // has the page's first token; the pages themselves follow from the sums, so no
 // workgroup reads what another writes: page number j that is taken is entry
 // n + P - 1 - j of the stack with the P given pages behind its n.
+// A chain of latencies: the lengths, the sums, a row's search, its page's id.
 __global__ __launch_bounds__(kPgThreads) void pages_kernel(PagesArgs a) {
-  extern __shared__ uint32_t sums[];             // tok [S + 1], grow [S + 1], give [S + 1]
-  __shared__ uint32_t wave_sum[3][kPgWaves];
+  // sums of the rows above: tokens added, pages taken, pages given back [S + 1];
+  // tokens held [S]
+  extern __shared__ uint32_t sums[];
+  __shared__ uint32_t wave_sum[2][3][kPgWaves];
   __shared__ int cut;
   const int S = a.num_seqs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t* tok = sums;
   uint32_t* grow = tok + S + 1;
   uint32_t* give = grow + S + 1;
+  int* old = reinterpret_cast<int*>(give + S + 1);
+  const int cap = a.max_blocks * 16;             // (max_blocks is below 2^27)
+  const int n_free = min(max(*a.num_free, 0), a.num_blocks);
   uint32_t base[3] = {0, 0, 0};
-  if (tid == 0) cut = S;
-  for (int r0 = 0; r0 < S; r0 += kPgThreads) {
-    const int r = r0 + tid;
-    RowChange c{0, 0, 0, 0};
-    if (r < S) c = row_change(a, r);
-    const uint32_t v[3] = {min(c.tokens, kPgMany), c.grow, c.give};
-    uint32_t incl[3];
+  if (tid == 0) {
+    cut = S;
+    tok[0] = grow[0] = give[0] = 0;
+  }
+  for (int r0 = 0, turn = 0; r0 < S; r0 += kPgRows * kPgThreads, turn ^= 1) {
+    const int r = r0 + kPgRows * tid;
+    int o[kPgRows], n[kPgRows];
+#pragma unroll
+    for (int k = 0; k < kPgRows; ++k) {
+      const int x = min(r + k, S - 1);
+      o[k] = a.old_lens[x];
+      n[k] = a.new_lens[x];
+    }
+    uint32_t s[3][kPgRows];                      // inclusive
+    uint32_t run[3] = {0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < kPgRows; ++k) {
+      o[k] = min(max(o[k], 0), cap);
+      n[k] = max(n[k], 0);
+      const bool real = r + k < S;
+      const int held = (o[k] + 15) >> 4, want = (int)(((uint32_t)n[k] + 15) >> 4);
+      const uint32_t v[3] = {real ? min((uint32_t)max(n[k] - o[k], 0), kPgMany) : 0u,
+                             real ? (uint32_t)max(want - held, 0) : 0u,
+                             real ? (uint32_t)max(held - want, 0) : 0u};
+#pragma unroll
+      for (int i = 0; i < 3; ++i) s[i][k] = run[i] = sat_add(run[i], v[i]);
+    }
+    uint32_t upto[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      incl[i] = wave_scan_sat(v[i]);
-      if (lane == 63) wave_sum[i][wave] = incl[i];
+      upto[i] = wave_scan_sat(run[i]);
+      if (lane == 63) wave_sum[turn][i][wave] = upto[i];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      uint32_t before = base[i];
+      uint32_t before = base[i], all = base[i];
 #pragma unroll
       for (int w = 0; w < kPgWaves; ++w) {
-        if (w == wave && r < S) {
-          // (inclusive sums at r + 1: entry r is then the sum of the rows above)
-          (i == 0 ? tok : i == 1 ? grow : give)[r + 1] = sat_add(before, incl[i]);
-        }
-        before = sat_add(before, wave_sum[i][w]);
+        if (w < wave) before = sat_add(before, wave_sum[turn][i][w]);
+        all = sat_add(all, wave_sum[turn][i][w]);
       }
-      base[i] = before;
+      base[i] = all;
+      // (the lane's own rows leave the wave's sum up to it: below the limit sums are
+      // exact, and at it the difference does not matter: rows there do not fit)
+      const uint32_t up = __shfl_up(upto[i], 1, kWave);
+      if (lane > 0) before = sat_add(before, up);
+      uint32_t* to = i == 0 ? tok : i == 1 ? grow : give;
+#pragma unroll
+      for (int k = 0; k < kPgRows; ++k)
+        if (r + k < S) to[r + k + 1] = sat_add(before, s[i][k]);
     }
-    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPgRows; ++k)
+      if (r + k < S) old[r + k] = o[k];
   }
-  if (tid == 0) tok[0] = grow[0] = give[0] = 0;
   __syncthreads();
   // Rows grow up to the first that does not fit.
-  const int n_free = min(max(*a.num_free, 0), a.num_blocks);
-  const uint32_t given = give[S];
-  const uint32_t avail = min((uint32_t)n_free + given, (uint32_t)a.num_blocks);
+  const uint32_t avail = min((uint32_t)n_free + give[S], (uint32_t)a.num_blocks);
   for (int r = tid; r < S; r += kPgThreads) {
-    if (tok[r + 1] == tok[r] && tok[r] < kPgMany) continue;    // adds nothing
-    if (row_change(a, r).tokens == 0) continue;
-    const bool fits = grow[r + 1] <= avail && tok[r + 1] <= (uint32_t)a.max_new_tokens &&
-                      row_change(a, r).want <= a.max_blocks;
+    const uint32_t t0 = tok[r], t1 = tok[r + 1], g0 = grow[r], g1 = grow[r + 1];
+    if (t1 == t0 && t0 < kPgMany) continue;      // adds nothing
+    // (sums at the limit fit neither; below it a row's pages are g1 - g0 more)
+    const bool fits = g1 <= avail && t1 <= (uint32_t)a.max_new_tokens &&
+                      (uint32_t)((old[r] + 15) >> 4) + (g1 - g0) <= (uint32_t)a.max_blocks;
     if (!fits) atomicMin(&cut, r);
   }
   __syncthreads();
@@ -122,8 +137,8 @@ __global__ __launch_bounds__(kPgThreads) void pages_kernel(PagesArgs a) {
       const int mid = (lo + hi + 1) >> 1;
       if (give[mid] <= g) lo = mid; else hi = mid - 1;
     }
-    const int want = max(row_change(a, lo).want, 0) + (int)(g - give[lo]);
-    return a.tables[(size_t)lo * a.max_blocks + min(want, a.max_blocks - 1)];
+    const int at = ((old[lo] + 15) >> 4) - (int)(give[lo + 1] - g);   // behind what it keeps
+    return a.tables[(size_t)lo * a.max_blocks + min(max(at, 0), a.max_blocks - 1)];
   };
 
   // ---- slots ----------------------------------------------------------------
@@ -137,7 +152,7 @@ __global__ __launch_bounds__(kPgThreads) void pages_kernel(PagesArgs a) {
         if ((int)tok[mid] <= i0) lo = mid; else hi = mid - 1;
       }
       int row = lo, page = -1, id = 0;
-      int o = min(max(a.old_lens[row], 0), a.max_blocks * 16);
+      int o = old[row];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = i0 + e;
@@ -145,7 +160,7 @@ __global__ __launch_bounds__(kPgThreads) void pages_kernel(PagesArgs a) {
         while ((int)tok[row + 1] <= i) {
           ++row;
           page = -1;
-          o = min(max(a.old_lens[row], 0), a.max_blocks * 16);
+          o = old[row];
         }
         const int t = o + (i - (int)tok[row]), p = t >> 4, held = (o + 15) >> 4;
         if (p != page) {
@@ -186,7 +201,7 @@ int64_t pages_grid(const PagesArgs& a) {
 }
 
 hipError_t launch_pages(const PagesArgs& a, hipStream_t stream) {
-  const size_t lds = 3 * ((size_t)a.num_seqs + 1) * sizeof(uint32_t);
+  const size_t lds = (4 * (size_t)a.num_seqs + 3) * sizeof(uint32_t);
   hipLaunchKernelGGL(pages_kernel, dim3((unsigned)pages_grid(a)), dim3(kPgThreads), lds, stream, a);
   return hipGetLastError();
 }
