@@ -42,6 +42,7 @@ _i32 = ctypes.c_int32
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _vp = ctypes.c_void_p
 _lib = None
+_marshal = None
 
 
 def exported_symbols():
@@ -81,7 +82,7 @@ class Config(ctypes.Structure):
 
 def lib():
     """Load (once) and return the ctypes handle of librag_attn.so."""
-    global _lib
+    global _lib, _marshal
     if _lib is not None:
         return _lib
     if not os.path.exists(LIBRARY):
@@ -150,6 +151,7 @@ def lib():
     L.rag_plan_prompts.restype = ctypes.c_int
     L.rag_plan_prompts.argtypes = [ctypes.c_int, _i32, _i32p, _i32p, _i32, _i32, _i32, _i32p,
                                    _i32, _i32p, _i32p]
+    from . import _marshal
     _lib = L
     return L
 
@@ -338,20 +340,24 @@ def rag_kv_cache_write(k, v, k_cache, v_cache, slot_mapping, stream=None) -> Non
         k.shape[1], k.shape[2], k_cache.shape[2], k_cache.shape[0], _stream(stream)))
 
 
-def _need_all(tensors) -> int:
-    """Each (tensor, dtype, name, rank) is a contiguous tensor of this dtype and
-    rank on the current device, where the call is enqueued; returns that device.
-    (One loop of plain tests: ten tensors cost as much as the launch otherwise.)"""
-    first = tensors[0][0]
-    dev = first.get_device() if isinstance(first, torch.Tensor) else -1
-    for t, dtype, name, ndim in tensors:
-        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or \
-                dev < 0 or not t.is_contiguous() or t.ndim != ndim:
-            _refuse(t, dtype, name, ndim)
-            raise ValueError(f"{name} is on {t.device}, not on {first.device}")
-    if torch.cuda.current_device() != dev:
-        raise ValueError(f"tensors on cuda:{dev}, not on the current device")
-    return dev
+def _pointers(spec, *tensors):
+    """(device, address and sizes of each tensor) of contiguous tensors on the
+    current device, with the types and ranks of spec (see csrc/marshal.cpp), or a
+    number for _refuse_at."""
+    lib()
+    return _marshal.pointers(spec, *tensors)
+
+
+_TYPES = {"i": torch.int32, "l": torch.int64, "b": torch.bfloat16, "f": torch.float32}
+
+
+def _refuse_at(i, spec, names, tensors):
+    """Why tensor i was not taken."""
+    if i == len(tensors):
+        raise ValueError(f"tensors on {tensors[0].device}, not on the current device")
+    t, name = tensors[i], names.split()[i]
+    _refuse(t, _TYPES[chr(spec[2 * i]).lower()], name, spec[2 * i + 1] - ord("0"))
+    raise ValueError(f"{name} is on {t.device}, not on {tensors[0].device}")
 
 
 def _raw_stream(stream, dev):
@@ -366,21 +372,20 @@ def rag_kv_pages_update(block_tables, free_pages, num_free, old_lens, new_lens, 
     int32 on the GPU; block_tables [S, max_blocks] and free_pages [num_blocks]
     in and out; num_free, num_free_out and num_granted [1]; lens_out [S],
     cu_new [S+1] and slot_mapping [max_new_tokens] outputs."""
-    i32 = torch.int32
-    dev = _need_all(((block_tables, i32, "block_tables", 2), (free_pages, i32, "free_pages", 1),
-                     (num_free, i32, "num_free", 1), (old_lens, i32, "old_lens", 1),
-                     (new_lens, i32, "new_lens", 1), (num_free_out, i32, "num_free_out", 1),
-                     (lens_out, i32, "lens_out", 1), (cu_new, i32, "cu_new", 1),
-                     (slot_mapping, i32, "slot_mapping", 1), (num_granted, i32, "num_granted", 1)))
-    S, width = block_tables.shape
-    if not (len(old_lens) == len(new_lens) == len(lens_out) == len(cu_new) - 1 == S and
-            len(num_free) == len(num_free_out) == len(num_granted) == 1):
+    t = (block_tables, free_pages, num_free, old_lens, new_lens, num_free_out, lens_out, cu_new,
+         slot_mapping, num_granted)
+    p = _pointers(b"i2i1i1i1i1i1i1i1i1i1", *t)
+    if p.__class__ is int:
+        _refuse_at(p, b"i2i1i1i1i1i1i1i1i1i1", "block_tables free_pages num_free old_lens new_lens "
+                   "num_free_out lens_out cu_new slot_mapping num_granted", t)
+    dev, table, S, width, pages, blocks, free, one, old, rows, new, rows2, free_out, one2, lens, rows3, \
+        cu, rows1, slots, tokens, granted, one3 = p
+    if not (rows == rows2 == rows3 == rows1 - 1 == S and one == one2 == one3 == 1):
         raise ValueError("kv pages: inconsistent shapes")
-    _check(lib().rag_kv_pages_update(
-        block_tables.data_ptr(), free_pages.data_ptr(), num_free.data_ptr(), old_lens.data_ptr(),
-        new_lens.data_ptr(), S, width, len(free_pages), 16, len(slot_mapping),
-        num_free_out.data_ptr(), lens_out.data_ptr(), cu_new.data_ptr(), slot_mapping.data_ptr(),
-        num_granted.data_ptr(), _raw_stream(stream, dev)))
+    status = _lib.rag_kv_pages_update(table, pages, free, old, new, S, width, blocks, 16, tokens,
+                                      free_out, lens, cu, slots, granted, _raw_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 def rag_kv_cache_keep(k_cache, v_cache, block_tables, base_lens, kept, num_kept,
@@ -388,19 +393,18 @@ def rag_kv_cache_keep(k_cache, v_cache, block_tables, base_lens, kept, num_kept,
     """Moves the K/V rows of the accepted drafted nodes behind their sequence's
     base_lens keys.  Caches [num_blocks, Hkv, 16, d] bf16; block_tables int32
     [S, max_blocks]; base_lens and num_kept int32 [S]; kept int32 [S, max_kept]."""
-    i32 = torch.int32
-    dev = _need_all(((k_cache, torch.bfloat16, "k_cache", 4), (v_cache, torch.bfloat16, "v_cache", 4),
-                     (block_tables, i32, "block_tables", 2), (kept, i32, "kept", 2),
-                     (base_lens, i32, "base_lens", 1), (num_kept, i32, "num_kept", 1)))
-    S, width = block_tables.shape
-    rows, max_kept = kept.shape
-    blocks, hkv, block, d = k_cache.shape
-    if not (rows == len(base_lens) == len(num_kept) == S) or v_cache.shape != k_cache.shape:
+    t = (k_cache, v_cache, block_tables, kept, base_lens, num_kept)
+    p = _pointers(b"b4b4i2i2i1i1", *t)
+    if p.__class__ is int:
+        _refuse_at(p, b"b4b4i2i2i1i1", "k_cache v_cache block_tables kept base_lens num_kept", t)
+    dev, kc, blocks, hkv, block, d, vc, b2, h2, s2, d2, table, S, width, nodes, rows, max_kept, base, \
+        rows2, num, rows3 = p
+    if not rows == rows2 == rows3 == S or (b2, h2, s2, d2) != (blocks, hkv, block, d):
         raise ValueError("kv keep: inconsistent shapes")
-    _check(lib().rag_kv_cache_keep(
-        k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), base_lens.data_ptr(),
-        kept.data_ptr(), num_kept.data_ptr(), S, width, max_kept, blocks, hkv, d, block,
-        _raw_stream(stream, dev)))
+    status = _lib.rag_kv_cache_keep(kc, vc, table, base, nodes, num, S, width, max_kept, blocks, hkv,
+                                    d, block, _raw_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 def rag_attn_decode_tree_workspace_size(num_seqs, max_nodes, num_q_heads, num_kv_heads, head_dim,
@@ -418,17 +422,15 @@ def rag_attn_decode_paged_tree(q, k_cache, v_cache, o, tree_mask, block_tables, 
     int32 [S, max_blocks]; kv_lens int32 [S], the nodes counted; cu_seqlens_q int32
     [S+1] offsets of the nodes; workspace a GPU tensor (torch.empty, uint8) of
     rag_attn_decode_tree_workspace_size bytes, or None when that size is 0."""
-    i32, bf16 = torch.int32, torch.bfloat16
-    dev = _need_all(((q, bf16, "q", 3), (o, bf16, "o", 3), (k_cache, bf16, "k_cache", 4),
-                     (v_cache, bf16, "v_cache", 4), (tree_mask, torch.int64, "tree_mask", 2),
-                     (block_tables, i32, "block_tables", 2), (kv_lens, i32, "kv_lens", 1),
-                     (cu_seqlens_q, i32, "cu_seqlens_q", 1)))
-    S, width = block_tables.shape
-    rows, hq, dq = q.shape
-    mask_rows, words = tree_mask.shape
-    blocks, hkv, block, d = k_cache.shape
-    if o.shape != q.shape or v_cache.shape != k_cache.shape or dq != d or mask_rows != rows or \
-            not (len(kv_lens) == len(cu_seqlens_q) - 1 == S):
+    t = (q, o, k_cache, v_cache, tree_mask, block_tables, kv_lens, cu_seqlens_q)
+    p = _pointers(b"b3b3b4b4l2i2i1i1", *t)
+    if p.__class__ is int:
+        _refuse_at(p, b"b3b3b4b4l2i2i1i1", "q o k_cache v_cache tree_mask block_tables kv_lens "
+                   "cu_seqlens_q", t)
+    dev, qp, rows, hq, dq, op, rows2, hq2, dq2, kc, blocks, hkv, block, d, vc, b2, h2, s2, d2, mask, \
+        rows3, words, table, S, width, kv, seqs, cu, seqs1 = p
+    if (rows2, hq2, dq2) != (rows, hq, dq) or (b2, h2, s2, d2) != (blocks, hkv, block, d) or \
+            dq != d or rows3 != rows or not seqs == seqs1 - 1 == S:
         raise ValueError("decode tree: inconsistent shapes")
     ws_ptr, ws_bytes = None, 0
     if workspace is not None:
@@ -437,11 +439,11 @@ def rag_attn_decode_paged_tree(q, k_cache, v_cache, o, tree_mask, block_tables, 
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     if rows == 0:
         return
-    _check(lib().rag_attn_decode_paged_tree(
-        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), o.data_ptr(), tree_mask.data_ptr(),
-        block_tables.data_ptr(), kv_lens.data_ptr(), cu_seqlens_q.data_ptr(), S, int(max_nodes),
-        words, width, blocks, hq, hkv, d, block, float(softmax_scale), int(num_splits), ws_ptr,
-        ws_bytes, _raw_stream(stream, dev)))
+    status = _lib.rag_attn_decode_paged_tree(
+        qp, kc, vc, op, mask, table, kv, cu, S, int(max_nodes), words, width, blocks, hq, hkv, d,
+        block, float(softmax_scale), int(num_splits), ws_ptr, ws_bytes, _raw_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, key_ranges,
@@ -449,23 +451,22 @@ def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, 
     """q, o [Tq, Hq, d]; k, v [Tk, Hkv, d] bf16; lse fp32 [Hq, Tq] or None;
     cu_seqlens_* int32 [S+1]; key_ranges int32 [Tq, 2]: the (shared, start) of each
     row, which sees the keys j < shared and start <= j <= its position."""
-    i32, bf16 = torch.int32, torch.bfloat16
-    tensors = ((q, bf16, "q", 3), (k, bf16, "k", 3), (v, bf16, "v", 3), (o, bf16, "o", 3),
-               (cu_seqlens_q, i32, "cu_seqlens_q", 1), (cu_seqlens_k, i32, "cu_seqlens_k", 1),
-               (key_ranges, i32, "key_ranges", 2))
-    dev = _need_all(tensors if lse is None else tensors + ((lse, torch.float32, "lse", 2),))
-    rows, hq, d = q.shape
-    _, hkv, dk = k.shape
-    if o.shape != q.shape or v.shape != k.shape or dk != d or \
-            len(cu_seqlens_k) != len(cu_seqlens_q) or tuple(key_ranges.shape) != (rows, 2) or \
-            (lse is not None and tuple(lse.shape) != (hq, rows)):
+    t = (q, k, v, o, cu_seqlens_q, cu_seqlens_k, key_ranges, lse)
+    p = _pointers(b"b3b3b3b3i1i1i2F2", *t)
+    if p.__class__ is int:
+        _refuse_at(p, b"b3b3b3b3i1i1i2F2", "q k v o cu_seqlens_q cu_seqlens_k key_ranges lse", t)
+    dev, qp, rows, hq, d, kp, keys, hkv, dk, vp, keys2, hkv2, dv, op, rows2, hq2, d2, cu_q, seqs1, \
+        cu_k, seqs2, ranges, rows3, two, lse_p = p[:25]
+    if (rows2, hq2, d2) != (rows, hq, d) or (keys2, hkv2, dv) != (keys, hkv, d) or dk != d or \
+            seqs1 != seqs2 or (rows3, two) != (rows, 2) or p[25:] not in ((), (hq, rows)):
         raise ValueError("prefill ranges: inconsistent shapes")
     if rows == 0:
         return
-    _check(lib().rag_attn_prefill_varlen_ranges(
-        q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), cu_seqlens_q.data_ptr(),
-        cu_seqlens_k.data_ptr(), key_ranges.data_ptr(), len(cu_seqlens_q) - 1, int(max_seqlen_q),
-        int(max_seqlen_k), hq, hkv, d, float(softmax_scale), _raw_stream(stream, dev)))
+    status = _lib.rag_attn_prefill_varlen_ranges(
+        qp, kp, vp, op, lse_p, cu_q, cu_k, ranges, seqs1 - 1, int(max_seqlen_q), int(max_seqlen_k),
+        hq, hkv, d, float(softmax_scale), _raw_stream(stream, dev))
+    if status:
+        _check(status)
 
 
 def rag_plan_prompts(method, query_len, num_chunks, chunk_len, intermediate_length=0,

@@ -51,6 +51,28 @@ def build_probes(verbose: bool = False) -> str:
     return PROBES
 
 
+MARSHAL = os.path.join(PKG, "_marshal.so")
+
+
+def build_marshal(verbose: bool = False) -> str:
+    """The binding's checks of tensors (host code against torch's headers)."""
+    import sysconfig
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    tmp = MARSHAL + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(f"-I{p}" for p in include_paths("cuda")), "-I" + sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "marshal.cpp"), "-o", tmp,
+           *(f"-L{p}" for p in library_paths("cuda")), "-ltorch_python", "-ltorch", "-ltorch_cpu",
+           "-lc10", "-lc10_hip"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True, stderr=None if verbose else subprocess.PIPE)
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
     objs = []
@@ -70,6 +92,7 @@ def build(verbose: bool = False) -> str:
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIBRARY)
     build_probes(verbose)
+    build_marshal(verbose)
     return LIBRARY
 
 

@@ -122,6 +122,9 @@ def test_binding_refuses_what_is_not_on_the_gpu():
                                                                 1.0)):
         with pytest.raises(ValueError, match="GPU tensor"):
             call()
+    for first in (None, [1, 2], 7):
+        with pytest.raises(TypeError, match="q must be a torch.Tensor"):
+            binding.rag_attn_prefill_varlen_ranges(first, x, x, x, None, i32, i32, t, 4, 4, 1.0)
 
 
 # ---------------------------------------------------------------------------
