@@ -199,8 +199,8 @@ __device__ __forceinline__ uint32_t lds_offset(const bf16_t* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char*)p);
 }
 
-// Slots of an item of n blocks: an even number, and at least four where another
-// item follows, whose first four K blocks are requested in the last four slots.
+// Slots of an item of n blocks: an even number, and at least a ring's where another
+// item follows, whose first K blocks are requested in those last slots.
 __device__ __forceinline__ int mt_slots(int n, bool more) {
   const int even = (n + 1) & ~1;
   return more ? max(even, kMtRing) : even;
@@ -220,7 +220,7 @@ struct BlockCopy {
   using Lay = BlockLayout<D>;
   static constexpr int kInstr = kMtKeys * Lay::kCh / (64 * kMtWaves);
   static_assert(kInstr == 1 || kInstr == 2, "block staging layout");
-  const KV& kv;
+  KV kv;
   int nk;                       // keys of the sequence, at least one
   int page;                     // page in the block of the wave's first instruction
   int run;                      // blocks left of the run at hand
@@ -374,6 +374,71 @@ __device__ __forceinline__ void mt_place_q(PfState<D>& st, bf16_t* io) {
   }
 }
 
+// A row's normalised output, element j of d tile dt at
+// d = 32 dt + 8 (j / 4) + 4 half + j % 4; returns its sum of weights.
+template <int D>
+__device__ __forceinline__ float mt_finish(PfState<D>& st) {
+  const float l = st.l + wave_xor(st.l, 32);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) st.oacc[dt][j] *= inv;
+  return l;
+}
+// And its log-sum-exp.
+template <int D>
+__device__ __forceinline__ float mt_lse(const PfState<D>& st, float l, float scale) {
+  return l == 0.f ? -INFINITY : st.m_used * scale + logf(l);
+}
+
+// Stores the wave's rows: rows(r) is where row r goes, or null.
+template <int D, class RowPtr>
+__device__ __forceinline__ void mt_store(const PfState<D>& st, bf16_t* io, const RowPtr& rows) {
+  const int lane = opaque_lane(), c = lane & 3, r = lane & 31, half = lane >> 5;
+  bf16_t* const to[2] = {rows(lane >> 2), rows((lane >> 2) + 16)};
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) {
+    const f32x16& o = st.oacc[dt];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<bf16x4*>(io + io_at(r, g) + 4 * half) =
+          to_bf16x4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
+    wave_lds_sync();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(io + io_at((lane >> 2) + 16 * i, c));
+      if (to[i] != nullptr) *reinterpret_cast<u32x4*>(to[i] + 32 * dt + 8 * c) = x;
+    }
+    wave_lds_sync();
+  }
+}
+
+// The same in fp32.
+template <int D, class RowPtr>
+__device__ __forceinline__ void mt_store_f32(const PfState<D>& st, bf16_t* io_, const RowPtr& rows) {
+  const int lane = opaque_lane(), c = lane & 3, r = lane & 31, half = lane >> 5;
+  float* const to[2] = {rows(lane >> 2), rows((lane >> 2) + 16)};
+  float* io = reinterpret_cast<float*>(io_);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                // columns 32 dt + 16 h on
+      const f32x16& o = st.oacc[dt];
+#pragma unroll
+      for (int g = 2 * h; g < 2 * h + 2; ++g)
+        *reinterpret_cast<f32x4*>(io + io_at(r, 2 * (g & 1) + half) / 2) =
+            f32x4{o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]};
+      wave_lds_sync();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(io + io_at((lane >> 2) + 16 * i, c) / 2);
+        if (to[i] != nullptr) *reinterpret_cast<f32x4*>(to[i] + 32 * dt + 16 * h + 4 * c) = x;
+      }
+      wave_lds_sync();
+    }
+}
+
 // The rows of one wave against the blocks of an item, where keys that some row
 // does not see have infinite or NaN values: one block at a time.  st.qf is set.
 template <int D, class Rows, class KV>
@@ -413,7 +478,9 @@ __device__ __forceinline__ void masked_item_odd(const Rows& rows, const KV& kv, 
 }
 
 // LDS of a workgroup: rings of K and V blocks, a block of zeros, and the waves'
-// 2 KiB for rows to and from memory (80 KiB at D = 128: two workgroups a CU).
+// 2 KiB for rows to and from memory (80 KiB at D = 128: two workgroups a CU; rings
+// of eight blocks where a launch leaves one to a CU cost 0.7 to 2.3 us a call, of
+// 10 to 20, for the longer start, and gained nothing).
 template <int D>
 struct MtLds {
   bf16_t k[kMtRing * BlockLayout<D>::kElems];
@@ -470,7 +537,7 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
     kc.ready(sp, 0);
     kc.next();
     kc.all(i);
-    if (i < 2) {
+    if (i < kMtRing - 2) {
       vc.ready(sp, 0);
       vc.next();
       vc.all(i);
@@ -567,9 +634,9 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
       turn();
       slot(i + 1, sO, sE, pO, pE, lds.k + rb, i + 1 > n ? lds.zero : lds.v + ra,
            copies(MtInt<kBytes>{}, ra * sizeof(bf16_t), rb * sizeof(bf16_t)));
-      const int t = ra;
+      const int x = ra;
       ra = rb;
-      rb = t;
+      rb = x;
     }
     // The copies are in the next item by now (an item has four slots), and may go on
     // to the one behind it.
@@ -631,71 +698,6 @@ __device__ __forceinline__ void masked_items(Src& src, const KV& kv, int nk, flo
     masked_item_odd<D>(src.rows, kv, sp, nk, scale, lds.k, lds.v, st);
     src.store(m, st, mt_finish<D>(st), scale, io);
   }
-}
-
-// A row's normalised output, element j of d tile dt at
-// d = 32 dt + 8 (j / 4) + 4 half + j % 4; returns its sum of weights.
-template <int D>
-__device__ __forceinline__ float mt_finish(PfState<D>& st) {
-  const float l = st.l + wave_xor(st.l, 32);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) st.oacc[dt][j] *= inv;
-  return l;
-}
-// And its log-sum-exp.
-template <int D>
-__device__ __forceinline__ float mt_lse(const PfState<D>& st, float l, float scale) {
-  return l == 0.f ? -INFINITY : st.m_used * scale + logf(l);
-}
-
-// Stores the wave's rows: rows(r) is where row r goes, or null.
-template <int D, class RowPtr>
-__device__ __forceinline__ void mt_store(const PfState<D>& st, bf16_t* io, const RowPtr& rows) {
-  const int lane = opaque_lane(), c = lane & 3, r = lane & 31, half = lane >> 5;
-  bf16_t* const to[2] = {rows(lane >> 2), rows((lane >> 2) + 16)};
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt) {
-    const f32x16& o = st.oacc[dt];
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<bf16x4*>(io + io_at(r, g) + 4 * half) =
-          to_bf16x4(o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]);
-    wave_lds_sync();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(io + io_at((lane >> 2) + 16 * i, c));
-      if (to[i] != nullptr) *reinterpret_cast<u32x4*>(to[i] + 32 * dt + 8 * c) = x;
-    }
-    wave_lds_sync();
-  }
-}
-
-// The same in fp32.
-template <int D, class RowPtr>
-__device__ __forceinline__ void mt_store_f32(const PfState<D>& st, bf16_t* io_, const RowPtr& rows) {
-  const int lane = opaque_lane(), c = lane & 3, r = lane & 31, half = lane >> 5;
-  float* const to[2] = {rows(lane >> 2), rows((lane >> 2) + 16)};
-  float* io = reinterpret_cast<float*>(io_);
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {                // columns 32 dt + 16 h on
-      const f32x16& o = st.oacc[dt];
-#pragma unroll
-      for (int g = 2 * h; g < 2 * h + 2; ++g)
-        *reinterpret_cast<f32x4*>(io + io_at(r, 2 * (g & 1) + half) / 2) =
-            f32x4{o[4 * g], o[4 * g + 1], o[4 * g + 2], o[4 * g + 3]};
-      wave_lds_sync();
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(io + io_at((lane >> 2) + 16 * i, c) / 2);
-        if (to[i] != nullptr) *reinterpret_cast<f32x4*>(to[i] + 32 * dt + 16 * h + 4 * c) = x;
-      }
-      wave_lds_sync();
-    }
 }
 
 }  // namespace rag

@@ -18,24 +18,23 @@ namespace {
 
 constexpr int kTrRows = 32 * kMtWaves;
 constexpr int kTrPlanSeqs = 256;     // sequences whose pieces are cut from their lengths
-#ifndef RAG_TR_MIN
-#define RAG_TR_MIN 8
-#endif
-#ifndef RAG_TR_ROUNDS
-#define RAG_TR_ROUNDS 1
-#endif
-constexpr int kTrMinBlocks = RAG_TR_MIN;    // blocks a piece is cut for, at least
-constexpr int kTrRounds = RAG_TR_ROUNDS;
+// Blocks that a piece is cut for, at least: a unit's start, end and join cost about
+// as much as eight.  One sequence of 8192 keys, 32 q / 8 kv heads, 32 nodes: 19.9 us;
+// cut down to 4 blocks 22.4, to 16 23.5, to 32 34.8.
+constexpr int kTrMinBlocks = 8;
 
 // What the lane's row sees.
 struct TreeRows {
-  const uint64_t* mask;         // its node's words
+  const uint64_t* mask;         // its node's words, the first two of them loaded
+  uint64_t w0, w1;
   int prior, n, words;          // keys before the nodes; nodes; words per node
   __device__ __forceinline__ FullBlocks full_blocks(const KeySpans& sp) const {
     return {max(prior - sp.a0, 0) / kMtKeys, 0, 0};
   }
   __device__ __forceinline__ uint64_t word(int w) const {
-    return w >= 0 && w < words ? mask[w] : 0;
+    // (w is the same for the wave; a load waits for every copy in flight)
+    if (w < 0 || w >= words) return 0;
+    return w == 0 ? w0 : w == 1 ? w1 : mask[w];
   }
   __device__ __forceinline__ uint32_t seen(int k0) const {
     const int j0 = k0 - prior;                   // node of the block's first key (may be < 0)
@@ -69,6 +68,8 @@ struct TreeSrc {
     rows.prior = kv_len - n;
     rows.n = n;
     rows.words = a.mask_words;
+    rows.w0 = rows.mask[0];
+    rows.w1 = rows.mask[min(1, a.mask_words - 1)];
     return spans;
   }
   __device__ __forceinline__ const bf16_t* q(int, int r) const { return (const bf16_t*)a.q + at(r); }
@@ -92,15 +93,16 @@ struct TreeSrc {
 
 }  // namespace
 
-__device__ __forceinline__ int tree_blocks(const TreeArgs& a, int s) {   // of sequence s
-  if (a.cu_q[s + 1] - a.cu_q[s] <= 0) return 0;
-  return (min(a.kv_lens[s], a.max_blocks * 16) + kMtKeys - 1) / kMtKeys;
+// Blocks of a sequence with n nodes and kv_len keys.
+__device__ __forceinline__ int tree_blocks(const TreeArgs& a, int n, int kv_len) {
+  return n <= 0 ? 0 : (min(kv_len, a.max_blocks * 16) + kMtKeys - 1) / kMtKeys;
 }
 
 // Piece `pi` of the launch: sequence s (-1: there is no such piece), the p-th of
 // its n pieces; `first` its first.
 struct TreePiece {
   int s, p, n, first;
+  int qb, nodes, kv_len;        // of sequence s
 };
 
 // With a number of splits given every sequence is cut into that many (or its
@@ -110,7 +112,10 @@ __device__ __forceinline__ TreePiece tree_piece_even(const TreeArgs& a, int pi) 
   t.s = pi / a.splits;
   t.p = pi % a.splits;
   t.first = pi - t.p;
-  t.n = t.s < a.num_seqs ? min(a.splits, max(tree_blocks(a, t.s), 1)) : 0;
+  t.qb = uniform_load(a.cu_q, t.s);
+  t.nodes = uniform_load(a.cu_q, t.s + 1) - t.qb;
+  t.kv_len = uniform_load(a.kv_lens, t.s);
+  t.n = min(a.splits, max(tree_blocks(a, t.nodes, t.kv_len), 1));
   if (t.p >= t.n) t.s = -1;
   return t;
 }
@@ -132,12 +137,16 @@ __device__ __forceinline__ int tree_scan(int x) {
 template <int kChunks>
 __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
   const int lane = threadIdx.x & 63;
-  int bl[kChunks], np[kChunks], pf[kChunks], longest = 0;
+  int bl[kChunks], np[kChunks], pf[kChunks], qb[kChunks], qe[kChunks], kv[kChunks], longest = 0;
   float total = 0.f;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
     const int s = c * kWave + lane;
-    bl[c] = tree_blocks(a, min(s, a.num_seqs - 1));
+    const int x = min(s, a.num_seqs - 1);
+    qb[c] = a.cu_q[x];
+    qe[c] = a.cu_q[x + 1];
+    kv[c] = a.kv_lens[x];
+    bl[c] = tree_blocks(a, qe[c] - qb[c], kv[c]);
     if (s >= a.num_seqs) bl[c] = 0;
     longest = max(longest, bl[c]);
   }
@@ -163,7 +172,7 @@ __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
     if (count <= a.pieces || q > (float)longest) break;
     q = fmaxf(q * 1.0625f, q + 1.f);
   }
-  TreePiece t{-1, 0, 0, 0};
+  TreePiece t{-1, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
     const uint64_t at = __builtin_amdgcn_ballot_w64(pi >= pf[c] && pi < pf[c] + np[c]);
@@ -173,6 +182,9 @@ __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
       t.first = __builtin_amdgcn_readlane(pf[c], l);
       t.n = __builtin_amdgcn_readlane(np[c], l);
       t.p = pi - t.first;
+      t.qb = __builtin_amdgcn_readlane(qb[c], l);
+      t.nodes = __builtin_amdgcn_readlane(qe[c], l) - t.qb;
+      t.kv_len = __builtin_amdgcn_readlane(kv[c], l);
     }
   }
   return t;
@@ -198,10 +210,10 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
   if (p == 0 && rb == 0 && kvh == 0 && threadIdx.x == 0 && a.part_of != nullptr)
     reinterpret_cast<int2*>(a.part_of)[s] = int2{t.first, t.n};   // for the join
   TreeSrc<D> src{a};
-  src.qb = uniform_load(a.cu_q, s);
-  src.n = uniform_load(a.cu_q, s + 1) - src.qb;
+  src.qb = __builtin_amdgcn_readfirstlane(t.qb);
+  src.n = __builtin_amdgcn_readfirstlane(t.nodes);
   src.r0 = rb * kTrRows;
-  const int nk = min(uniform_load(a.kv_lens, s), a.max_blocks * 16);
+  const int nk = min(__builtin_amdgcn_readfirstlane(t.kv_len), a.max_blocks * 16);
   if (src.r0 >= src.n * group || nk <= 0) return;
   src.n_sp = n_sp;
   src.unit = ((size_t)pi * a.hkv + kvh) * a.row_blocks + rb;
@@ -290,7 +302,9 @@ TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int ma
     return t;
   }
   t.splits = 0;
-  const int64_t units = (int64_t)kTrRounds * (d == 64 ? 3 : 2) * 256;
+  // As many units as are on the chip at a time (the LDS of two workgroups a CU, three
+  // at D = 64).
+  const int64_t units = (d == 64 ? 3 : 2) * 256;
   int64_t n = units / ((int64_t)hkv * t.row_blocks);
   n = std::min(n, num_seqs * std::max<int64_t>(1, blocks / kTrMinBlocks));
   n = std::min<int64_t>(n, (int64_t)num_seqs * kTreeMaxSplits);
