@@ -32,7 +32,8 @@
  *   - Calls are thread-safe; the only mutable global state is the
  *     thread-local error message (and the static scratch of
  *     rag_attn_decode_paged_noalloc, see there).
- *   - RAG_ATTN_PF_ITEMS=n (read at each rag_attn_prefill_varlen call) fixes
+ *   - RAG_ATTN_PF_ITEMS=n (read at each rag_attn_prefill_varlen and
+ *     rag_attn_prefill_varlen_ranges call) fixes
  *     how many query tiles one prefill workgroup runs in sequence instead of
  *     the library's load-balancing choice; a testing and tuning knob that
  *     changes no output bit.

@@ -86,7 +86,7 @@ TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int ma
 size_t tree_partial_rows(const TreeShape& t, int hkv);
 int64_t tree_grid(const TreeShape& t, const TreeArgs& a);
 hipError_t launch_tree(const TreeArgs& a, hipStream_t stream);
-int64_t ranges_grid(const RangesArgs& a);
+int64_t ranges_grid(const RangesArgs& a);       // workgroups, at most
 hipError_t launch_ranges(const RangesArgs& a, hipStream_t stream);
 
 }  // namespace rag

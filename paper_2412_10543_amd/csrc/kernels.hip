@@ -36,7 +36,6 @@ namespace rag {
 #endif
 constexpr int kPfWgPerCu = RAG_PF_WG_PER_CU;  // workgroups per CU aimed at (load balance)
 constexpr int kPfCus = 256;
-constexpr int kPfMaxItems = 32;
 constexpr int kBalMaxChunks = kBalMaxRows / kWave;   // balanced decode: chunks of 64 rows
 
 struct TileCoord {
@@ -72,17 +71,6 @@ __device__ __forceinline__ int snake_tile(int j, int k, int per) {
 struct PfSplit {
   int items, per, n_qt;
 };
-// RAG_ATTN_PF_ITEMS=n (read at each launch) fixes the query tiles per
-// workgroup at n instead of the load-balancing choice below: a testing and
-// tuning knob (every tile is computed the same way whichever workgroup runs
-// it, so outputs are bit-identical for any n).
-static int pf_items_override() {
-  const char* e = std::getenv("RAG_ATTN_PF_ITEMS");
-  if (e == nullptr || e[0] == 0) return 0;
-  const int n = std::atoi(e);
-  return n >= 1 ? std::min(n, kPfMaxItems) : 0;
-}
-
 static PfSplit pf_split(int num_seqs, int hkv, int group, int max_seqlen_q, bool multi) {
   const int rows = pf_rows_per_tile(group, kPfWavesDense);
   PfSplit p;

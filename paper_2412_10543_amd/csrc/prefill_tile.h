@@ -26,9 +26,26 @@
 //     end; blocks fully above the diagonal are skipped per wave.
 #pragma once
 
+#include <algorithm>
+#include <cstdlib>
+
 #include "common.h"
 
 namespace rag {
+
+// Query tiles of a workgroup, at most.
+constexpr int kPfMaxItems = 32;
+// RAG_ATTN_PF_ITEMS=n (read at each launch) fixes the query tiles per
+// workgroup at n instead of the launch's own choice: a testing and
+// tuning knob (every tile is computed the same way whichever workgroup runs
+// it, so outputs are bit-identical for any n).
+inline int pf_items_override() {
+  const char* e = std::getenv("RAG_ATTN_PF_ITEMS");
+  if (e == nullptr || e[0] == 0) return 0;
+  const int n = std::atoi(e);
+  return n >= 1 ? std::min(n, kPfMaxItems) : 0;
+}
+
 
 // K/V rows of one (sequence, kv head) stored densely: token j at k + j*stride.
 struct DenseKV {

@@ -196,24 +196,28 @@ static int ranges_tiles(const RangesArgs& a) {
 }
 
 static int ranges_items(const RangesArgs& a) {
+  if (const int forced = pf_items_override()) return forced;
   const int group = a.hq / a.hkv, ng = group / pf_heads_per_wg(group);
   const int64_t tiles = (int64_t)(ranges_tiles(a) - kRgLast) * a.num_seqs * a.hkv * ng;
   return tiles >= kRgMany ? kRgItems : 1;
 }
 
-int64_t ranges_grid(const RangesArgs& a) {
+static int64_t ranges_grid_of(const RangesArgs& a, int items) {
   const int group = a.hq / a.hkv;
   const int64_t streams = (int64_t)a.num_seqs * a.hkv;
-  return (streams + kNumXcd - 1) / kNumXcd * kNumXcd *
-         ranges_groups(ranges_tiles(a), ranges_items(a)) * (group / pf_heads_per_wg(group));
+  return (streams + kNumXcd - 1) / kNumXcd * kNumXcd * ranges_groups(ranges_tiles(a), items) *
+         (group / pf_heads_per_wg(group));
 }
 
+int64_t ranges_grid(const RangesArgs& a) { return ranges_grid_of(a, 1); }
+
 hipError_t launch_ranges(const RangesArgs& a, hipStream_t stream) {
-  const int64_t grid = ranges_grid(a);
+  const int items = ranges_items(a);
+  const int64_t grid = ranges_grid_of(a, items);
   if (grid == 0) return hipSuccess;
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a,
-                       ranges_tiles(a), ranges_items(a));
+                       ranges_tiles(a), items);
   };
   a.d == 64 ? go(ranges_kernel<64>) : go(ranges_kernel<128>);
   return hipGetLastError();

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import draft_support as ds
+import gpu_support as G
 from paper_2412_10543_amd import binding
 from paper_2412_10543_amd.workloads import normal_bf16
 
@@ -204,3 +205,66 @@ def test_another_stream():
     c, _ = run(q, k, v, lens, lens, i32(r), stream=s)
     torch.cuda.synchronize()
     assert torch.equal(a, b) and torch.equal(a, c)
+
+
+ITEMS = [
+    # (prompts as (system prompt, documents, query), hq, hkv, d)
+    ([(17, [100, 33, 300], 40), (3, [700], 9), (0, [40], 0)], 8, 2, 128),
+    ([(40, [400, 1, 64], 300)], 8, 4, 64),
+    ([(0, [900, 900], 33), (1, [], 0)], 2, 2, 128),
+    ([(200, [90] * 5, 7)], 16, 1, 64),
+]
+
+
+@pytest.mark.parametrize("case", range(len(ITEMS)))
+@pytest.mark.parametrize("kind", ["documents", "any", "nan"])
+def test_several_tiles_a_workgroup(case, kind):
+    """Tiles that one workgroup runs one after another are the bits of tiles of their
+    own: long and short ones, ones without a key, ones with values that must not
+    arrive."""
+    prompts, hq, hkv, d = ITEMS[case]
+    lens = [s + sum(x) + y for s, x, y in prompts]
+    r = sum((doc_ranges(*p) for p in prompts), [])
+    x = inputs(lens, lens, hq, hkv, d, 60 + case)
+    if kind == "any":
+        rng = random.Random(case)
+        at = 0
+        for n in lens:
+            for a in range(at, at + n, 50):              # the same for 50 rows, or none
+                e = rng.choice([(0, 1 << 30), (rng.randint(0, n), rng.randint(0, n)), (0, 0)])
+                r[a:min(a + 50, at + n)] = [e] * (min(a + 50, at + n) - a)
+            at += n
+    if kind == "nan":
+        for t, row in ((1, lens[0] // 3), (2, lens[0] // 2), (2, 1)):
+            x[t][row, :, 7] = math.nan
+    ranges = i32(r).reshape(-1, 2)
+    with G.env("RAG_ATTN_PF_ITEMS", 1):
+        o1, l1 = run(*x, lens, lens, ranges)
+    wo, _, bo, _ = ds.reference_ranges(*x, lens, lens, ranges, 1.0 / math.sqrt(d))
+    ds.within(o1, wo, bo)
+    for items in (2, 3, 5, 32):
+        print(f"items {items}", flush=True)
+        with G.env("RAG_ATTN_PF_ITEMS", items):
+            o, lse = run(*x, lens, lens, ranges)
+        torch.cuda.synchronize()
+        # (a NaN is one, of whatever bits)
+        assert torch.equal(torch.isnan(o), torch.isnan(o1))
+        assert torch.equal(o.nan_to_num(9.0).view(torch.int16), o1.nan_to_num(9.0).view(torch.int16))
+        assert torch.equal(torch.isnan(lse), torch.isnan(l1))
+        assert torch.equal(lse.nan_to_num(9.0), l1.nan_to_num(9.0))
+
+
+def test_a_launch_of_many_tiles():
+    """More tiles than workgroups are made for one by one."""
+    lens = [5000, 100]
+    q, k, v = inputs(lens, lens, 32, 32, 64, 70)
+    q = q.repeat(1, 4, 1)                                # 128 heads on 32: 4 to a workgroup
+    r = i32(doc_ranges(30, [60] * 82, 50) + doc_ranges(0, [40, 40], 20))
+    o, _ = run(q, k, v, lens, lens, r)
+    with G.env("RAG_ATTN_PF_ITEMS", 1):
+        o1, _ = run(q, k, v, lens, lens, r)
+    assert torch.equal(o, o1)
+    sub = [0, 3, 127]                                    # q heads, and the kv heads they read
+    w = ds.reference_ranges(q[:, sub].contiguous(), k[:, [0, 0, 31]].contiguous(),
+                            v[:, [0, 0, 31]].contiguous(), lens, lens, r, 1.0 / 8)
+    ds.within(o[:, sub], w[0], w[2])

@@ -150,6 +150,16 @@ def test_one_node_is_a_decode_row():
     ds.within(o, want, b)
 
 
+@pytest.mark.parametrize("rows", [64, 65, 130, 256, 257])
+def test_batches_of_many_sequences(rows):
+    """The cuts are made from 64 lengths at a time; with more than 256 none are."""
+    rng = random.Random(rows)
+    counts = [rng.choice([0, 1, 2, 5, 9]) for _ in range(rows)]
+    priors = [rng.choice([0, 3, rng.randint(0, 90), rng.randint(0, 400)]) for _ in range(rows)]
+    priors[rows // 2], priors[rows - 1], counts[rows - 1] = 5000, 1700, 4
+    Case(priors, trees(rng, counts), 2, 1, 64, rows).check((0, 2))
+
+
 def test_wide_table_and_long_context():
     rng = random.Random(3)
     Case([9000, 40, 2500], trees(rng, [25, 60, 3]), 8, 2, 128, 21, max_blocks=2300).check((0, 64))
