@@ -582,6 +582,9 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
 #pragma unroll
     for (int j = 1; j < 16; ++j) tmax = fmaxf(tmax, sE[j]);
     st.m_used = max_halves(tmax);
+    // (K(0) is read by all waves before the first slot requests K(4) into its place)
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    pf_barrier();
     const bool more = m + 1 < src.count;
     // Block i with scores s_cur; the next block's K, the last one's V.
     auto slot = [&](int i, f32x16& s_cur, f32x16& s_next, bf16x8 (&p_cur)[2],
