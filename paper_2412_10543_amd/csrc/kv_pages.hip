@@ -5,6 +5,8 @@
 //                 their sequence
 // Both move a few bytes per token; a call's time is its launch and its chain of
 // dependent reads.
+#include <algorithm>
+
 #include "common.h"
 #include "draft.h"
 
@@ -196,8 +198,13 @@ __global__ __launch_bounds__(kPgThreads) void pages_kernel(PagesArgs a) {
   }
 }
 
+// Workgroups for the slots, and for the pages given back (of which the host knows
+// only that the pool has no more), at most one a CU: a row of 36000 tokens that ends
+// leaves 2250.
 int64_t pages_grid(const PagesArgs& a) {
-  return a.max_new_tokens > 0 ? ((int64_t)a.max_new_tokens + kPgSlots - 1) / kPgSlots : 1;
+  const int64_t slots = ((int64_t)a.max_new_tokens + kPgSlots - 1) / kPgSlots;
+  const int64_t pages = ((int64_t)a.num_blocks + kPgSlots - 1) / kPgSlots;
+  return std::max<int64_t>({1, slots, std::min<int64_t>(pages, 256)});
 }
 
 hipError_t launch_pages(const PagesArgs& a, hipStream_t stream) {

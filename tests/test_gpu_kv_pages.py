@@ -102,6 +102,16 @@ def test_one_long_row_among_short_ones():
     check(table, stack, n, old, new, 70100, 4400)
 
 
+def test_long_rows_that_end():
+    """Many more pages come back than the slots' workgroups would put away."""
+    rng = random.Random(11)
+    old = [rng.randint(20000, 36000) for _ in range(30)] + [40, 7, 0]
+    new = [0] * 29 + [17, 41, 0, 50]
+    table, stack, n = layout(rng, old, 2300, 3)
+    want = check(table, stack, n, old, new, 60, 2300)
+    assert want["granted"] == 33 and want["free"] > 30000
+
+
 def test_many_steps_keep_every_page_once():
     rng = random.Random(9)
     rows, width, blocks = 33, 20, 300
