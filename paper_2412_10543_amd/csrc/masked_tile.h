@@ -28,7 +28,6 @@ struct MtInt {
 constexpr int kMtWaves = 4;
 constexpr int kMtKeys = 32;      // keys of a block
 constexpr int kMtRing = 4;       // blocks of K, and of V, in LDS
-constexpr int kMtAhead = 3;      // steps of a slot that LDS reads run ahead
 
 // The blocks of an item: na from key a0 on, then nb from key b0 on (both multiples
 // of 32).
@@ -600,8 +599,8 @@ __device__ __forceinline__ uint32_t masked_items_fast(Src& src, const KV& kv, in
         mt_mask(s_cur, partial ? rows.seen(sp.key0(i)) : 0u);
         run = max(min(fb.run(i + 1), n - i - 1), 0);
       }
-      float sum = pf_full_slot<D, 0, 0, Lay, kMtAhead>(st, lay, kst, vst, s_cur, s_next, p_cur,
-                                                       p_prev, c, -st.m_used * c, hook);
+      float sum = pf_full_slot<D, 0, 0>(st, lay, kst, vst, s_cur, s_next, p_cur, p_prev, c,
+                                        -st.m_used * c, hook);
       if (__builtin_expect(wave_any(!(sum <= kPfSumBound)), 0)) sum = pf_reref(st, s_cur, c, p_cur);
       st.l += sum;
     };

@@ -396,7 +396,7 @@ struct PfPipeCtx {
 struct PfNoHook {
   __device__ __forceinline__ void operator()(int) const {}
 };
-template <int D, int HK, int HV, class Lay, int kAhead = 2, class Hook = PfNoHook>
+template <int D, int HK, int HV, class Lay, class Hook = PfNoHook>
 __device__ __forceinline__ float pf_full_slot(PfState<D>& st, const Lay& lay,
                                               const bf16_t* __restrict__ kst,
                                               const bf16_t* __restrict__ vstage,
@@ -444,13 +444,13 @@ __device__ __forceinline__ float pf_full_slot(PfState<D>& st, const Lay& lay,
     }
     asm volatile("" : "+v"(sum));
   };
-#pragma unroll
-  for (int i = 0; i < kAhead && i < kSteps; ++i) load(i);
+  load(0);
+  if (kSteps > 1) load(1);
   arg(0);
   f32x16 acc = {};
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    if (i + kAhead < kSteps) load(i + kAhead);
+    if (i + 2 < kSteps) load(i + 2);
     hook(i);
     __builtin_amdgcn_sched_barrier(0);
     acc = mfma32(ka[i], st.qf[i], acc);
