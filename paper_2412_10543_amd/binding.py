@@ -448,9 +448,10 @@ def rag_attn_decode_paged_tree(q, k_cache, v_cache, o, tree_mask, block_tables, 
 
 def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, key_ranges,
                                    max_seqlen_q, max_seqlen_k, softmax_scale, stream=None) -> None:
-    """q, o [Tq, Hq, d]; k, v [Tk, Hkv, d] bf16; lse fp32 [Hq, Tq] or None;
-    cu_seqlens_* int32 [S+1]; key_ranges int32 [Tq, 2]: the (shared, start) of each
-    row, which sees the keys j < shared and start <= j <= its position."""
+    """q, o [Tq, Hq, d]; k, v [Tk, Hkv, d] bf16; lse fp32 [Hq, cu_seqlens_q[-1]] or
+    None (q and o may have rows behind those, lse not); cu_seqlens_* int32 [S+1];
+    key_ranges int32 [Tq, 2]: the (shared, start) of each row, which sees the keys
+    j < shared and start <= j <= its position."""
     t = (q, k, v, o, cu_seqlens_q, cu_seqlens_k, key_ranges, lse)
     p = _pointers(b"b3b3b3b3i1i1i2F2", *t)
     if p.__class__ is int:
@@ -458,7 +459,8 @@ def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, 
     dev, qp, rows, hq, d, kp, keys, hkv, dk, vp, keys2, hkv2, dv, op, rows2, hq2, d2, cu_q, seqs1, \
         cu_k, seqs2, ranges, rows3, two, lse_p = p[:25]
     if (rows2, hq2, d2) != (rows, hq, d) or (keys2, hkv2, dv) != (keys, hkv, d) or dk != d or \
-            seqs1 != seqs2 or (rows3, two) != (rows, 2) or p[25:] not in ((), (hq, rows)):
+            seqs1 != seqs2 or (rows3, two) != (rows, 2) or \
+            (lse_p and (p[25] != hq or p[26] > rows)):
         raise ValueError("prefill ranges: inconsistent shapes")
     if rows == 0:
         return

@@ -170,6 +170,15 @@ def test_rows_behind_the_last_sequence_stay():
     binding.rag_attn_prefill_varlen_ranges(q, k, v, o, None, cu(lens), cu(lens), r, 100, 100, 0.125)
     torch.cuda.synchronize()
     assert (o[133:] == 7.0).all() and not (o[:133] == 7.0).all() and (lse == 7.0).all()
+    # with a log-sum-exp, of the sequences' rows
+    packed = torch.full((8, 133), 7.0, device="cuda")
+    binding.rag_attn_prefill_varlen_ranges(q, k, v, o, packed, cu(lens), cu(lens), r, 100, 100, 0.125)
+    _, want, _, bound = ds.reference_ranges(q[:133], k, v, lens, lens, r[:133], 0.125)
+    ds.within(packed, want, bound)
+    assert (o[133:] == 7.0).all()
+    for bad in (lse[:7], torch.full((8, 174), 7.0, device="cuda")):
+        with pytest.raises(ValueError, match="inconsistent shapes"):
+            binding.rag_attn_prefill_varlen_ranges(q, k, v, o, bad, cu(lens), cu(lens), r, 100, 100, 0.125)
 
 
 def test_offsets_past_32_bits():
