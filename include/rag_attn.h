@@ -413,7 +413,8 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
  *            each 32 keys) that every sequence's keys are cut into.  Automatic: with
  *            at most 256 sequences the pieces are cut on the GPU from the
  *            sequences' lengths, about equally long and about as many as the GPU
- *            works on at a time; with more, none.
+ *            works on at a time (of sequences that are as many or more, the much
+ *            longer ones are cut); with more, none.
  *   workspace, workspace_bytes  device scratch of at least
  *            rag_attn_decode_tree_workspace_size(...) bytes for the same
  *            arguments (NULL when that is 0); 256-byte aligned, of any contents.

@@ -29,6 +29,13 @@ constexpr int kTrPlanSeqs = 256;     // sequences whose pieces are cut from thei
 // cut down to 4 blocks 22.4, to 16 23.5, to 32 34.8.
 constexpr int kTrMinBlocks = 8;
 
+// With sequences for a chipful of units, or more, those are cut that are longer than
+// twice an even share of a chipful, where the tables have at least this many blocks
+// (or the join's launch would cost more): 63 sequences of 500 keys and one of 30,000,
+// 8 nodes, 76 us (uncut 584); 64 of 4,096 keys 203 (198), 32 of 2,000 to 8,000 and 64
+// nodes 227 (223; cut from one even share on 235).
+constexpr int kTrLongBlocks = 64;
+
 // What the lane's row sees.
 struct TreeRows {
   const uint64_t* mask;         // its node's words, the first two of them loaded
@@ -105,7 +112,7 @@ __device__ __forceinline__ int tree_blocks(const TreeArgs& a, int n, int kv_len)
 }
 
 // Piece `pi` of the launch: sequence s (-1: there is no such piece), the p-th of
-// its n pieces; `first` its first.
+// its n pieces; `first` its first one's place among the partials (where n > 1).
 struct TreePiece {
   int s, p, n, first;
   int qb, nodes, kv_len;        // of sequence s
@@ -138,8 +145,8 @@ __device__ __forceinline__ int tree_scan(int x) {
 }
 
 // Otherwise (at most kTrPlanSeqs sequences) into pieces of at most a quota of blocks,
-// the smallest quota tried for which the pieces are at most a.pieces.  Wave-parallel,
-// one lane per sequence; every wave finds the same.
+// from an even share of them on the smallest tried for which the pieces are at most
+// a.pieces.  Wave-parallel, one lane per sequence; every wave finds the same.
 template <int kChunks>
 __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
   const int lane = threadIdx.x & 63;
@@ -162,7 +169,7 @@ __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) longest = max(longest, __shfl_xor(longest, m, kWave));
   // (single precision: every wave forms the same numbers, and any cut is a valid one)
-  float q = fmaxf((float)kTrMinBlocks, fmaxf(total / (float)a.pieces,
+  float q = fmaxf((float)kTrMinBlocks, fmaxf(total / (float)a.share,
                                              (float)longest / (float)kTreeMaxSplits));
   for (;;) {
     const float rq = 1.f / q;
@@ -178,6 +185,15 @@ __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
     if (count <= a.pieces || q > (float)longest) break;
     q = fmaxf(q * 1.0625f, q + 1.f);
   }
+  // Only sequences of several pieces have partials: a piece more than its share each,
+  // which is more than one, so at most 2 a.share of them.
+  int place[kChunks], places = 0;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int cut = np[c] > 1 ? np[c] : 0, incl = tree_scan(cut);
+    place[c] = places + incl - cut;
+    places += __builtin_amdgcn_readlane(incl, 63);
+  }
   TreePiece t{-1, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
@@ -185,9 +201,9 @@ __device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
     if (at != 0) {
       const int l = __builtin_ctzll(at);
       t.s = c * kWave + l;
-      t.first = __builtin_amdgcn_readlane(pf[c], l);
+      t.first = __builtin_amdgcn_readlane(place[c], l);
       t.n = __builtin_amdgcn_readlane(np[c], l);
-      t.p = pi - t.first;
+      t.p = pi - __builtin_amdgcn_readlane(pf[c], l);
       t.qb = __builtin_amdgcn_readlane(qb[c], l);
       t.nodes = __builtin_amdgcn_readlane(qe[c], l) - t.qb;
       t.kv_len = __builtin_amdgcn_readlane(kv[c], l);
@@ -222,7 +238,7 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
   const int nk = min(__builtin_amdgcn_readfirstlane(t.kv_len), a.max_blocks * 16);
   if (src.r0 >= src.n * group || nk <= 0) return;
   src.n_sp = n_sp;
-  src.unit = ((size_t)pi * a.hkv + kvh) * a.row_blocks + rb;
+  src.unit = ((size_t)(t.first + p) * a.hkv + kvh) * a.row_blocks + rb;
   src.group = group;
   src.h0 = kvh * group;
   src.kv_len = nk;
@@ -297,30 +313,38 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
 
 TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
                      int requested) {
-  TreeShape t;
+  TreeShape t{};
   const int64_t rows = (int64_t)max_nodes * (hq / hkv);
   t.row_blocks = (int)((rows + kTrRows - 1) / kTrRows);
   t.part_rows = (int)std::min<int64_t>(rows, kTrRows);
   const int64_t blocks = ((int64_t)max_blocks + 1) / 2;          // of the longest sequence
   if (requested > 0 || num_seqs > kTrPlanSeqs) {
     t.splits = (int)std::max<int64_t>(1, std::min<int64_t>({requested, kTreeMaxSplits, blocks}));
-    t.pieces = (int64_t)num_seqs * t.splits;
+    t.pieces = t.places = (int64_t)num_seqs * t.splits;
     return t;
   }
   t.splits = 0;
   // As many units as are on the chip at a time (the LDS of two workgroups a CU, three
   // at D = 64).
   const int64_t units = (d == 64 ? 3 : 2) * 256;
-  int64_t n = units / ((int64_t)hkv * t.row_blocks);
+  int64_t n = std::max<int64_t>(1, units / ((int64_t)hkv * t.row_blocks));
   n = std::min(n, num_seqs * std::max<int64_t>(1, blocks / kTrMinBlocks));
   n = std::min<int64_t>(n, (int64_t)num_seqs * kTreeMaxSplits);
-  t.pieces = std::max<int64_t>(n, num_seqs);
+  if (n > num_seqs) {
+    t.share = t.pieces = t.places = n;
+  } else if (blocks >= kTrLongBlocks) {
+    t.share = (n + 1) / 2;
+    t.pieces = num_seqs + t.share;
+    t.places = 2 * t.share;
+  } else {
+    t.pieces = num_seqs;
+  }
   if (t.pieces == num_seqs) t.splits = 1;                        // nothing to cut
   return t;
 }
 
 size_t tree_partial_rows(const TreeShape& t, int hkv) {
-  return t.splits == 1 ? 0 : (size_t)t.pieces * hkv * t.row_blocks * t.part_rows;
+  return t.splits == 1 ? 0 : (size_t)t.places * hkv * t.row_blocks * t.part_rows;
 }
 
 static int64_t tree_join_grid(const TreeArgs& a) {

@@ -160,6 +160,20 @@ def test_batches_of_many_sequences(rows):
     Case(priors, trees(rng, counts), 2, 1, 64, rows).check((0, 2))
 
 
+@pytest.mark.parametrize("rows,hkv", [(64, 8), (65, 8), (200, 4), (256, 8)])
+def test_a_few_long_sequences_among_many_short_ones(rows, hkv):
+    """Alone the short ones are units enough; the long ones are cut all the same, and
+    their partials have the workspace to themselves."""
+    rng = random.Random(rows + hkv)
+    counts = [rng.choice([0, 1, 2, 4]) for _ in range(rows)]
+    priors = [rng.choice([0, 5, rng.randint(0, 70)]) for _ in range(rows)]
+    for s, n in ((0, 3000), (rows // 3, 1100), (rows - 1, 2100)):
+        priors[s], counts[s] = n, 5
+    c = Case(priors, trees(rng, counts), hkv, hkv, 64, rows)
+    assert 0 < c.workspace().numel() < 1 << 25
+    c.check()
+
+
 def test_wide_table_and_long_context():
     rng = random.Random(3)
     Case([9000, 40, 2500], trees(rng, [25, 60, 3]), 8, 2, 128, 21, max_blocks=2300).check((0, 64))
