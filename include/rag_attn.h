@@ -412,9 +412,8 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
  *   num_splits  0 = automatic; else the number of pieces (at most 64, and one for
  *            each 32 keys) that every sequence's keys are cut into.  Automatic: with
  *            at most 256 sequences the pieces are cut on the GPU from the
- *            sequences' lengths, about equally long and about as many as the GPU
- *            works on at a time (of sequences that are as many or more, the much
- *            longer ones are cut); with more, none.
+ *            sequences' lengths, so that the workgroups that the GPU works on
+ *            at a time get even shares of all keys; with more, none.
  *   workspace, workspace_bytes  device scratch of at least
  *            rag_attn_decode_tree_workspace_size(...) bytes for the same
  *            arguments (NULL when that is 0); 256-byte aligned, of any contents.

@@ -46,11 +46,10 @@ struct TreeArgs {
   float scale;
   int row_blocks = 1;           // blocks of 128 (node, q head of a group) rows, at most
   int splits = 1;               // pieces of every sequence (0: cut from the lengths)
-  int pieces = 0;               // of all sequences, at most
-  int share = 1;                // splits 0: sequences are cut into pieces of all keys / share
+  int units = 0;                // for one kv head and row block
   int part_rows = 0;            // rows of a row block in the partials
   // a launch that may cut: partial outputs [place][kv head][row block][part_rows][d], their
-  // log-sum-exps, and each sequence's first place and its number of pieces (else null)
+  // log-sum-exps, and what places a sequence's pieces have and their number (else null)
   float* part_o = nullptr;
   float* part_lse = nullptr;
   int32_t* part_of = nullptr;
@@ -59,7 +58,7 @@ struct TreeArgs {
 // How a tree launch is cut (requested splits 0: chosen).
 struct TreeShape {
   int row_blocks, splits, part_rows;
-  int64_t pieces, share, places;          // (places: of the pieces of cut sequences)
+  int64_t units, places;
 };
 
 struct RangesArgs {

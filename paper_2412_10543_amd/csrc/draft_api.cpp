@@ -269,8 +269,7 @@ rag_status rag_attn_decode_paged_tree(const void* q, const void* k_cache, const 
     return fail(RAG_ERR_UNSUPPORTED, "%s: batch too large for one grid", who);
   a.row_blocks = t.row_blocks;
   a.splits = t.splits;
-  a.pieces = (int)t.pieces;
-  a.share = (int)t.share;
+  a.units = (int)t.units;
   a.part_rows = t.part_rows;
   const TreeWs ws = tree_workspace(t, num_seqs, num_kv_heads, head_dim);
   if (ws.bytes > 0) {

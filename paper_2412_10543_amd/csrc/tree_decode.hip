@@ -4,14 +4,15 @@
 //
 // A unit is (piece of a sequence's keys, kv head, 128 rows): its rows are (node, q
 // head of the group) pairs, node by node, so that every K/V byte is read once for
-// 128 of them.  The pieces are cut on the GPU from the sequences' lengths, about
-// as many units as the chip takes at a time and about equally long (tree_plan);
-// where a sequence has several, they write normalised partial outputs and their
-// log-sum-exp, which a second kernel joins.
+// 128 of them.  The pieces are cut on the GPU from the sequences' lengths: as many
+// workgroups as the chip takes at a time get even shares of all blocks, which may
+// end in one sequence and begin in another (tree_share); where a sequence has
+// several pieces, they write normalised partial outputs and their log-sum-exp, which
+// a second kernel joins.
 //
 // Measured (32 q / 8 kv heads of 128): 48 sequences of 700 to 10,304 keys and 5 to
-// 12 nodes 156 us, K/V at 4.4 TB/s (HBM); 16 of 2,600 to 10,300 keys and 64 nodes 125
-// us, 650 TFLOP/s (the tile loop, and pieces that are not all equal); one of 4,782
+// 12 nodes 151 us, K/V at 4.5 TB/s (HBM); 16 of 2,600 to 10,300 keys and 64 nodes 125
+// us, 650 TFLOP/s (the tile loop); one of 4,782
 // and 25 nodes 19.8 us: 16.0 for pieces of 8 or 9 blocks, of which the chain of
 // lengths, page ids, first copies and queries takes 4, and 4.4 for the join.
 #include "common.h"
@@ -24,17 +25,21 @@ namespace {
 
 constexpr int kTrRows = 32 * kMtWaves;
 constexpr int kTrPlanSeqs = 256;     // sequences whose pieces are cut from their lengths
-// Blocks that a piece is cut for, at least: a unit's start, end and join cost about
+// Blocks of a share, at least: a unit's start, end and join cost about
 // as much as eight.  One sequence of 8192 keys, 32 q / 8 kv heads, 32 nodes: 19.9 us;
 // cut down to 4 blocks 22.4, to 16 23.5, to 32 34.8.
 constexpr int kTrMinBlocks = 8;
 
-// With sequences for a chipful of units, or more, those are cut that are longer than
-// twice an even share of a chipful, where the tables have at least this many blocks
-// (or the join's launch would cost more): 63 sequences of 500 keys and one of 30,000,
-// 8 nodes, 76 us (uncut 584); 64 of 4,096 keys 203 (198), 32 of 2,000 to 8,000 and 64
-// nodes 227 (223; cut from one even share on 235).
+// With sequences for a chipful of units, or more, nothing is cut where the tables have
+// fewer blocks than this (the join's launch would cost more).
 constexpr int kTrLongBlocks = 64;
+
+// Blocks that the start of a sequence in a unit counts for.  40 sequences of 600 keys
+// and one of 20,000, 12 nodes: 45 us; with 3 or 6 blocks 51, as more short sequences are
+// cut; 63 of 500 and one of 30,000, 8 nodes: 56, with 3 blocks 63, with 14 59.
+// (Against a quota of blocks a piece and sequences apart: 48 of 700 to 10,304 keys
+// 161 -> 151 us, 96 of them 530 -> 470, 63 and one 75 -> 56, but 200 of 2,048 326 -> 342.)
+constexpr int kTrStart = 10;
 
 // What the lane's row sees.
 struct TreeRows {
@@ -111,25 +116,35 @@ __device__ __forceinline__ int tree_blocks(const TreeArgs& a, int n, int kv_len)
   return n <= 0 ? 0 : (min(kv_len, a.max_blocks * 16) + kMtKeys - 1) / kMtKeys;
 }
 
-// Piece `pi` of the launch: sequence s (-1: there is no such piece), the p-th of
-// its n pieces; `first` its first one's place among the partials (where n > 1).
+// Blocks [b0, b1) of sequence s (-1: no more), the p-th of its n pieces, and their
+// place among the partials where n > 1; `first` for the join (tree_place).
 struct TreePiece {
-  int s, p, n, first;
+  int s, p, n, b0, b1, first;
   int qb, nodes, kv_len;        // of sequence s
+  int next;                     // where in the unit the next piece starts
 };
 
+// The place of a sequence's piece p.
+__device__ __forceinline__ int tree_place(const TreeArgs& a, int first, int p) {
+  return a.splits > 0 ? first + p : 2 * (first + p) + (p == 0);
+}
+
 // With a number of splits given every sequence is cut into that many (or its
-// blocks), and piece s * splits + p is sequence s's p-th.
-__device__ __forceinline__ TreePiece tree_piece_even(const TreeArgs& a, int pi) {
+// blocks), and unit s * splits + p is sequence s's p-th piece.
+__device__ __forceinline__ TreePiece tree_even(const TreeArgs& a, int unit, int at) {
   TreePiece t;
-  t.s = pi / a.splits;
-  t.p = pi % a.splits;
-  t.first = pi - t.p;
+  t.s = unit / a.splits;
+  t.p = unit % a.splits;
+  t.first = unit - t.p;
   t.qb = uniform_load(a.cu_q, t.s);
   t.nodes = uniform_load(a.cu_q, t.s + 1) - t.qb;
   t.kv_len = uniform_load(a.kv_lens, t.s);
-  t.n = min(a.splits, max(tree_blocks(a, t.nodes, t.kv_len), 1));
-  if (t.p >= t.n) t.s = -1;
+  const int64_t blocks = tree_blocks(a, t.nodes, t.kv_len);
+  t.n = min(a.splits, max((int)blocks, 1));
+  t.b0 = (int)(blocks * t.p / t.n);
+  t.b1 = (int)(blocks * (t.p + 1) / t.n);
+  t.next = 1;
+  if (t.p >= t.n || at > 0) t.s = -1;
   return t;
 }
 
@@ -144,66 +159,54 @@ __device__ __forceinline__ int tree_scan(int x) {
   return x;
 }
 
-// Otherwise (at most kTrPlanSeqs sequences) into pieces of at most a quota of blocks,
-// from an even share of them on the smallest tried for which the pieces are at most
-// a.pieces.  Wave-parallel, one lane per sequence; every wave finds the same.
+// Otherwise (at most kTrPlanSeqs sequences) all sequences' blocks, kTrStart more in
+// front of each for what its start costs, stand in one row that is cut into even
+// shares, one a unit: a unit has the end of a sequence, whole ones and the
+// beginning of one, of which the first and the last may have partials (places 2 unit
+// and 2 unit + 1).  The piece at `at` of the unit's share; wave-parallel, one lane per
+// sequence, and every wave finds the same.
 template <int kChunks>
-__device__ __forceinline__ TreePiece tree_plan(const TreeArgs& a, int pi) {
-  const int lane = threadIdx.x & 63;
-  int bl[kChunks], np[kChunks], pf[kChunks], qb[kChunks], qe[kChunks], kv[kChunks], longest = 0;
-  float total = 0.f;
+__device__ __forceinline__ TreePiece tree_share(const TreeArgs& a, int unit, int at) {
+  const int lane = opaque_lane();
+  int end[kChunks], len[kChunks], qb[kChunks], qe[kChunks], kv[kChunks], longest = 0, total = 0;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
-    const int s = c * kWave + lane;
-    const int x = min(s, a.num_seqs - 1);
+    const int s = c * kWave + lane, x = min(s, a.num_seqs - 1);
     qb[c] = a.cu_q[x];
     qe[c] = a.cu_q[x + 1];
     kv[c] = a.kv_lens[x];
-    bl[c] = tree_blocks(a, qe[c] - qb[c], kv[c]);
-    if (s >= a.num_seqs) bl[c] = 0;
-    longest = max(longest, bl[c]);
+    const int bl = s < a.num_seqs ? tree_blocks(a, qe[c] - qb[c], kv[c]) : 0;
+    len[c] = bl > 0 ? bl + kTrStart : 0;
+    longest = max(longest, len[c]);
   }
 #pragma unroll
-  for (int c = 0; c < kChunks; ++c)
-    total += (float)(uint32_t)__builtin_amdgcn_readlane(tree_scan(bl[c]), 63);
+  for (int c = 0; c < kChunks; ++c) {
+    end[c] = total + tree_scan(len[c]);
+    total = __builtin_amdgcn_readlane(end[c], 63);
+  }
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) longest = max(longest, __shfl_xor(longest, m, kWave));
-  // (single precision: every wave forms the same numbers, and any cut is a valid one)
-  float q = fmaxf((float)kTrMinBlocks, fmaxf(total / (float)a.share,
-                                             (float)longest / (float)kTreeMaxSplits));
-  for (;;) {
-    const float rq = 1.f / q;
-    int count = 0;
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-      np[c] = bl[c] > 0 ? min(max((int)ceilf((float)bl[c] * rq - 1e-3f), 1), kTreeMaxSplits) : 0;
-      const int incl = tree_scan(np[c]);
-      pf[c] = count + incl - np[c];
-      count += __builtin_amdgcn_readlane(incl, 63);
-    }
-    // (from the longest on every sequence is one piece: at most num_seqs <= pieces)
-    if (count <= a.pieces || q > (float)longest) break;
-    q = fmaxf(q * 1.0625f, q + 1.f);
-  }
-  // Only sequences of several pieces have partials: a piece more than its share each,
-  // which is more than one, so at most 2 a.share of them.
-  int place[kChunks], places = 0;
+  // (of kTreeMaxSplits units at most that a sequence touches)
+  const int share = max(max((total + a.units - 1) / a.units, kTrMinBlocks),
+                        (longest + kTreeMaxSplits - 3) / (kTreeMaxSplits - 2));
+  const int from = unit * share, to = min(from + share, total);
+  TreePiece t{-1, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+  const int g = from + at;
+  if (from >= total || g >= to) return t;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
-    const int cut = np[c] > 1 ? np[c] : 0, incl = tree_scan(cut);
-    place[c] = places + incl - cut;
-    places += __builtin_amdgcn_readlane(incl, 63);
-  }
-  TreePiece t{-1, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-  for (int c = 0; c < kChunks; ++c) {
-    const uint64_t at = __builtin_amdgcn_ballot_w64(pi >= pf[c] && pi < pf[c] + np[c]);
-    if (at != 0) {
-      const int l = __builtin_ctzll(at);
+    const uint64_t here = __builtin_amdgcn_ballot_w64(g >= end[c] - len[c] && g < end[c]);
+    if (here != 0) {
+      const int l = __builtin_ctzll(here);
+      const int e = __builtin_amdgcn_readlane(end[c], l);
+      const int b = e - __builtin_amdgcn_readlane(len[c], l) + kTrStart;   // of its blocks
       t.s = c * kWave + l;
-      t.first = __builtin_amdgcn_readlane(place[c], l);
-      t.n = __builtin_amdgcn_readlane(np[c], l);
-      t.p = pi - __builtin_amdgcn_readlane(pf[c], l);
+      t.first = b / share;
+      t.n = (e - 1) / share - t.first + 1;
+      t.p = unit - t.first;
+      t.b0 = max(g - b, 0);
+      t.b1 = max(min(e, to) - b, 0);
+      t.next = min(e, to) - from;
       t.qb = __builtin_amdgcn_readlane(qb[c], l);
       t.nodes = __builtin_amdgcn_readlane(qe[c], l) - t.qb;
       t.kv_len = __builtin_amdgcn_readlane(kv[c], l);
@@ -222,33 +225,39 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
   xcd_slot(blockIdx.x, xcd, local);
   const int rb = local % a.row_blocks;
   const int stream = xcd + kNumXcd * (local / a.row_blocks);
-  const int kvh = stream % a.hkv, pi = stream / a.hkv;
-  if (pi >= a.pieces) return;
-  TreePiece t;
-  if constexpr (kChunks == 0) t = tree_piece_even(a, pi); else t = tree_plan<kChunks>(a, pi);
-  const int s = __builtin_amdgcn_readfirstlane(t.s);
-  if (s < 0) return;
-  const int p = __builtin_amdgcn_readfirstlane(t.p), n_sp = __builtin_amdgcn_readfirstlane(t.n);
-  if (p == 0 && rb == 0 && kvh == 0 && threadIdx.x == 0 && a.part_of != nullptr)
-    reinterpret_cast<int2*>(a.part_of)[s] = int2{t.first, t.n};   // for the join
-  TreeSrc<D> src{a};
-  src.qb = __builtin_amdgcn_readfirstlane(t.qb);
-  src.n = __builtin_amdgcn_readfirstlane(t.nodes);
-  src.r0 = rb * kTrRows;
-  const int nk = min(__builtin_amdgcn_readfirstlane(t.kv_len), a.max_blocks * 16);
-  if (src.r0 >= src.n * group || nk <= 0) return;
-  src.n_sp = n_sp;
-  src.unit = ((size_t)(t.first + p) * a.hkv + kvh) * a.row_blocks + rb;
-  src.group = group;
-  src.h0 = kvh * group;
-  src.kv_len = nk;
-  const int64_t blocks = (nk + kMtKeys - 1) / kMtKeys;
-  const int b0 = (int)(blocks * p / n_sp), b1 = (int)(blocks * (p + 1) / n_sp);
-  src.spans = KeySpans{b0 * kMtKeys, b1 - b0, 0, 0};
-  const PagedDmaKV<D> kv{(const bf16_t*)a.k_cache + (size_t)kvh * 16 * D,
-                         (const bf16_t*)a.v_cache + (size_t)kvh * 16 * D,
-                         a.tables + (size_t)s * a.max_blocks, (size_t)a.hkv * 16 * D};
-  masked_items<D>(src, kv, nk, a.scale, lds);
+  const int kvh = stream % a.hkv, unit = stream / a.hkv;
+  if (unit >= a.units) return;
+#pragma unroll 1
+  for (int at = 0;;) {
+    TreePiece t;
+    if constexpr (kChunks == 0) t = tree_even(a, unit, at); else t = tree_share<kChunks>(a, unit, at);
+    const int s = __builtin_amdgcn_readfirstlane(t.s);
+    if (s < 0) return;
+    at = __builtin_amdgcn_readfirstlane(t.next);
+    const int p = __builtin_amdgcn_readfirstlane(t.p), n_sp = __builtin_amdgcn_readfirstlane(t.n);
+    const int b0 = __builtin_amdgcn_readfirstlane(t.b0), b1 = __builtin_amdgcn_readfirstlane(t.b1);
+    if (b0 >= b1) continue;                      // (its start only, or no key)
+    if (p == 0 && rb == 0 && kvh == 0 && threadIdx.x == 0 && a.part_of != nullptr)
+      reinterpret_cast<int2*>(a.part_of)[s] = int2{t.first, t.n};   // for the join
+    TreeSrc<D> src{a};
+    src.qb = __builtin_amdgcn_readfirstlane(t.qb);
+    src.n = __builtin_amdgcn_readfirstlane(t.nodes);
+    src.r0 = rb * kTrRows;
+    const int nk = min(__builtin_amdgcn_readfirstlane(t.kv_len), a.max_blocks * 16);
+    if (src.r0 >= src.n * group) continue;
+    src.n_sp = n_sp;
+    src.unit = ((size_t)__builtin_amdgcn_readfirstlane(tree_place(a, t.first, p)) * a.hkv + kvh) *
+                   a.row_blocks + rb;
+    src.group = group;
+    src.h0 = kvh * group;
+    src.kv_len = nk;
+    src.spans = KeySpans{b0 * kMtKeys, b1 - b0, 0, 0};
+    const PagedDmaKV<D> kv{(const bf16_t*)a.k_cache + (size_t)kvh * 16 * D,
+                           (const bf16_t*)a.v_cache + (size_t)kvh * 16 * D,
+                           a.tables + (size_t)s * a.max_blocks, (size_t)a.hkv * 16 * D};
+    masked_items<D>(src, kv, nk, a.scale, lds);
+    __syncthreads();                             // (the next piece takes the same LDS)
+  }
 }
 
 // o = sum_i 2^(lse_i - m) o_i / sum_i 2^(lse_i - m): one wave per (node, q head).
@@ -266,19 +275,19 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   if (n_sp <= 1) return;
   const int group = a.hq / a.hkv, node = i / a.hq, head = i % a.hq, kvh = head / group;
   const int r = node * group + head % group;     // row of the unit's row blocks
-  const size_t stride = (size_t)a.hkv * a.row_blocks * a.part_rows;     // rows between pieces
-  const size_t row = (((size_t)first * a.hkv + kvh) * a.row_blocks + r / kTrRows) * a.part_rows +
-                     r % kTrRows;
+  const size_t stride = (size_t)a.hkv * a.row_blocks * a.part_rows;     // rows between places
+  const size_t row0 = ((size_t)kvh * a.row_blocks + r / kTrRows) * a.part_rows + r % kTrRows;
+  auto row = [&](int p) { return row0 + tree_place(a, first, p) * stride; };
   // kBatch pieces requested at a time, the first beside the log-sum-exps.
   constexpr int kBatch = 8;
-  const float lse = lane < n_sp ? a.part_lse[row + lane * stride] : -INFINITY;
-  const float* po = a.part_o + row * D + lane * kPer;
+  const float lse = lane < n_sp ? a.part_lse[row(lane)] : -INFINITY;
+  const float* po = a.part_o + lane * kPer;
   float x[kBatch][kPer];
   auto request = [&](int k0) {
 #pragma unroll
     for (int b = 0; b < kBatch; ++b)
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) x[b][e] = po[min(k0 + b, n_sp - 1) * stride * D + e];
+      for (int e = 0; e < kPer; ++e) x[b][e] = po[row(min(k0 + b, n_sp - 1)) * D + e];
   };
   request(0);
   float mx = lse;
@@ -318,9 +327,10 @@ TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int ma
   t.row_blocks = (int)((rows + kTrRows - 1) / kTrRows);
   t.part_rows = (int)std::min<int64_t>(rows, kTrRows);
   const int64_t blocks = ((int64_t)max_blocks + 1) / 2;          // of the longest sequence
-  if (requested > 0 || num_seqs > kTrPlanSeqs) {
+  // (the plan's sums are 32-bit)
+  if (requested > 0 || num_seqs > kTrPlanSeqs || num_seqs * (blocks + kTrStart) >= 1 << 30) {
     t.splits = (int)std::max<int64_t>(1, std::min<int64_t>({requested, kTreeMaxSplits, blocks}));
-    t.pieces = t.places = (int64_t)num_seqs * t.splits;
+    t.units = t.places = (int64_t)num_seqs * t.splits;
     return t;
   }
   t.splits = 0;
@@ -329,17 +339,12 @@ TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int ma
   const int64_t units = (d == 64 ? 3 : 2) * 256;
   int64_t n = std::max<int64_t>(1, units / ((int64_t)hkv * t.row_blocks));
   n = std::min(n, num_seqs * std::max<int64_t>(1, blocks / kTrMinBlocks));
-  n = std::min<int64_t>(n, (int64_t)num_seqs * kTreeMaxSplits);
-  if (n > num_seqs) {
-    t.share = t.pieces = t.places = n;
-  } else if (blocks >= kTrLongBlocks) {
-    t.share = (n + 1) / 2;
-    t.pieces = num_seqs + t.share;
-    t.places = 2 * t.share;
-  } else {
-    t.pieces = num_seqs;
+  if (n <= num_seqs && blocks < kTrLongBlocks) {                 // nothing to cut
+    t.splits = 1;
+    n = num_seqs;
   }
-  if (t.pieces == num_seqs) t.splits = 1;                        // nothing to cut
+  t.units = n;
+  t.places = 2 * n;
   return t;
 }
 
@@ -350,18 +355,18 @@ size_t tree_partial_rows(const TreeShape& t, int hkv) {
 static int64_t tree_join_grid(const TreeArgs& a) {
   return (int64_t)a.num_seqs * (((int64_t)a.max_nodes * a.hq + 3) / 4);
 }
-static int64_t tree_units_grid(int64_t pieces, int hkv, int row_blocks) {
-  return (pieces * hkv + kNumXcd - 1) / kNumXcd * kNumXcd * row_blocks;
+static int64_t tree_units_grid(int64_t units, int hkv, int row_blocks) {
+  return (units * hkv + kNumXcd - 1) / kNumXcd * kNumXcd * row_blocks;
 }
 
 int64_t tree_grid(const TreeShape& t, const TreeArgs& a) {
-  return std::max(tree_units_grid(t.pieces, a.hkv, t.row_blocks),
+  return std::max(tree_units_grid(t.units, a.hkv, t.row_blocks),
                   t.splits == 1 ? 0 : tree_join_grid(a));        // (the larger of the launches)
 }
 
 template <int D>
 static hipError_t launch_tree_d(const TreeArgs& a, hipStream_t stream) {
-  const int64_t grid = tree_units_grid(a.pieces, a.hkv, a.row_blocks);
+  const int64_t grid = tree_units_grid(a.units, a.hkv, a.row_blocks);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kMtWaves), 0, stream, a);
   };
