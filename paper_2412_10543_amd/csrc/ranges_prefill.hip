@@ -155,25 +155,33 @@ __host__ __device__ constexpr int ranges_groups(int n_qt, int items) {
   return n_qt <= kRgLast ? n_qt : kRgLast + (n_qt - kRgLast + items - 1) / items;
 }
 
+// Where the kv heads divide among the XCDs, each has all sequences' tiles of its own
+// heads and their K/V in its L2.  Elsewhere that would give the XCDs other sequences,
+// and other amounts of work, and tiles go round them one by one (32 q / 2 kv heads: 4
+// prompts with prefixes 87 us for 165, 4 with windows 47 for 54; 14 q / 2 kv heads of
+// 64: 4 prompts of documents 152 for 148).
+__host__ __device__ constexpr int ranges_parts(int hkv) { return hkv % kNumXcd == 0 ? kNumXcd : 1; }
+
 template <int D>
 __global__ __launch_bounds__(64 * kMtWaves, 2) void ranges_kernel(RangesArgs a, int n_qt, int items) {
   __shared__ __attribute__((aligned(16))) MtLds<D> lds;
   const int group = a.hq / a.hkv, hw = pf_heads_per_wg(group), ng = group / hw;
-  int xcd, local;
-  xcd_slot(blockIdx.x, xcd, local);
-  const int streams = (a.num_seqs * a.hkv + kNumXcd - 1) / kNumXcd;   // per XCD
+  const int parts = ranges_parts(a.hkv);
+  const int xcd = blockIdx.x % parts;
+  int local = blockIdx.x / parts;
+  const int streams = (a.num_seqs * a.hkv + parts - 1) / parts;       // per XCD
   const int hg = local % ng;
   local /= ng;
   const int first = min(n_qt, kRgLast) * streams;
   int j, stream, count = 1;
   if (local < first) {
     j = local / streams;
-    stream = xcd + kNumXcd * (local % streams);
+    stream = xcd + parts * (local % streams);
   } else {
     const int per = ranges_groups(n_qt, items) - kRgLast;
     j = kRgLast + (local - first) % per * items;
     count = items;
-    stream = xcd + kNumXcd * ((local - first) / per);
+    stream = xcd + parts * ((local - first) / per);
   }
   if (stream >= a.num_seqs * a.hkv) return;
   const int s = stream / a.hkv, kvh = stream % a.hkv;
@@ -218,7 +226,8 @@ static int ranges_items(const RangesArgs& a) {
 static int64_t ranges_grid_of(const RangesArgs& a, int items) {
   const int group = a.hq / a.hkv;
   const int64_t streams = (int64_t)a.num_seqs * a.hkv;
-  return (streams + kNumXcd - 1) / kNumXcd * kNumXcd * ranges_groups(ranges_tiles(a), items) *
+  const int parts = ranges_parts(a.hkv);
+  return (streams + parts - 1) / parts * parts * ranges_groups(ranges_tiles(a), items) *
          (group / pf_heads_per_wg(group));
 }
 
