@@ -129,6 +129,24 @@ def test_unseen_values_never_arrive(value, side, prior, hq):
             assert torch.isnan(got[seeing.cuda()].float()).any(-1).all()
 
 
+def test_unseen_values_where_a_workgroup_has_several_sequences():
+    """Wide tables, short and long sequences: shares end in one and begin in another,
+    some of them with values that must not arrive."""
+    rng = random.Random(12)
+    counts = [9, 1, 30, 0, 17, 64, 3, 5]
+    c = Case([50, 20, 0, 70, 7, 700, 33, 400], trees(rng, counts), 8, 8, 128, 12, max_blocks=256)
+    for s, node in ((0, 4), (2, 11), (4, 2), (5, 40), (7, 1)):
+        at = c.kv[s] - counts[s] + node
+        for cache, value in ((c.pool.v_cache, math.nan), (c.pool.k_cache, math.inf)):
+            cache[c.pool.block_tables[s, at // 16].long(), :, at % 16, 9] = value
+    o, b = c.want()
+    assert 0 < torch.isnan(b).double().mean() < 0.8
+    for s in (0, 2):
+        got = c.run(s)
+        torch.cuda.synchronize()
+        ds.within(got, o, b, f"splits {s}")
+
+
 @pytest.mark.parametrize("q_scale", [0.0, 8.0, 40.0])
 def test_flat_and_peaky_scores(q_scale):
     rng = random.Random(1)
