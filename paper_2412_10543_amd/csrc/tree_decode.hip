@@ -11,8 +11,8 @@
 // a second kernel joins.
 //
 // Measured (32 q / 8 kv heads of 128): 48 sequences of 700 to 10,304 keys and 5 to
-// 12 nodes 151 us, K/V at 4.5 TB/s (HBM); 16 of 2,600 to 10,300 keys and 64 nodes 125
-// us, 650 TFLOP/s (the tile loop); one of 4,782
+// 12 nodes 150 us, K/V at 4.6 TB/s (HBM); 16 of 2,600 to 10,300 keys and 64 nodes 119
+// us, 685 TFLOP/s (the tile loop, 106, and the join, 13); one of 4,782
 // and 25 nodes 19.8 us: 16.0 for pieces of 8 or 9 blocks, of which the chain of
 // lengths, page ids, first copies and queries takes 4, and 4.4 for the join.
 #include "common.h"
@@ -260,64 +260,90 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
   }
 }
 
-// o = sum_i 2^(lse_i - m) o_i / sum_i 2^(lse_i - m): one wave per (node, q head).
-template <int D>
+// o = sum_i 2^(lse_i - m) o_i / sum_i 2^(lse_i - m): one wave per kRows (node, q head)
+// pairs.  Small launches are one chain of reads long, with a wave a pair; where the
+// waves would come in several rounds, four pairs share the chain (tree_join_rows):
+// 16 trees of 64 nodes, 32 heads, in about 3 pieces 13.4 us, with a wave a pair 17.6.
+template <int D, int kRows>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   constexpr int kPer = D / 64;
   const int wave = wave_id(), lane = threadIdx.x & 63;
-  const int per = (a.max_nodes * a.hq + 3) / 4;  // workgroups of a sequence
+  const int per = (a.max_nodes * a.hq + 4 * kRows - 1) / (4 * kRows);   // workgroups of a sequence
   const int s = blockIdx.x / per;
   const int qb = uniform_load(a.cu_q, s), n = uniform_load(a.cu_q, s + 1) - qb;
-  const int i = blockIdx.x % per * 4 + wave;     // (node, head) of the sequence
-  if (i >= n * a.hq) return;
+  const int i0 = (blockIdx.x % per * 4 + wave) * kRows;   // the first (node, head) of the sequence
+  if (i0 >= n * a.hq) return;
   if (uniform_load(a.kv_lens, s) <= 0) return;
   const int first = uniform_load(a.part_of, 2 * s), n_sp = uniform_load(a.part_of, 2 * s + 1);
   if (n_sp <= 1) return;
-  const int group = a.hq / a.hkv, node = i / a.hq, head = i % a.hq, kvh = head / group;
-  const int r = node * group + head % group;     // row of the unit's row blocks
+  const int group = a.hq / a.hkv;
   const size_t stride = (size_t)a.hkv * a.row_blocks * a.part_rows;     // rows between places
-  const size_t row0 = ((size_t)kvh * a.row_blocks + r / kTrRows) * a.part_rows + r % kTrRows;
-  auto row = [&](int p) { return row0 + tree_place(a, first, p) * stride; };
+  size_t row[kRows];                             // in a place
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) {
+    const int i = min(i0 + j, n * a.hq - 1), node = i / a.hq, head = i % a.hq, kvh = head / group;
+    const int r = node * group + head % group;   // row of the unit's row blocks
+    row[j] = ((size_t)kvh * a.row_blocks + r / kTrRows) * a.part_rows + r % kTrRows;
+  }
   // kBatch pieces requested at a time, the first beside the log-sum-exps.
-  constexpr int kBatch = 8;
-  const float lse = lane < n_sp ? a.part_lse[row(lane)] : -INFINITY;
-  const float* po = a.part_o + lane * kPer;
-  float x[kBatch][kPer];
+  constexpr int kBatch = kRows == 1 ? 8 : 4;
+  float lse[kRows], x[kRows][kBatch][kPer];
+#pragma unroll
+  for (int j = 0; j < kRows; ++j)
+    lse[j] = lane < n_sp ? a.part_lse[row[j] + tree_place(a, first, lane) * stride] : -INFINITY;
   auto request = [&](int k0) {
 #pragma unroll
     for (int b = 0; b < kBatch; ++b)
+      if (k0 + b < n_sp) {
+        const float* po = a.part_o + tree_place(a, first, k0 + b) * stride * D + lane * kPer;
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) x[b][e] = po[row(min(k0 + b, n_sp - 1)) * D + e];
+        for (int j = 0; j < kRows; ++j)
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) x[j][b][e] = po[row[j] * D + e];
+      }
   };
   request(0);
-  float mx = lse;
+  float w[kRows], inv[kRows], acc[kRows][kPer] = {};
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) mx = fmaxf(mx, wave_xor(mx, m));
-  // (a NaN among them stays one: fmaxf drops it, the difference below does not)
-  const float w = lse == -INFINITY ? 0.f : fast_exp2((lse - mx) * kLog2e);
-  float den = w;
+  for (int j = 0; j < kRows; ++j) {
+    float mx = lse[j];
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) den += wave_xor(den, m);
-  const float inv = den == 0.f ? 0.f : 1.f / den;
-  float acc[kPer] = {};
+    for (int m = 32; m >= 1; m >>= 1) mx = fmaxf(mx, wave_xor(mx, m));
+    // (a NaN among them stays one: fmaxf drops it, the difference below does not)
+    w[j] = lse[j] == -INFINITY ? 0.f : fast_exp2((lse[j] - mx) * kLog2e);
+    float den = w[j];
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) den += wave_xor(den, m);
+    inv[j] = den == 0.f ? 0.f : 1.f / den;
+  }
   for (int k0 = 0; k0 < n_sp; k0 += kBatch) {
     if (k0 > 0) request(k0);
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const float wk = __uint_as_float(
-          __builtin_amdgcn_readlane(__float_as_uint(w), min(k0 + b, n_sp - 1)));
+    for (int b = 0; b < kBatch; ++b)
       if (k0 + b < n_sp) {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] += wk * x[b][e];
+        for (int j = 0; j < kRows; ++j) {
+          const float wk = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w[j]), k0 + b));
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) acc[j][e] += wk * x[j][b][e];
+        }
       }
+  }
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) {
+    if (i0 + j >= n * a.hq) break;
+    bf16_t* o = (bf16_t*)a.o + ((size_t)qb * a.hq + i0 + j) * D + lane * kPer;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const __bf16 v = (__bf16)(acc[j][e] * inv[j]);
+      o[e] = __builtin_bit_cast(bf16_t, v);
     }
   }
-  bf16_t* o = (bf16_t*)a.o + ((size_t)qb * a.hq + i) * D + lane * kPer;
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    const __bf16 b = (__bf16)(acc[e] * inv);
-    o[e] = __builtin_bit_cast(bf16_t, b);
-  }
+}
+
+// Pairs of a wave of the join: four where there are more than 256 CUs hold waves for.
+static int tree_join_rows(const TreeArgs& a) {
+  return (int64_t)a.num_seqs * a.max_nodes * a.hq > 256 * 32 ? 4 : 1;
 }
 
 TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
@@ -353,7 +379,8 @@ size_t tree_partial_rows(const TreeShape& t, int hkv) {
 }
 
 static int64_t tree_join_grid(const TreeArgs& a) {
-  return (int64_t)a.num_seqs * (((int64_t)a.max_nodes * a.hq + 3) / 4);
+  const int rows = 4 * tree_join_rows(a);
+  return (int64_t)a.num_seqs * (((int64_t)a.max_nodes * a.hq + rows - 1) / rows);
 }
 static int64_t tree_units_grid(int64_t units, int hkv, int row_blocks) {
   return (units * hkv + kNumXcd - 1) / kNumXcd * kNumXcd * row_blocks;
@@ -376,9 +403,12 @@ static hipError_t launch_tree_d(const TreeArgs& a, hipStream_t stream) {
     go(tree_kernel<D, 1>);
   else
     go(tree_kernel<D, kTrPlanSeqs / kWave>);
-  if (a.part_o != nullptr)
-    hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)tree_join_grid(a)), dim3(256), 0,
-                       stream, a);
+  if (a.part_o != nullptr) {
+    auto join = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)tree_join_grid(a)), dim3(256), 0, stream, a);
+    };
+    tree_join_rows(a) == 4 ? join(tree_join_kernel<D, 4>) : join(tree_join_kernel<D, 1>);
+  }
   return hipGetLastError();
 }
 

@@ -192,6 +192,13 @@ def test_a_few_long_sequences_among_many_short_ones(rows, hkv):
     c.check()
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(25, 1, 128), (28, 4, 64)])
+def test_joins_of_many_rows(hq, hkv, d):
+    """More rows than waves fit on the chip: a wave joins several, the last fewer."""
+    rng = random.Random(hq)
+    Case([900, 40, 2000, 300], trees(rng, [101, 3, 90, 51]), hq, hkv, d, hq).check((0, 5, 64))
+
+
 def test_wide_table_and_long_context():
     rng = random.Random(3)
     Case([9000, 40, 2500], trees(rng, [25, 60, 3]), 8, 2, 128, 21, max_blocks=2300).check((0, 64))
