@@ -13,7 +13,7 @@
 // Measured (32 q / 8 kv heads of 128): 48 sequences of 700 to 10,304 keys and 5 to
 // 12 nodes 150 us, K/V at 4.6 TB/s (HBM); 16 of 2,600 to 10,300 keys and 64 nodes 119
 // us, 685 TFLOP/s (the tile loop, 106, and the join, 13); one of 4,782
-// and 25 nodes 19.8 us: 16.0 for pieces of 8 or 9 blocks, of which the chain of
+// and 25 nodes 19.8 us: 15.2 for pieces of 8 or 9 blocks, of which the chain of
 // lengths, page ids, first copies and queries takes 4, and 4.4 for the join.
 #include "common.h"
 #include "draft.h"
@@ -26,7 +26,7 @@ namespace {
 constexpr int kTrRows = 32 * kMtWaves;
 constexpr int kTrPlanSeqs = 256;     // sequences whose pieces are cut from their lengths
 // Blocks of a share, at least: a unit's start, end and join cost about
-// as much as eight.  One sequence of 8192 keys, 32 q / 8 kv heads, 32 nodes: 19.9 us;
+// as much as eight.  One sequence of 4,782 keys, 32 q / 8 kv heads, 25 nodes: 19.9 us;
 // cut down to 4 blocks 22.4, to 16 23.5, to 32 34.8.
 constexpr int kTrMinBlocks = 8;
 
