@@ -352,14 +352,14 @@ rag_status rag_kv_cache_write(const void *k, const void *v, void *k_cache,
  * top, rows in order, pages in order.  A row fits while there are pages on the
  * stack for it, its pages fit the table and its tokens slot_mapping; from the
  * first row that does not fit on no row grows (shrinking rows shrink all the
- * same).  num_free_out, num_granted and lens_out must not be num_free, old_lens
- * or new_lens: every workgroup reads those.
+ * same).  An array that the call writes must not overlap any other of its arrays:
+ * every workgroup reads the inputs.
  * Preconditions (checked when RAG_ATTN_CHECK=1): 0 <= old_lens[s] <=
  * max_blocks_per_seq * 16, new_lens[s] >= 0, 0 <= num_free <= num_blocks, every
  * page at most once on the stack or in a row.
  *
- * Returns RAG_OK, RAG_ERR_INVALID_ARG (null pointer, negative size, an output
- * that is an input, violated precondition in debug mode), RAG_ERR_UNSUPPORTED
+ * Returns RAG_OK, RAG_ERR_INVALID_ARG (null pointer, negative size, arrays that
+ * overlap, violated precondition in debug mode), RAG_ERR_UNSUPPORTED
  * (block_size not 16, num_seqs over 4096, num_blocks over 2^27,
  * max_blocks_per_seq from 2^27 on, max_new_tokens from 2^30 on) or RAG_ERR_HIP.
  */

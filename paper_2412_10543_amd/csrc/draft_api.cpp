@@ -45,6 +45,26 @@ rag_status check_paging(const char* who, int32_t block_size, int32_t max_blocks,
   return RAG_OK;
 }
 
+// An int32 array of a call.
+struct Array {
+  const char* name;
+  const int32_t* at;
+  size_t count;
+};
+
+// None of the first `written` arrays overlaps another one.
+rag_status check_apart(const char* who, const Array* arrays, int count, int written) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < count; ++j) {
+      const Array &a = arrays[i], &b = arrays[j];
+      const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+      if (a.count > 0 && b.count > 0 &&
+          (x >= y ? x - y < b.count * sizeof(int32_t) : y - x < a.count * sizeof(int32_t)))
+        return fail(RAG_ERR_INVALID_ARG, "%s: %s and %s overlap", who, a.name, b.name);
+    }
+  return RAG_OK;
+}
+
 // Debug mode: the first `pages` entries of table row s are pages of the pool.
 rag_status check_table(const char* who, const std::vector<int32_t>& bt, int32_t s,
                        int32_t max_blocks, int32_t first, int32_t pages, int32_t num_blocks) {
@@ -174,9 +194,20 @@ rag_status rag_kv_pages_update(int32_t* block_tables, int32_t* free_pages, const
       (num_seqs > 0 && max_blocks_per_seq > 0 && !block_tables) || (num_blocks > 0 && !free_pages) ||
       (max_new_tokens > 0 && !slot_mapping))
     return fail(RAG_ERR_INVALID_ARG, "kv pages: null pointer argument");
-  if (num_free_out == num_free || num_granted == num_free || num_granted == num_free_out ||
-      (num_seqs > 0 && (lens_out == old_lens || lens_out == new_lens)))
-    return fail(RAG_ERR_INVALID_ARG, "kv pages: an output is also an input");
+  // (every workgroup reads the inputs, and no workgroup waits for another)
+  const size_t rows = (size_t)num_seqs;
+  const Array arrays[] = {{"block_tables", block_tables, rows * (size_t)max_blocks_per_seq},
+                          {"free_pages", free_pages, (size_t)num_blocks},
+                          {"num_free_out", num_free_out, 1},
+                          {"lens_out", lens_out, rows},
+                          {"cu_new", cu_new, rows + 1},
+                          {"slot_mapping", slot_mapping, (size_t)max_new_tokens},
+                          {"num_granted", num_granted, 1},
+                          {"num_free", num_free, 1},
+                          {"old_lens", old_lens, rows},
+                          {"new_lens", new_lens, rows}};
+  st = check_apart("kv pages", arrays, 10, 7);
+  if (st != RAG_OK) return st;
   const rag::PagesArgs a{block_tables, free_pages, num_free,     old_lens,           new_lens,
                          num_free_out, lens_out,   cu_new,       slot_mapping,       num_granted,
                          num_seqs,     max_blocks_per_seq,       num_blocks,         max_new_tokens};

@@ -44,6 +44,29 @@ def test_pages_refusals(kw, status):
     _says(binding.lib().rag_kv_pages_update(*a.values(), None), status)
 
 
+# the arrays of rag_kv_pages_update and their int32 values for 4 rows, 8 pages a row, 100 pages
+# and 64 slots; the call writes those of the first line
+PAGES_ARRAYS = dict(table=32, stack=100, num_free_out=1, lens=4, cu=5, slots=64, granted=1,
+                    num_free=1, old=4, new=4)
+PAGES_WRITTEN = list(PAGES_ARRAYS)[:7]
+
+
+@needs_lib
+@pytest.mark.parametrize("a,b", [(a, b) for i, a in enumerate(PAGES_WRITTEN)
+                                 for b in list(PAGES_ARRAYS)[i + 1:]])
+def test_pages_refuse_a_written_array_that_overlaps_another(a, b):
+    """Every workgroup reads the inputs while others write: whole, by the first
+    value and by the last."""
+    at = {name: FAKE + 4096 * i for i, name in enumerate(PAGES_ARRAYS)}
+    order = ["table", "stack", "num_free", "old", "new", "S", "width", "blocks", "bs", "tokens",
+             "num_free_out", "lens", "cu", "slots", "granted"]
+    for shift in (0, PAGES_ARRAYS[b] - 1, 1 - PAGES_ARRAYS[a]):
+        v = dict(at, S=4, width=8, blocks=100, bs=16, tokens=64)
+        v[a] = at[b] + 4 * shift
+        _says(binding.lib().rag_kv_pages_update(*(v[n] for n in order), None), BAD)
+        assert "overlap" in binding.rag_last_error()
+
+
 @needs_lib
 @pytest.mark.parametrize("kw,status", [
     (dict(kc=None), BAD), (dict(vc=None), BAD), (dict(table=None), BAD), (dict(base=None), BAD),

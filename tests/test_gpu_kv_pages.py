@@ -124,6 +124,29 @@ def test_many_steps_keep_every_page_once():
         assert sorted(held + stack[:free]) == list(range(blocks))
 
 
+def test_arrays_side_by_side_in_one_buffer():
+    """A program's step state as one allocation: arrays may touch, and the two inputs
+    may be one."""
+    rng = random.Random(5)
+    old = [20, 0, 47, 16, 3]
+    table, stack, n = layout(rng, old, 6, 20)
+    for new in ([33, 50, 10, 17, 0], old):
+        parts = [sum(table, []), stack, [n], [-5], [-5] * 5, [-5] * 6, [-5] * 80, [-5]] + \
+            ([old] if new is old else [old, new])
+        buf, at, views = i32(sum(parts, [])), 0, []
+        for x in parts:
+            views.append(buf[at:at + len(x)])
+            at += len(x)
+        t, s, free, free_out, lens, cu, slots, granted, o = views[:9]
+        binding.rag_kv_pages_update(t.view(5, 6), s, free, o, views[-1], free_out, lens, cu, slots,
+                                    granted)
+        want = ds.reference_pages(table, stack, n, old, new, 80)
+        got = [t.view(5, 6).tolist(), s.tolist(), free_out.item(), lens.tolist(), cu.tolist(),
+               slots.tolist(), granted.item()]
+        assert got == [want[x] for x in ("table", "stack", "free", "lens", "cu", "slots", "granted")]
+        assert free.item() == n and o.tolist() == old and views[-1].tolist() == list(new)
+
+
 # ---------------------------------------------------------------------------
 # keep
 # ---------------------------------------------------------------------------
