@@ -82,7 +82,7 @@ class Config(ctypes.Structure):
 
 def lib():
     """Load (once) and return the ctypes handle of librag_attn.so."""
-    global _lib, _marshal
+    global _lib
     if _lib is not None:
         return _lib
     if not os.path.exists(LIBRARY):
@@ -151,7 +151,6 @@ def lib():
     L.rag_plan_prompts.restype = ctypes.c_int
     L.rag_plan_prompts.argtypes = [ctypes.c_int, _i32, _i32p, _i32p, _i32, _i32, _i32, _i32p,
                                    _i32, _i32p, _i32p]
-    from . import _marshal
     _lib = L
     return L
 
@@ -344,8 +343,21 @@ def _pointers(spec, *tensors):
     """(device, address and sizes of each tensor) of contiguous tensors on the
     current device, with the types and ranks of spec (see csrc/marshal.cpp), or a
     number for _refuse_at."""
-    lib()
+    if _marshal is None:
+        _load_marshal()
     return _marshal.pointers(spec, *tensors)
+
+
+def _load_marshal():
+    """The library, and the native checks of tensors beside it."""
+    global _marshal
+    lib()
+    try:
+        from . import _marshal as loaded
+    except ImportError as e:
+        raise ImportError("_marshal.so is not built, or for another torch; run "
+                          f"__graft_entry__.build() or python -m paper_2412_10543_amd.build ({e})") from e
+    _marshal = loaded
 
 
 _TYPES = {"i": torch.int32, "l": torch.int64, "b": torch.bfloat16, "f": torch.float32}

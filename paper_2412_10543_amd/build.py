@@ -4,6 +4,7 @@
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -57,10 +58,12 @@ MARSHAL = os.path.join(PKG, "_marshal.so")
 def build_marshal(verbose: bool = False) -> str:
     """The binding's checks of tensors (host code against torch's headers)."""
     import sysconfig
+
     import torch
     from torch.utils.cpp_extension import include_paths, library_paths
     tmp = MARSHAL + ".tmp"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+    cmd = [HIPCC, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared",
+           "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            *(f"-I{p}" for p in include_paths("cuda")), "-I" + sysconfig.get_paths()["include"],
            os.path.join(CSRC, "marshal.cpp"), "-o", tmp,
@@ -92,7 +95,8 @@ def build(verbose: bool = False) -> str:
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIBRARY)
     build_probes(verbose)
-    build_marshal(verbose)
+    if importlib.util.find_spec("torch") is not None:   # (without it there are no tensors to check)
+        build_marshal(verbose)
     return LIBRARY
 
 
