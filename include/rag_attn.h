@@ -373,11 +373,14 @@ rag_status rag_kv_pages_update(int32_t *block_tables, int32_t *free_pages,
                                int32_t *num_granted, hipStream_t stream);
 
 /*
- * Bytes of workspace that rag_attn_decode_paged_tree needs (0 where it does not
- * cut its sequences, and for invalid sizes).  Library-internal layout: fp32
- * partial outputs (head_dim values for every piece and (node, q head) pair, in
- * whole blocks of 128 pairs of a kv head above that number), their fp32
- * log-sum-exp values, and two int32 for every sequence.
+ * Bytes of workspace for rag_attn_decode_paged_tree calls of these sizes and of
+ * smaller ones: with the same heads and num_splits it never falls as num_seqs,
+ * max_nodes or max_blocks_per_seq grow, so that the size for a program's largest
+ * step serves all its steps.  0 where none of them cuts its sequences, and for
+ * invalid sizes.  Library-internal layout: fp32 partial outputs (head_dim values
+ * for every piece and (node, q head) pair, in whole blocks of 128 pairs of a kv
+ * head above that number), their fp32 log-sum-exp values, and two int32 for every
+ * sequence.
  */
 size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
                                            int32_t num_q_heads,
@@ -416,8 +419,9 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
  *            at a time get even shares of all keys; with more, none.
  *   workspace, workspace_bytes  device scratch of at least
  *            rag_attn_decode_tree_workspace_size(...) bytes for the same
- *            arguments (NULL when that is 0); 256-byte aligned, of any contents.
- *            Calls that may overlap, and graphs that may be replayed at once,
+ *            arguments or for larger sizes (NULL when that is 0); 256-byte
+ *            aligned, of any contents.  Calls of any sizes may follow each other
+ *            in it.  Calls that may overlap, and graphs that may be replayed at once,
  *            must not share it.
  *
  * Any num_q_heads / num_kv_heads.  Returns RAG_OK (num_seqs == 0 or max_nodes == 0

@@ -76,6 +76,7 @@ struct RangesArgs {
 
 constexpr int kPagesMaxSeqs = 4096;        // rows of one rag_kv_pages_update call (LDS)
 constexpr int kTreeMaxSplits = 64;
+constexpr int kTreePlanSeqs = 256;         // sequences whose pieces are cut from their lengths
 
 int64_t pages_grid(const PagesArgs& a);
 hipError_t launch_pages(const PagesArgs& a, hipStream_t stream);
@@ -84,6 +85,8 @@ hipError_t launch_keep(const KeepArgs& a, hipStream_t stream);
 TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
                      int requested);
 size_t tree_partial_rows(const TreeShape& t, int hkv);
+size_t tree_partial_rows_upto(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
+                              int requested);
 int64_t tree_grid(const TreeShape& t, const TreeArgs& a);
 hipError_t launch_tree(const TreeArgs& a, hipStream_t stream);
 int64_t ranges_grid(const RangesArgs& a);       // workgroups, at most

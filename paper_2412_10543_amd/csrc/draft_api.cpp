@@ -155,14 +155,16 @@ rag_status check_tree(const rag::TreeArgs& a, int32_t num_blocks, hipStream_t st
   return RAG_OK;
 }
 
+// (Rows of a sequence are counted in 32 bits, with room for their blocks.)
+bool too_many_rows(int32_t nodes, int32_t hq) { return (int64_t)nodes * hq >= 1 << 24; }
+
 // Workspace of a tree launch that may cut: fp32 partial outputs, fp32
 // log-sum-exps, int32 pairs per sequence.
 struct TreeWs {
   size_t lse_off, of_off, bytes;
 };
 
-TreeWs tree_workspace(const rag::TreeShape& t, int32_t num_seqs, int32_t hkv, int32_t d) {
-  const size_t rows = rag::tree_partial_rows(t, hkv);
+TreeWs tree_workspace(size_t rows, int32_t num_seqs, int32_t d) {
   if (rows == 0) return {0, 0, 0};
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   TreeWs w;
@@ -255,11 +257,13 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes, 
                                            int32_t num_splits) {
   (void)block_size;
   if (num_seqs <= 0 || max_nodes <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 ||
-      num_q_heads % num_kv_heads != 0 || head_dim <= 0 || max_blocks_per_seq <= 0 || num_splits < 0)
+      num_q_heads % num_kv_heads != 0 || head_dim <= 0 || max_blocks_per_seq <= 0 || num_splits < 0 ||
+      too_many_rows(max_nodes, num_q_heads) || max_blocks_per_seq >= kMaxPages)
     return 0;
-  const rag::TreeShape t = rag::tree_shape(num_seqs, max_nodes, num_q_heads, num_kv_heads,
-                                           head_dim, max_blocks_per_seq, num_splits);
-  return tree_workspace(t, num_seqs, num_kv_heads, head_dim).bytes;
+  const size_t rows = rag::tree_partial_rows_upto(num_seqs, max_nodes, num_q_heads, num_kv_heads,
+                                                  head_dim, max_blocks_per_seq, num_splits);
+  return tree_workspace(rows, num_splits > 0 ? num_seqs : std::min(num_seqs, rag::kTreePlanSeqs),
+                        head_dim).bytes;
 }
 
 rag_status rag_attn_decode_paged_tree(const void* q, const void* k_cache, const void* v_cache,
@@ -289,7 +293,7 @@ rag_status rag_attn_decode_paged_tree(const void* q, const void* k_cache, const 
   if (num_seqs == 0 || max_nodes == 0) return ok();
   if (max_blocks_per_seq == 0)
     return fail(RAG_ERR_INVALID_ARG, "%s: max_blocks_per_seq is 0", who);
-  if ((int64_t)max_nodes * num_q_heads >= 1 << 24)
+  if (too_many_rows(max_nodes, num_q_heads))
     return fail(RAG_ERR_UNSUPPORTED, "%s: %d nodes of %d heads", who, max_nodes, num_q_heads);
   rag::TreeArgs a{q, k_cache, v_cache, o, tree_mask, block_tables, kv_lens, cu_seqlens_q, num_seqs,
                   max_nodes, mask_words, max_blocks_per_seq, num_q_heads, num_kv_heads, head_dim,
@@ -302,7 +306,8 @@ rag_status rag_attn_decode_paged_tree(const void* q, const void* k_cache, const 
   a.splits = t.splits;
   a.units = (int)t.units;
   a.part_rows = t.part_rows;
-  const TreeWs ws = tree_workspace(t, num_seqs, num_kv_heads, head_dim);
+  // (what this launch uses; the size asked for before may be that of a larger one)
+  const TreeWs ws = tree_workspace(rag::tree_partial_rows(t, num_kv_heads), num_seqs, head_dim);
   if (ws.bytes > 0) {
     if (workspace == nullptr || workspace_bytes < ws.bytes)
       return fail(RAG_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, ws.bytes,

@@ -24,7 +24,6 @@ namespace rag {
 namespace {
 
 constexpr int kTrRows = 32 * kMtWaves;
-constexpr int kTrPlanSeqs = 256;     // sequences whose pieces are cut from their lengths
 // Blocks of a share, at least: a unit's start, end and join cost about
 // as much as eight.  One sequence of 4,782 keys, 32 q / 8 kv heads, 25 nodes: 19.9 us;
 // cut down to 4 blocks 22.4, to 16 23.5, to 32 34.8.
@@ -159,7 +158,7 @@ __device__ __forceinline__ int tree_scan(int x) {
   return x;
 }
 
-// Otherwise (at most kTrPlanSeqs sequences) all sequences' blocks, kTrStart more in
+// Otherwise (at most kTreePlanSeqs sequences) all sequences' blocks, kTrStart more in
 // front of each for what its start costs, stand in one row that is cut into even
 // shares, one a unit: a unit has the end of a sequence, whole ones and the
 // beginning of one, of which the first and the last may have partials (places 2 unit
@@ -346,24 +345,28 @@ static int tree_join_rows(const TreeArgs& a) {
   return (int64_t)a.num_seqs * a.max_nodes * a.hq > 256 * 32 ? 4 : 1;
 }
 
+// Workgroups that are on the chip at a time (the LDS of two a CU, three at D = 64).
+static int64_t tree_places(int d) { return (d == 64 ? 3 : 2) * 256; }
+
+// Key blocks of the longest sequence.
+static int64_t tree_longest(int max_blocks) { return ((int64_t)max_blocks + 1) / 2; }
+
 TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
                      int requested) {
   TreeShape t{};
   const int64_t rows = (int64_t)max_nodes * (hq / hkv);
   t.row_blocks = (int)((rows + kTrRows - 1) / kTrRows);
   t.part_rows = (int)std::min<int64_t>(rows, kTrRows);
-  const int64_t blocks = ((int64_t)max_blocks + 1) / 2;          // of the longest sequence
+  const int64_t blocks = tree_longest(max_blocks);
   // (the plan's sums are 32-bit)
-  if (requested > 0 || num_seqs > kTrPlanSeqs || num_seqs * (blocks + kTrStart) >= 1 << 30) {
+  if (requested > 0 || num_seqs > kTreePlanSeqs || num_seqs * (blocks + kTrStart) >= 1 << 30) {
     t.splits = (int)std::max<int64_t>(1, std::min<int64_t>({requested, kTreeMaxSplits, blocks}));
     t.units = t.places = (int64_t)num_seqs * t.splits;
     return t;
   }
   t.splits = 0;
-  // As many units as are on the chip at a time (the LDS of two workgroups a CU, three
-  // at D = 64).
-  const int64_t units = (d == 64 ? 3 : 2) * 256;
-  int64_t n = std::max<int64_t>(1, units / ((int64_t)hkv * t.row_blocks));
+  // As many units as are on the chip at a time.
+  int64_t n = std::max<int64_t>(1, tree_places(d) / ((int64_t)hkv * t.row_blocks));
   n = std::min(n, num_seqs * std::max<int64_t>(1, blocks / kTrMinBlocks));
   if (n <= num_seqs && blocks < kTrLongBlocks) {                 // nothing to cut
     t.splits = 1;
@@ -376,6 +379,23 @@ TreeShape tree_shape(int num_seqs, int max_nodes, int hq, int hkv, int d, int ma
 
 size_t tree_partial_rows(const TreeShape& t, int hkv) {
   return t.splits == 1 ? 0 : (size_t)t.places * hkv * t.row_blocks * t.part_rows;
+}
+
+// No less than tree_partial_rows of a launch of these sizes or of smaller ones.  (The
+// launch's own number goes up and down: with more rows the same workgroups make fewer
+// units, and with more sequences none may be cut.)  Its units are limited as in
+// tree_shape, by the chip and by the blocks; in each limit, times hkv * row_blocks, the
+// sizes only add.
+size_t tree_partial_rows_upto(int num_seqs, int max_nodes, int hq, int hkv, int d, int max_blocks,
+                              int requested) {
+  const TreeShape t = tree_shape(num_seqs, max_nodes, hq, hkv, d, max_blocks, requested);
+  if (requested > 0) return tree_partial_rows(t, hkv);           // (adds with the sizes by itself)
+  const int64_t pieces = tree_longest(max_blocks) / kTrMinBlocks;
+  if (pieces <= 1) return 0;                                     // no sequence is ever cut
+  const int64_t streams = (int64_t)hkv * t.row_blocks;
+  const int64_t units = std::min(std::max(tree_places(d), streams),
+                                 std::min(num_seqs, kTreePlanSeqs) * pieces * streams);
+  return (size_t)(2 * units) * t.part_rows;
 }
 
 static int64_t tree_join_grid(const TreeArgs& a) {
@@ -402,7 +422,7 @@ static hipError_t launch_tree_d(const TreeArgs& a, hipStream_t stream) {
   else if (a.num_seqs <= kWave)
     go(tree_kernel<D, 1>);
   else
-    go(tree_kernel<D, kTrPlanSeqs / kWave>);
+    go(tree_kernel<D, kTreePlanSeqs / kWave>);
   if (a.part_o != nullptr) {
     auto join = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)tree_join_grid(a)), dim3(256), 0, stream, a);

@@ -132,6 +132,25 @@ def test_tree_workspace_sizes():
 
 
 @needs_lib
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (4, 2, 64), (64, 8, 128), (25, 1, 128), (14, 2, 64),
+                                      (600, 600, 128), (900, 900, 64)])
+@pytest.mark.parametrize("splits", [0, 1, 2, 3, 64])
+def test_tree_workspace_of_the_largest_step_serves_every_smaller_one(hq, hkv, d, splits):
+    axes = [(1, 2, 4, 8, 16, 17, 63, 64, 65, 100, 255, 256, 257, 1000, 100000),
+            (1, 2, 7, 8, 16, 17, 31, 32, 33, 64, 65, 100, 127, 128, 130, 300, 1000),
+            (1, 15, 16, 29, 31, 32, 33, 64, 100, 125, 126, 127, 128, 650, 2300, 1 << 20)]
+    size = {(s, n, w): binding.rag_attn_decode_tree_workspace_size(s, n, hq, hkv, d, w,
+                                                                   num_splits=splits)
+            for s in axes[0] for n in axes[1] for w in axes[2]}
+    for at in size:
+        for i, axis in enumerate(axes):
+            k = axis.index(at[i]) + 1
+            if k < len(axis):
+                more = (*at[:i], axis[k], *at[i + 1:])
+                assert size[at] <= size[more], (at, more)
+
+
+@needs_lib
 def test_binding_refuses_what_is_not_on_the_gpu():
     i32 = torch.zeros(4, dtype=torch.int32)
     x = torch.zeros((4, 2, 64), dtype=torch.bfloat16)

@@ -276,6 +276,26 @@ def test_streams_and_workspaces():
         ds.within(got, *want[i])
 
 
+def test_smaller_steps_in_the_workspace_of_the_largest():
+    """One workspace for a serving program's largest step; its steps of fewer rows,
+    smaller trees and narrower tables run in it."""
+    rng = random.Random(13)
+    n = binding.rag_attn_decode_tree_workspace_size(260, 70, 16, 8, 128, 100)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    for rows, nodes, width in ((260, 9, 33), (70, 9, 100), (63, 9, 100), (64, 8, 100), (7, 70, 100),
+                               (7, 64, 100), (1, 70, 100), (1, 1, 100), (3, 16, 40), (9, 65, 31)):
+        counts = [rng.randint(0, nodes) for _ in range(rows)]
+        counts[-1] = nodes
+        priors = [rng.choice([0, 5, rng.randint(0, min(width * 16 - nodes, 200))]) for _ in range(rows)]
+        priors[0] = width * 16 - nodes
+        print(f"{rows} rows of up to {nodes} nodes, {width} pages", flush=True)
+        c = Case(priors, trees(rng, counts), 16, 8, 128, rows + nodes, max_blocks=width)
+        want, bound = c.want()
+        got = c.run(0, ws=ws)
+        torch.cuda.synchronize()
+        ds.within(got, want, bound, f"{rows} rows")
+
+
 def test_refused_on_the_gpu():
     c = Case([900], trees(random.Random(7), [40]), 32, 8, 128, 50)
     with pytest.raises(binding.RagError) as e:
