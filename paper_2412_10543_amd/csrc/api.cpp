@@ -145,7 +145,9 @@ WsLayout workspace_layout(int32_t num_decode, int32_t hq, int32_t d, int32_t spl
 // Debug-mode check of a slot mapping: in range, no slot written twice.
 rag_status check_slots(const std::vector<int32_t>& sl, int32_t num_blocks, const char* who) {
   const int64_t slots = (int64_t)num_blocks * kBlock;
-  std::vector<char> seen((size_t)std::max<int64_t>(slots, 0), 0);
+  std::vector<char> seen;
+  if (!rag::room(seen, (size_t)std::max<int64_t>(slots, 0)))
+    return fail(RAG_ERR_HIP, "%s: no host memory for the debug check", who);
   for (size_t t = 0; t < sl.size(); ++t) {
     const int32_t s = sl[t];
     if (s < 0) continue;

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cstdlib>
+#include <exception>
 #include <vector>
 
 #include "errors.h"
@@ -25,10 +26,21 @@ inline bool check_mode() {
   return on;
 }
 
+// n zeros, if the host has the memory.
+template <class T>
+inline bool room(std::vector<T>& dst, size_t n) {
+  try {
+    dst.assign(n, T());
+    return true;
+  } catch (const std::exception&) {              // (none may leave the C entries)
+    return false;
+  }
+}
+
 // Copies n values from device memory (stream-ordered, synchronous).
 template <class T>
 inline bool fetch(std::vector<T>& dst, const T* src, size_t n, hipStream_t stream) {
-  dst.resize(n);
+  if (!room(dst, n)) return false;
   if (n == 0) return true;
   if (hipMemcpyAsync(dst.data(), src, n * sizeof(T), hipMemcpyDeviceToHost, stream) != hipSuccess)
     return false;

@@ -87,7 +87,9 @@ rag_status check_pages(const rag::PagesArgs& a, hipStream_t stream) {
     return fail(RAG_ERR_HIP, "kv pages: debug copy of device arrays failed");
   if (nf[0] < 0 || nf[0] > a.num_blocks)
     return fail(RAG_ERR_INVALID_ARG, "kv pages: num_free %d outside [0, %d]", nf[0], a.num_blocks);
-  std::vector<char> seen((size_t)a.num_blocks, 0);
+  std::vector<char> seen;
+  if (!rag::room(seen, (size_t)a.num_blocks))
+    return fail(RAG_ERR_HIP, "kv pages: no host memory for the debug check");
   auto once = [&](int32_t id) { return id >= 0 && id < a.num_blocks && !seen[(size_t)id]++; };
   for (int32_t i = 0; i < nf[0]; ++i)
     if (!once(st[(size_t)i]))
