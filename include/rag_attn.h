@@ -494,7 +494,10 @@ rag_status rag_kv_cache_keep(void *k_cache, void *v_cache,
  *   key_ranges  device int32 [Tq, 2], 8-byte aligned; any values (shared beyond
  *            nk is nk, a negative one 0; start beyond p: no key of its own).
  * Key tiles that no row of a query tile sees are not read.  A token generated
- * behind such a prompt sees all its keys: rag_attn_decode_paged.
+ * behind documents or a prefix sees all its keys: rag_attn_decode_paged.  One
+ * behind a window does not, and the paged calls have no first key: it is a
+ * sequence of one row (nq = 1, the window's range at its p) of this call, over
+ * packed keys.
  *
  * Returns the statuses of rag_attn_prefill_varlen.
  */

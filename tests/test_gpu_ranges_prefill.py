@@ -92,6 +92,19 @@ def test_prefix_and_window():
     check(*inputs(lens, lens, 8, 8, 64, 6), lens, lens, r)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 2, 64)])
+def test_tokens_behind_windows_are_sequences_of_one_row(hq, hkv, d):
+    """A generated token's row alone over its packed keys, windows of 50 keys and
+    the first 4: what the row would see as a prompt's last."""
+    lens = [1, 2, 50, 54, 55, 400, 1000]
+    q, k, v = inputs(lens, lens, hq, hkv, d, 17)
+    at = torch.tensor(lens).cumsum(0) - 1
+    alone = check(q[at.cuda()].contiguous(), k, v, [1] * len(lens), lens, [(4, n - 50) for n in lens])
+    whole = i32([(4, p - 49) for n in lens for p in range(n)])
+    want, _, bound, _ = ds.reference_ranges(q, k, v, lens, lens, whole, 1.0 / math.sqrt(d))
+    ds.within(alone, want[at], bound[at])
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_any_ranges(seed):
     """Values in and out of range, empty rows, fewer and more rows than keys, a
