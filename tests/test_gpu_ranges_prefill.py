@@ -194,6 +194,28 @@ def test_rows_behind_the_last_sequence_stay():
             binding.rag_attn_prefill_varlen_ranges(q, k, v, o, bad, cu(lens), cu(lens), r, 100, 100, 0.125)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (32, 8, 128)])
+@pytest.mark.parametrize("lens", [[100, 33], [1], [64, 64, 257]])
+def test_nothing_is_written_behind_the_log_sum_exps(hq, hkv, d, lens):
+    """They stand at the front of a longer buffer; q and o have rows behind the last
+    sequence."""
+    n = sum(lens)
+    q, k, v = inputs([n + 40], [n], hq, hkv, d, 3)
+    buf = torch.full((hq * n + 3000,), 7.0, device="cuda")
+    lse, o = buf[:hq * n].view(hq, n), torch.full_like(q, 7.0)
+    r = i32(sum(([(x // 3, x // 2)] * x for x in lens), []) + [(0, 0)] * 40)
+    binding.rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu(lens), cu(lens), r, max(lens), max(lens),
+                                           1.0 / math.sqrt(d))
+    wo, wl, bo, bl = ds.reference_ranges(q[:n], k, v, lens, lens, r[:n], 1.0 / math.sqrt(d))
+    torch.cuda.synchronize()
+    empty = wl == -math.inf
+    assert (lse.cpu()[empty] == -math.inf).all()
+    bl[empty] = math.nan
+    ds.within(lse, wl, bl, "lse")
+    ds.within(o[:n], wo, bo, "o")
+    assert (buf[hq * n:] == 7.0).all() and (o[n:] == 7.0).all()
+
+
 def test_offsets_past_32_bits():
     """A window over a packed batch whose last rows lie beyond 2^31 elements."""
     hq, hkv, d, n = 64, 1, 128, 2 ** 31 // (64 * 128) + 200

@@ -296,6 +296,43 @@ def test_smaller_steps_in_the_workspace_of_the_largest():
         ds.within(got, want, bound, f"{rows} rows")
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (14, 2, 64)])
+@pytest.mark.parametrize("splits", [0, 2, 5])
+def test_nothing_is_written_behind_the_workspace(hq, hkv, d, splits):
+    """Batches whose units are a chipful, and one alone, in a workspace of their size
+    with other bytes behind it."""
+    rng = random.Random(hq + splits)
+    for priors, counts in (([2500, 30, 900, 1700], [9, 4, 16, 1]), ([3000, 2000], [70, 25]), ([1200], [3]),
+                           ([700 + 40 * i for i in range(20)], [1 + i % 7 for i in range(20)])):
+        c = Case(priors, trees(rng, counts), hq, hkv, d, len(priors) + hq)
+        n = binding.rag_attn_decode_tree_workspace_size(len(c.n), c.max_nodes, hq, hkv, d,
+                                                        c.pool.block_tables.shape[1], num_splits=splits)
+        assert n > 0
+        buf = torch.full((n + (1 << 20),), 90, dtype=torch.uint8, device="cuda")
+        got = c.run(splits, ws=buf[:n])
+        want, bound = c.want()
+        torch.cuda.synchronize()
+        ds.within(got, want, bound)
+        assert (buf[n:] == 90).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (14, 2, 64)])
+@pytest.mark.parametrize("bound", [0, 20, 65, 300])
+@pytest.mark.parametrize("large", [0, 128])
+def test_bound_of_the_nodes_far_above_the_trees(hq, hkv, d, bound, large):
+    """max_nodes of a step that is made for larger trees, and one large tree among
+    small ones: row blocks that few sequences, or none, have rows in."""
+    rng = random.Random(bound + large + hq)
+    counts = [rng.choice([0, 1, 3, 9, 12]) for _ in range(14)]
+    priors = [rng.choice([0, 40, 900, rng.randint(0, 2500)]) for _ in counts]
+    counts[3], priors[3] = 5, 2500
+    if large:
+        counts[9], priors[9] = large, 1100
+    c = Case(priors, trees(rng, counts), hq, hkv, d, bound + hq, words=5)
+    c.max_nodes = max(c.max_nodes, bound)
+    c.check((0, 3))
+
+
 def test_refused_on_the_gpu():
     c = Case([900], trees(random.Random(7), [40]), 32, 8, 128, 50)
     with pytest.raises(binding.RagError) as e:
