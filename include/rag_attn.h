@@ -411,7 +411,9 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
  *            nodes, 0 <= n <= max_nodes and n <= kv_lens[s] <=
  *            max_blocks_per_seq * 16 (checked when RAG_ATTN_CHECK=1, and the ids
  *            of the pages read).  A sequence without nodes may hold no key.
- *   max_nodes  host upper bound of n (sizes the grid).
+ *   max_nodes  host upper bound of n (sizes the grid, in blocks of 128 (node, q head)
+ *            pairs of a kv head: a bound, or one tree, many such blocks above the
+ *            other trees leaves a part of the GPU idle).
  *   num_splits  0 = automatic; else the number of pieces (at most 64, and one for
  *            each 32 keys) that every sequence's keys are cut into.  Automatic: with
  *            at most 256 sequences the pieces are cut on the GPU from the
@@ -427,7 +429,8 @@ size_t rag_attn_decode_tree_workspace_size(int32_t num_seqs, int32_t max_nodes,
  * Any num_q_heads / num_kv_heads.  Returns RAG_OK (num_seqs == 0 or max_nodes == 0
  * is a no-op), RAG_ERR_INVALID_ARG (null or misaligned pointer, negative size,
  * heads, scale, too few mask words), RAG_ERR_UNSUPPORTED (head_dim not 64 or 128,
- * block_size not 16, max_nodes * num_q_heads from 2^24 on),
+ * block_size not 16, max_nodes * num_q_heads from 2^24 on, num_blocks over 2^27,
+ * max_blocks_per_seq from 2^27 on, a batch too large for one grid),
  * RAG_ERR_WORKSPACE or RAG_ERR_HIP.
  */
 rag_status rag_attn_decode_paged_tree(

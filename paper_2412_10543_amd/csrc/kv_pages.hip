@@ -4,8 +4,9 @@
 //   keep_kernel   the K/V rows of accepted drafted tokens moved to the end of
 //                 their sequence
 // Both move a few bytes per token; a call's time is its launch and its chain of
-// dependent reads (64 rows that grow by 1 to 64 tokens 6.3 us, 640 that get 576
-// each 6.8; 1 and 256 accepted paths 4.7 and 5.1; an empty launch takes 3.6).
+// dependent reads (64 rows that grow by 1 to 64 tokens 6.3 us a call, 640 that get 576
+// each 6.7; 1 and 256 accepted paths 5.2, of which the kernel 2.6 and 3.7; an empty
+// launch takes 3.6).
 #include <algorithm>
 
 #include "common.h"
@@ -201,7 +202,8 @@ __global__ __launch_bounds__(kPgThreads) void pages_kernel(PagesArgs a) {
 
 // Workgroups for the slots, and for the pages given back (of which the host knows
 // only that the pool has no more), at most one a CU: a row of 36000 tokens that ends
-// leaves 2250.
+// leaves 2250 (16 rows of 20,000 to 36,000 tokens that end beside 48 that get up to 8
+// more: 8.4 us, with workgroups for the slots alone 76).
 int64_t pages_grid(const PagesArgs& a) {
   const int64_t slots = ((int64_t)a.max_new_tokens + kPgSlots - 1) / kPgSlots;
   const int64_t pages = ((int64_t)a.num_blocks + kPgSlots - 1) / kPgSlots;

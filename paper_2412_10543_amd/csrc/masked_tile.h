@@ -342,8 +342,9 @@ struct BlockCopy {
 // Rows of a wave go to and from memory as 64-byte pieces, 16 rows an instruction,
 // through 2 KiB of LDS of the wave's own (io: 32 rows of 64 bytes, 16-byte chunk c
 // of row r at c ^ (r / 4) % 4), where a lane has its own row.  (A lane's row in
-// 16-byte pieces straight from memory is 64 pieces an instruction: queries and
-// outputs of 16 prompts of 6000 tokens took 160 us of 518.)
+// 16-byte pieces straight from memory, 8-byte ones back, is 64 pieces an instruction:
+// 16 prompts of 5 to 20 documents of 400 to 512 tokens 958 us for 880, with windows 1242
+// for 1154; trees, of fewer rows, the same.)
 __device__ __forceinline__ int io_at(int r, int c) { return 32 * r + 8 * (c ^ ((r >> 2) & 3)); }
 
 // The lane's query row: rows(r) is row r of the wave's 32.
@@ -506,8 +507,8 @@ struct MtLds {
 // first with zeros as the values of the block before it, and slots without a
 // block (their number is even) with weights of 0: with slots of several kinds the
 // accumulators had other registers in each, and the spills made every slot wait
-// for the copies (16 prompts of 5800 tokens in documents of 456: 2273 us against
-// 1441).
+// for the copies (in a first form, with eight waves and tiles of 64 keys, 16 prompts
+// of 5 to 20 documents: 2273 us against 1441).
 // Returns the items (a bit each) where a key that some row of the wave does not
 // see has an infinite or NaN value: its weight of 0 has then made NaN of rows that
 // it should not reach.

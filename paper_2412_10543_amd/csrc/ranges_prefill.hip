@@ -9,7 +9,7 @@
 // position.
 //
 // Measured (32 q / 8 kv heads of 128): 16 prompts of 5 to 20 documents of 400 to
-// 512 tokens and 64 query rows 0.90 ms, 560 TFLOP/s of visible pairs, matrix
+// 512 tokens and 64 query rows 0.88 ms, 567 TFLOP/s of visible pairs, matrix
 // cores 34%, vector issue 40% and LDS 23% busy: the waves' chains of one slot
 // after another, and the starts and ends of tiles of 14 blocks, bound it.  One
 // prompt of nine documents 88 us: its query's tiles, 150 blocks at 0.6 us one
@@ -28,12 +28,14 @@ namespace {
 
 // Tiles of every sequence that are dispatched first: those of a prompt's query, which
 // sees all its documents, would end a launch alone.  16 prompts of 5 to 20 documents
-// and 64 query rows (three tiles of 32): one first 1143 us, two 1077, four 902, six
-// 905; 128 query rows (five tiles): four 1169, six 1006, eight 1007.
+// and 64 query rows (three tiles of 32): one first 1072 us, two 1010, four 877, six 878,
+// eight 882; 128 query rows (five tiles): one 1161, two 1090, four 1117, six 976, eight
+// 979.
 constexpr int kRgLast = 6;
 // Of the others a workgroup takes kRgItems where there are at least kRgMany (eight
-// for each place of the GPU): 21800 tiles of 14 blocks 955 us one by one, 912 by
-// twos, 914 by fours; but 1024 rows with 8192 keys 163 us one by one, 526 by fours.
+// for each place of the GPU): 21800 tiles of 14 blocks 916 us one by one, 880 by twos,
+// 885 by fours; the same prompts with windows of 512 keys 1196, 1160 and 1170; but 1024
+// rows with 8192 keys 142 us one by one, 257 and 503.
 constexpr int kRgItems = 2;
 constexpr int64_t kRgMany = 4096;
 
@@ -156,10 +158,14 @@ __host__ __device__ constexpr int ranges_groups(int n_qt, int items) {
 }
 
 // Where the kv heads divide among the XCDs, each has all sequences' tiles of its own
-// heads and their K/V in its L2.  Elsewhere that would give the XCDs other sequences,
-// and other amounts of work, and tiles go round them one by one (32 q / 2 kv heads: 4
-// prompts with prefixes 87 us for 165, 4 with windows 47 for 54; 14 q / 2 kv heads of
-// 64: 4 prompts of documents 152 for 148).
+// heads and their K/V in its L2 (16 prompts of 5 to 20 documents, 32 q / 8 kv heads: 878
+// us, with tiles round the XCDs one by one 914; 16 / 16 heads 812 and 844).  Elsewhere
+// that would give the XCDs other sequences, and other amounts of work, and tiles go round
+// them.  4 prompts of 5 to 20 chunks with prefixes, tiles round the XCDs and not: 8 q / 1
+// kv heads 704 and 1764 us, 32 / 2 2762 and 3921, 32 / 4 2791 and 3893, 24 / 6 2178 and
+// 2587; with windows 87 and 180, 311 and 361, 333 and 360, 259 and 257; with documents 209
+// and 213, 264 and 287, 272 and 295, 229 and 224; 16 prompts of documents 261 and 275, 980
+// and 956, 998 and 975, 782 and 761.
 __host__ __device__ constexpr int ranges_parts(int hkv) { return hkv % kNumXcd == 0 ? kNumXcd : 1; }
 
 template <int D>

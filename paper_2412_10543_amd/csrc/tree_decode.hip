@@ -11,8 +11,8 @@
 // a second kernel joins.
 //
 // Measured (32 q / 8 kv heads of 128): 48 sequences of 700 to 10,304 keys and 5 to
-// 12 nodes 150 us, K/V at 4.6 TB/s (HBM); 16 of 2,600 to 10,300 keys and 64 nodes 119
-// us, 685 TFLOP/s (the tile loop, 106, and the join, 13); one of 4,782
+// 12 nodes 149 us, K/V at 4.6 TB/s (HBM); 16 of 2,600 to 10,300 keys and 64 nodes 117
+// us, 695 TFLOP/s (the tile loop 104 of them, the join 13); one of 4,782
 // and 25 nodes 19.8 us: 15.2 for pieces of 8 or 9 blocks, of which the chain of
 // lengths, page ids, first copies and queries takes 4, and 4.4 for the join.
 #include "common.h"
@@ -26,18 +26,20 @@ namespace {
 constexpr int kTrRows = 32 * kMtWaves;
 // Blocks of a share, at least: a unit's start, end and join cost about
 // as much as eight.  One sequence of 4,782 keys, 32 q / 8 kv heads, 25 nodes: 19.9 us;
-// cut down to 4 blocks 22.4, to 16 23.5, to 32 34.8.
+// cut down to 4 blocks 19.7, for twice the partials, to 16 23.6, to 32 36.2.
 constexpr int kTrMinBlocks = 8;
 
 // With sequences for a chipful of units, or more, nothing is cut where the tables have
-// fewer blocks than this (the join's launch would cost more).
+// fewer blocks than this (the join's launch would cost more: 64 sequences of 500 to
+// 1500 keys and 8 nodes 61 us, cut 73; 256 of 1000 keys 199, cut 211).
 constexpr int kTrLongBlocks = 64;
 
 // Blocks that the start of a sequence in a unit counts for.  40 sequences of 600 keys
-// and one of 20,000, 12 nodes: 45 us; with 3 or 6 blocks 51, as more short sequences are
-// cut; 63 of 500 and one of 30,000, 8 nodes: 56, with 3 blocks 63, with 14 59.
+// and one of 20,000, 12 nodes: 51 us; with 3 blocks 60, with 6 or 14 57 (more short
+// sequences are cut, or the long one less); 63 of 500 and one of 30,000, 8 nodes: 70,
+// with 3, 6 or 14 71, 69 and 72; 96 of 700 to 10,304 and 200 of 2,048 keys the same.
 // (Against a quota of blocks a piece and sequences apart: 48 of 700 to 10,304 keys
-// 161 -> 151 us, 96 of them 530 -> 470, 63 and one 75 -> 56, but 200 of 2,048 326 -> 342.)
+// 161 -> 149 us, 96 of them 519 -> 437, 63 and one 80 -> 70, but 200 of 2,048 325 -> 338.)
 constexpr int kTrStart = 10;
 
 // What the lane's row sees.
@@ -164,6 +166,11 @@ __device__ __forceinline__ int tree_scan(int x) {
 // beginning of one, of which the first and the last may have partials (places 2 unit
 // and 2 unit + 1).  The piece at `at` of the unit's share; wave-parallel, one lane per
 // sequence, and every wave finds the same.
+// The shares count key blocks, for the row blocks of max_nodes alike: where most trees
+// are far smaller, the workgroups of the other row blocks have nothing to do (48 trees of
+// up to 12 nodes, 32 q / 8 kv heads: 150 us, with max_nodes 64 192, with 128 311).  More
+// than kTreePlanSeqs sequences (four a lane) would take a scan of a second level: 256 of
+// 1,000 keys and one of 30,000 take 752 us, with one fewer 253.
 template <int kChunks>
 __device__ __forceinline__ TreePiece tree_share(const TreeArgs& a, int unit, int at) {
   const int lane = opaque_lane();
@@ -260,9 +267,10 @@ __global__ __launch_bounds__(64 * kMtWaves, 2) void tree_kernel(TreeArgs a) {
 }
 
 // o = sum_i 2^(lse_i - m) o_i / sum_i 2^(lse_i - m): one wave per kRows (node, q head)
-// pairs.  Small launches are one chain of reads long, with a wave a pair; where the
-// waves would come in several rounds, four pairs share the chain (tree_join_rows):
-// 16 trees of 64 nodes, 32 heads, in about 3 pieces 13.4 us, with a wave a pair 17.6.
+// pairs.  Small launches are one chain of reads long, with a wave a pair (one tree of 25
+// nodes, 32 heads: 19.8 us a call, by fours 22.1); where the waves would come in several
+// rounds, four pairs share the chain (tree_join_rows: 16 trees of 64 nodes in about 3
+// pieces 115.5 us a call, with a wave a pair 118.2).
 template <int D, int kRows>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   constexpr int kPer = D / 64;
