@@ -522,6 +522,236 @@ typedef enum {
 } rag_synthesis;
 
 /*
+ * New tokens between the projection and their attention, in one pass over the
+ * projection's output: the RMS norm of each head of Q and K, the rotation of both
+ * by the tokens' positions, and the K and V rows' way into the paged cache that
+ * rag_attn_decode_paged reads (Sec. "Implementation": the engine's paged KV cache).
+ *
+ *   norm      x -> x w / sqrt(mean(x^2) + eps) over the head_dim channels of a head
+ *   rotation  (a, b) -> (a cos - b sin, b cos + a sin) for the pairs of channels
+ *             (i, i + rotary_dim/2), or (2i, 2i+1) with interleaved = 1; channels from
+ *             rotary_dim on stay
+ * Both in fp32, rounded to bf16 once.  V is copied.
+ *
+ *   q        device [num_tokens, num_q_heads, head_dim], q_stride elements from token
+ *            to token (so that q, k and v may be parts of one projection's rows); NULL
+ *            with q_out NULL: K and V alone
+ *   k, v     device [num_tokens, num_kv_heads, head_dim], k_stride and v_stride
+ *            elements from token to token.  Strides are multiples of 8, at least the
+ *            heads' width, and not looked at for a single token.
+ *   q_out    device [num_tokens, num_q_heads, head_dim]; output
+ *   k_out, v_out  device [num_tokens, num_kv_heads, head_dim] or both NULL: the rows
+ *            also packed, for the prefill calls; output
+ *   k_cache, v_cache, slot_mapping, num_blocks, block_size  as in rag_kv_cache_write;
+ *            all three NULL: no cache (then k_out and v_out are needed).  A token
+ *            with a negative slot is padding: its position is not looked at, and
+ *            neither the cache nor its rows of q_out, k_out and v_out are written.
+ *   positions  device int32 [num_tokens], 0 <= positions[t] < max_position
+ *   cos_sin  device fp32 [max_position, rotary_dim]: for each position the cosines of
+ *            its rotary_dim/2 angles, then the sines.  positions and cos_sin NULL: no
+ *            rotation (max_position and rotary_dim are not looked at).
+ *   rotary_dim  a multiple of 16, at most head_dim
+ *   q_weight, k_weight  device [head_dim] or NULL: no norm of Q, of K
+ * An output may be its own input (q_out = q with q_stride = num_q_heads * head_dim, and
+ * so on); nothing else may overlap an output.
+ * Preconditions (checked when RAG_ATTN_CHECK=1): positions in the table, slots below
+ * num_blocks * 16, none repeated.
+ *
+ * Returns RAG_OK (num_tokens == 0 is a no-op), RAG_ERR_INVALID_ARG (null, misaligned or
+ * overlapping pointers, sizes, strides, eps, arguments that go together apart),
+ * RAG_ERR_UNSUPPORTED (head_dim not 64 or 128, block_size, rotary_dim not a multiple of
+ * 16, more than 65,536 heads) or RAG_ERR_HIP.
+ */
+rag_status rag_qkv_rope_write(
+    const void *q, const void *k, const void *v, int64_t q_stride,
+    int64_t k_stride, int64_t v_stride, void *q_out, void *k_out, void *v_out,
+    void *k_cache, void *v_cache, const int32_t *slot_mapping,
+    const int32_t *positions, const float *cos_sin, int32_t max_position,
+    int32_t rotary_dim, int32_t interleaved, const void *q_weight,
+    const void *k_weight, float eps, int32_t num_tokens, int32_t num_q_heads,
+    int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+    int32_t num_blocks, hipStream_t stream);
+
+/*
+ * The same into a paged cache held in 4 bits, which takes 9/32 of the bf16 cache's
+ * memory.  k_cache and v_cache are device uint8 [num_blocks, num_kv_heads,
+ * 9 * head_dim]: 16 tokens' rows of a kv head each.  slot_mapping, k_cache and v_cache
+ * are required.
+ *
+ * Every 64 channels of a token's K or V row, as rounded to bf16, have a scale s and a
+ * zero point z: with lo and hi their least and greatest value, or 0 where that is less
+ * or greater,
+ *   s = bf16((hi - lo) / 15),   z = round(-lo / s) in 0..15,
+ * and a value x has the code c = round(x / s) + z in 0..15, which stands for s (c - z)
+ * (rounding to nearest even; at most 0.56 s from x).  Groups of zeros, and those whose s
+ * rounds to 0, stand for 0; groups with a NaN or an infinity for NaN.  A page is
+ *   K codes  uint32 [16 tokens][4][head_dim/64][2]: word (i, g, w) holds channels 64 g +
+ *            16 i + 8 w + e, e = 0..7, in nibble e/2 (from the low end), + 4 for odd e
+ *   V codes  uint16 [16][16 tokens][head_dim/64]: unit (i, g) of a token holds channels
+ *            64 g + 4 i + e, e = 0..3, in nibble e
+ *   behind either, at byte 8 * head_dim: uint32 [head_dim/64][16 tokens], the bits of s
+ *            above those of 128 + z in bf16
+ * The rows of q_out, k_out and v_out are not quantized.
+ */
+rag_status rag_qkv_rope_write_kv4(
+    const void *q, const void *k, const void *v, int64_t q_stride,
+    int64_t k_stride, int64_t v_stride, void *q_out, void *k_out, void *v_out,
+    void *k_cache, void *v_cache, const int32_t *slot_mapping,
+    const int32_t *positions, const float *cos_sin, int32_t max_position,
+    int32_t rotary_dim, int32_t interleaved, const void *q_weight,
+    const void *k_weight, float eps, int32_t num_tokens, int32_t num_q_heads,
+    int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+    int32_t num_blocks, hipStream_t stream);
+
+/*
+ * The first keys of every sequence in a 4-bit paged cache, back as packed bf16 rows:
+ * with them rag_attn_prefill_varlen attends a chunked-prefill piece over keys that
+ * the cache already holds.
+ *
+ *   k_cache, v_cache  as in rag_qkv_rope_write_kv4
+ *   block_tables  device int32 [num_seqs, max_blocks_per_seq]
+ *   cu_seqlens_k  device int32 [num_seqs + 1], as in rag_attn_prefill_varlen: rows
+ *            [cu[s], cu[s+1]) get the first cu[s+1] - cu[s] keys of sequence s
+ *   k, v     device [num_rows, num_kv_heads, head_dim]; output: s (c - z) rounded to
+ *            bf16.  num_rows >= cu[num_seqs]; rows behind those stay as they are.
+ * Preconditions (checked when RAG_ATTN_CHECK=1): cu starts at 0 and does not decrease,
+ * keys inside the table, pages inside the pool.
+ *
+ * Returns RAG_OK (no rows, no sequences or a table of no pages is a no-op),
+ * RAG_ERR_INVALID_ARG, RAG_ERR_UNSUPPORTED (head_dim, block_size, sizes) or RAG_ERR_HIP.
+ */
+rag_status rag_kv4_read(const void *k_cache, const void *v_cache,
+                        const int32_t *block_tables,
+                        const int32_t *cu_seqlens_k, void *k, void *v,
+                        int32_t num_rows, int32_t num_seqs,
+                        int32_t max_blocks_per_seq, int32_t num_blocks,
+                        int32_t num_kv_heads, int32_t head_dim,
+                        int32_t block_size, hipStream_t stream);
+
+/*
+ * Bytes of workspace for rag_attn_decode_paged_kv4 calls of these sizes and of smaller
+ * ones (it does not depend on num_seqs and max_blocks_per_seq).  0 for invalid sizes.
+ * Library-internal layout: 4096 int32 arrival counters, fp32 log-sum-exps and fp32
+ * partial outputs of the workgroups.
+ */
+size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q,
+                                          int32_t num_q_heads,
+                                          int32_t num_kv_heads, int32_t head_dim,
+                                          int32_t max_blocks_per_seq,
+                                          int32_t block_size);
+
+/*
+ * Attention of the last rows of every sequence against a 4-bit paged cache: one decode
+ * step, or a chain of drafted tokens judged in one step (rag_draft_verify).  K and V of
+ * the rows are in the cache already (rag_qkv_rope_write_kv4).
+ *
+ *   q, o     device [Tq, num_q_heads, head_dim]; o is output, written in full
+ *   k_cache, v_cache  as in rag_qkv_rope_write_kv4
+ *   block_tables, num_blocks, block_size  as in rag_attn_decode_paged
+ *   kv_lens  device int32 [num_seqs]: keys of sequence s, counting those of its rows
+ *   cu_seqlens_q  device int32 [num_seqs + 1] or NULL.  NULL: one row a sequence
+ *            (Tq = num_seqs; a sequence without keys gives 0).  Otherwise sequence s has
+ *            n = cu[s+1] - cu[s] rows, 0 <= n <= max_seqlen_q and n <= kv_lens[s]: row i
+ *            sees its first kv_lens[s] - n + i + 1 keys.  What a row does not see never
+ *            reaches it, whatever it is.
+ *   max_seqlen_q  host upper bound of n.  Every 64 (row, q head) pairs of a kv head read
+ *            the sequence's keys again: for pieces of hundreds of rows rag_kv4_read and
+ *            rag_attn_prefill_varlen are faster.
+ *   workspace, workspace_bytes  device scratch of at least
+ *            rag_attn_decode_kv4_workspace_size(...) bytes for the same arguments or for
+ *            larger sizes; 256-byte aligned.  It must be zero-filled before its first
+ *            use; every completed call leaves its counters zero again, so that calls of
+ *            any sizes may follow each other in it.  Calls that may overlap, and graphs
+ *            that may be replayed at once, must not share it.
+ *
+ * Any num_q_heads / num_kv_heads.  Up to 1024 sequences are cut on the GPU from their
+ * lengths into even shares for the workgroups that it works on at a time; with more,
+ * none is cut.  Preconditions (checked when RAG_ATTN_CHECK=1): the above, keys inside
+ * the table, pages inside the pool.
+ *
+ * Returns RAG_OK (num_seqs == 0 or max_seqlen_q == 0 is a no-op), RAG_ERR_INVALID_ARG,
+ * RAG_ERR_UNSUPPORTED (head_dim, block_size, max_seqlen_q * num_q_heads from 2^24 on,
+ * sizes), RAG_ERR_WORKSPACE or RAG_ERR_HIP.
+ */
+rag_status rag_attn_decode_paged_kv4(
+    const void *q, const void *k_cache, const void *v_cache, void *o,
+    const int32_t *block_tables, const int32_t *kv_lens,
+    const int32_t *cu_seqlens_q, int32_t num_seqs, int32_t max_seqlen_q,
+    int32_t max_blocks_per_seq, int32_t num_blocks, int32_t num_q_heads,
+    int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+    float softmax_scale, void *workspace, size_t workspace_bytes,
+    hipStream_t stream);
+
+/*
+ * Bytes of workspace for rag_draft_verify calls of these sizes and of smaller ones; 0
+ * for sizes that it does not take.  Library-internal layout: 65,536 int32 arrival
+ * counters, then maxima and sums of parts of the rows.
+ */
+size_t rag_draft_verify_workspace_size(int32_t num_rows, int32_t num_seqs,
+                                       int32_t vocab);
+
+/*
+ * Verification of drafted tokens against the model's logits, from given random numbers:
+ * the step between the attention of the drafts and rag_kv_cache_keep.  Sequence s has
+ * n = cu[s+1] - cu[s] nodes; node 0 is the last token of its text (its K/V, like the
+ * drafts', is new in the cache), the others are drafted tokens behind their parents.
+ * The logits of node i judge what comes after it: p_i = softmax(logits_i / T), T the
+ * sequence's temperature.
+ *
+ *   without draft_probs (drafts chosen in any way, chains or trees)
+ *            At node i the token t_i is drawn from p_i with u_i: the first index whose
+ *            running sum of p_i exceeds u_i; with T = 0 it is the first index of the
+ *            largest logit.  From node 0 on, the child whose token is t_i is kept and
+ *            followed (of several the first); where there is none, t_i is the next token.
+ *   with draft_probs (chains whose token i was drawn from q_i)
+ *            Node i >= 1 is kept where u_i q_i(x_i) < p_{i-1}(x_i) (T = 0: where x_i is
+ *            the first index of the largest logit of i - 1), up to the first that is not.
+ *            Behind it the next token is drawn with u_0 from max(p_{i-1} - q_i, 0), or,
+ *            where all are kept, from the last node's p.
+ * Either way the text that results is distributed as the model's own.
+ *
+ *   logits   device [num_rows, vocab] bf16, or fp32 with logits_fp32 = 1; logits_stride
+ *            elements from row to row.  -inf masks a token, NaN counts as -inf.  A row
+ *            whose weights have no sum above 0 (all -inf, or +inf among them) gives the
+ *            first index of its maximum.
+ *   draft_probs  device fp32 [num_rows, vocab] or NULL, draft_stride elements from row to
+ *            row: row i is q_i, not looked at for node 0.
+ *   tokens   device int32 [num_rows]: x_i (node 0's is not looked at)
+ *   parents  device int32 [num_rows] or NULL (chains): the parent of node i >= 1 among
+ *            its sequence's nodes, below i.  NULL with draft_probs.
+ *   cu_seqlens_q  device int32 [num_seqs + 1]; cu[num_seqs] <= num_rows
+ *   temperature  device fp32 [num_seqs]; what is not above 0 counts as 0
+ *   uniforms  device fp32 [num_rows]: u_i in [0, 1)
+ *   kept     device int32 [num_seqs, max_kept]: the kept nodes, from node 0 on, as
+ *            rag_kv_cache_keep takes them; -1 behind the last.  Where max_kept nodes are
+ *            kept, the last of them counts as having no children.
+ *   num_kept, next_token  device int32 [num_seqs]: their number, and the token after
+ *            them; 0 and -1 for a sequence without nodes
+ *   workspace, workspace_bytes  device scratch of at least
+ *            rag_draft_verify_workspace_size(...) bytes; 256-byte aligned, zero-filled
+ *            before its first use; every completed call leaves its counters zero again, so
+ *            that calls of any sizes may follow each other in it.  Calls that may overlap,
+ *            and graphs that may be replayed at once, must not share it.
+ * The outputs and the workspace must not overlap anything else.  Exponentials and sums
+ * are fp64, so that a draw does not depend on their order.
+ * Preconditions (checked when RAG_ATTN_CHECK=1): cu starts at 0 and does not decrease;
+ * tokens of nodes i >= 1 in [0, vocab) (others are never kept); parents as above.
+ *
+ * Returns RAG_OK (num_seqs == 0 is a no-op), RAG_ERR_INVALID_ARG (null, misaligned or
+ * overlapping pointers, sizes, strides, max_kept 0), RAG_ERR_UNSUPPORTED (draft_probs with
+ * parents, more than 49,152 rows, 8,192 sequences or 2^28 tokens), RAG_ERR_WORKSPACE or
+ * RAG_ERR_HIP.
+ */
+rag_status rag_draft_verify(
+    const void *logits, int32_t logits_fp32, int64_t logits_stride,
+    const float *draft_probs, int64_t draft_stride, const int32_t *tokens,
+    const int32_t *parents, const int32_t *cu_seqlens_q,
+    const float *temperature, const float *uniforms, int32_t *kept,
+    int32_t *num_kept, int32_t *next_token, int32_t num_rows, int32_t num_seqs,
+    int32_t vocab, int32_t max_kept, void *workspace, size_t workspace_bytes,
+    hipStream_t stream);
+
+/*
  * Host-only prompt planner: the packed-batch descriptor of the LLM calls a
  * synthesis method issues for a list of queries.
  *

@@ -39,6 +39,7 @@ class RagError(RuntimeError):
 
 
 _i32 = ctypes.c_int32
+_i64 = ctypes.c_int64
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _vp = ctypes.c_void_p
 _lib = None
@@ -54,7 +55,9 @@ def exported_symbols():
             "rag_device_free_memory", "rag_awq_pack_weights", "rag_awq_workspace_size",
             "rag_awq_gemm", "rag_kv_pages_update", "rag_kv_cache_keep",
             "rag_attn_decode_tree_workspace_size", "rag_attn_decode_paged_tree",
-            "rag_attn_prefill_varlen_ranges"]
+            "rag_attn_prefill_varlen_ranges", "rag_qkv_rope_write", "rag_qkv_rope_write_kv4",
+            "rag_kv4_read", "rag_attn_decode_kv4_workspace_size", "rag_attn_decode_paged_kv4",
+            "rag_draft_verify_workspace_size", "rag_draft_verify"]
 
 
 class QueryProfile(ctypes.Structure):
@@ -148,6 +151,25 @@ def lib():
     L.rag_attn_prefill_varlen_ranges.restype = ctypes.c_int
     L.rag_attn_prefill_varlen_ranges.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32,
                                                  _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp]
+    for call in (L.rag_qkv_rope_write, L.rag_qkv_rope_write_kv4):
+        call.restype = ctypes.c_int
+        call.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                         _i32, _i32, _i32, _vp, _vp, ctypes.c_float, _i32, _i32, _i32, _i32, _i32,
+                         _i32, _vp]
+    L.rag_kv4_read.restype = ctypes.c_int
+    L.rag_kv4_read.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
+                               _i32, _vp]
+    L.rag_attn_decode_kv4_workspace_size.restype = ctypes.c_size_t
+    L.rag_attn_decode_kv4_workspace_size.argtypes = [_i32] * 7
+    L.rag_attn_decode_paged_kv4.restype = ctypes.c_int
+    L.rag_attn_decode_paged_kv4.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32,
+                                            _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp,
+                                            ctypes.c_size_t, _vp]
+    L.rag_draft_verify_workspace_size.restype = ctypes.c_size_t
+    L.rag_draft_verify_workspace_size.argtypes = [_i32, _i32, _i32]
+    L.rag_draft_verify.restype = ctypes.c_int
+    L.rag_draft_verify.argtypes = [_vp, _i32, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                   _vp, _i32, _i32, _i32, _i32, _vp, ctypes.c_size_t, _vp]
     L.rag_plan_prompts.restype = ctypes.c_int
     L.rag_plan_prompts.argtypes = [ctypes.c_int, _i32, _i32p, _i32p, _i32, _i32, _i32, _i32p,
                                    _i32, _i32p, _i32p]
@@ -360,16 +382,37 @@ def _load_marshal():
     _marshal = loaded
 
 
-_TYPES = {"i": torch.int32, "l": torch.int64, "b": torch.bfloat16, "f": torch.float32}
+_TYPES = {"i": torch.int32, "l": torch.int64, "u": torch.uint8, "b": torch.bfloat16,
+          "f": torch.float32, "r": torch.bfloat16, "g": torch.float32}
 
 
 def _refuse_at(i, spec, names, tensors):
     """Why tensor i was not taken."""
+    first = next(t for t in tensors if isinstance(t, torch.Tensor))
     if i == len(tensors):
-        raise ValueError(f"tensors on {tensors[0].device}, not on the current device")
-    t, name = tensors[i], names.split()[i]
-    _refuse(t, _TYPES[chr(spec[2 * i]).lower()], name, spec[2 * i + 1] - ord("0"))
-    raise ValueError(f"{name} is on {t.device}, not on {tensors[0].device}")
+        raise ValueError(f"tensors on {first.device}, not on the current device")
+    t, name, kind = tensors[i], names.split()[i], chr(spec[2 * i]).lower()
+    rank = spec[2 * i + 1] - ord("0")
+    if kind in "rgh" and isinstance(t, torch.Tensor):
+        if kind == "h" and t.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+        if t.dim() == rank and t.is_cuda and t.dtype == _TYPES.get(kind, t.dtype) and \
+                first.device == t.device:
+            raise ValueError(f"{name} must be contiguous but for the step from row to row, of at "
+                             f"least a row; its strides are {tuple(t.stride())}")
+        _refuse(t[:0].contiguous() if t.dim() else t, _TYPES.get(kind, t.dtype), name, rank)
+    else:
+        _refuse(t, _TYPES.get(kind, torch.bfloat16), name, rank)
+    raise ValueError(f"{name} is on {t.device}, not on {first.device}")
+
+
+def _scratch(workspace, dev):
+    """(address, bytes) of a call's workspace tensor, or of None."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _raw_stream(stream, dev):
@@ -479,6 +522,143 @@ def rag_attn_prefill_varlen_ranges(q, k, v, o, lse, cu_seqlens_q, cu_seqlens_k, 
     status = _lib.rag_attn_prefill_varlen_ranges(
         qp, kp, vp, op, lse_p, cu_q, cu_k, ranges, seqs1 - 1, int(max_seqlen_q), int(max_seqlen_k),
         hq, hkv, d, float(softmax_scale), _raw_stream(stream, dev))
+    if status:
+        _check(status)
+
+
+def _rope_write(call, cache, q, k, v, q_out, positions, cos_sin, slot_mapping, k_cache, v_cache, k_out,
+                v_out, q_weight, k_weight, eps, interleaved, stream):
+    """`cache`: the spec of the caches, of which None gives zeros throughout."""
+    t = (k, v, q, q_out, positions, cos_sin, slot_mapping, k_out, v_out, q_weight, k_weight, k_cache,
+         v_cache)
+    spec = b"r3r3R3B3I1F2I1B3B3B1B1" + cache
+    p = _pointers(spec, *t)
+    if p.__class__ is int:
+        _refuse_at(p, spec, "k v q q_out positions cos_sin slot_mapping k_out v_out q_weight k_weight "
+                   "k_cache v_cache", t)
+    dev, kp, T, hkv, d, ks, vp, T2, hkv2, d2, vs, qp, T3, hq, d3, qs, qo, T4, hq4, d4, pos, T5, angles, \
+        most, rot, slots, T6, ko, T7, h7, d7, vo, T8, h8, d8, qw, wq, kw, wk = p[:39]
+    half = len(p) + 39 >> 1
+    kc, *pages = p[39:half]
+    vc, *pages2 = p[half:]
+    blocks = pages[0]
+    want = [blocks, hkv, 16, d] if len(pages) == 4 else [blocks, hkv, 9 * d]
+    if (T2, hkv2, d2) != (T, hkv, d) or (q is not None and (T3, d3) != (T, d)) or \
+            (q_out is not None and (T4, hq4, d4) != (T3, hq, d3)) or \
+            (positions is not None and T5 != T) or (slot_mapping is not None and T6 != T) or \
+            (k_out is not None and (T7, h7, d7) != (T, hkv, d)) or \
+            (v_out is not None and (T8, h8, d8) != (T, hkv, d)) or \
+            (q_weight is not None and wq != d) or (k_weight is not None and wk != d) or \
+            (k_cache is not None and pages != want) or (v_cache is not None and pages2 != want):
+        raise ValueError("qkv rope write: inconsistent shapes")
+    status = getattr(_lib, call)(
+        qp or None, kp, vp, qs, ks, vs, qo or None, ko or None, vo or None, kc or None, vc or None,
+        slots or None, pos or None, angles or None, most, rot, 1 if interleaved else 0, qw or None,
+        kw or None, float(eps), T, hq, hkv, d, 16, blocks, _raw_stream(stream, dev))
+    if status:
+        _check(status)
+
+
+def rag_qkv_rope_write(q, k, v, q_out, positions, cos_sin, slot_mapping=None, k_cache=None,
+                       v_cache=None, k_out=None, v_out=None, q_weight=None, k_weight=None, eps=1e-6,
+                       interleaved=False, stream=None) -> None:
+    """Norm of each head of Q and K, rotation, and the paged cache's write.  q
+    [T, Hq, d] and k, v [T, Hkv, d] bf16, contiguous but for the step from token to
+    token; q_out [T, Hq, d] (q and q_out None: K and V alone); positions int32 [T] and
+    cos_sin fp32 [max_position, rotary_dim], or None (no rotation); slot_mapping int32
+    [T] (negative = padding) and caches [num_blocks, Hkv, 16, d] bf16, or None; k_out,
+    v_out [T, Hkv, d] or None; q_weight, k_weight bf16 [d] or None (no norm)."""
+    _rope_write("rag_qkv_rope_write", b"B4B4", q, k, v, q_out, positions, cos_sin, slot_mapping,
+                k_cache, v_cache, k_out, v_out, q_weight, k_weight, eps, interleaved, stream)
+
+
+def rag_qkv_rope_write_kv4(q, k, v, q_out, positions, cos_sin, slot_mapping, k_cache, v_cache,
+                           k_out=None, v_out=None, q_weight=None, k_weight=None, eps=1e-6,
+                           interleaved=False, stream=None) -> None:
+    """rag_qkv_rope_write into a 4-bit paged cache: k_cache, v_cache uint8
+    [num_blocks, Hkv, 9 * d], slot_mapping int32 [T]."""
+    _rope_write("rag_qkv_rope_write_kv4", b"U3U3", q, k, v, q_out, positions, cos_sin, slot_mapping,
+                k_cache, v_cache, k_out, v_out, q_weight, k_weight, eps, interleaved, stream)
+
+
+def rag_kv4_read(k_cache, v_cache, block_tables, cu_seqlens_k, k, v, stream=None) -> None:
+    """The first cu_seqlens_k[s+1] - cu_seqlens_k[s] keys of every sequence of a 4-bit
+    cache (uint8 [num_blocks, Hkv, 9 * d]) as bf16 rows: k, v [T, Hkv, d] outputs (rows
+    behind cu_seqlens_k[S] stay); block_tables int32 [S, max_blocks]; cu_seqlens_k
+    int32 [S+1]."""
+    t = (k_cache, v_cache, block_tables, cu_seqlens_k, k, v)
+    p = _pointers(b"u3u3i2i1b3b3", *t)
+    if p.__class__ is int:
+        _refuse_at(p, b"u3u3i2i1b3b3", "k_cache v_cache block_tables cu_seqlens_k k v", t)
+    dev, kc, blocks, hkv, page, vc, b2, h2, p2, table, S, width, cu, seqs1, kp, T, hkv3, d, vp, T2, hkv4, \
+        d2 = p
+    if (b2, h2, p2) != (blocks, hkv, page) or (T2, hkv4, d2) != (T, hkv3, d) or hkv3 != hkv or \
+            page != 9 * d or S != seqs1 - 1:
+        raise ValueError("kv4 read: inconsistent shapes")
+    status = _lib.rag_kv4_read(kc, vc, table, cu, kp, vp, T, S, width, blocks, hkv, d, 16,
+                               _raw_stream(stream, dev))
+    if status:
+        _check(status)
+
+
+def rag_attn_decode_kv4_workspace_size(num_seqs, max_seqlen_q, num_q_heads, num_kv_heads, head_dim,
+                                       max_blocks_per_seq, block_size=16) -> int:
+    return lib().rag_attn_decode_kv4_workspace_size(num_seqs, max_seqlen_q, num_q_heads, num_kv_heads,
+                                                    head_dim, max_blocks_per_seq, block_size)
+
+
+def rag_attn_decode_paged_kv4(q, k_cache, v_cache, o, block_tables, kv_lens, softmax_scale,
+                              cu_seqlens_q=None, max_seqlen_q=1, workspace=None, stream=None) -> None:
+    """q, o [Tq, Hq, d] bf16; caches uint8 [num_blocks, Hkv, 9 * d]; block_tables int32
+    [S, max_blocks]; kv_lens int32 [S], the rows counted; cu_seqlens_q int32 [S+1]
+    offsets of the sequences' last rows, or None: one row each; workspace a GPU tensor of
+    rag_attn_decode_kv4_workspace_size bytes, zero-filled once before its first use."""
+    t = (q, o, k_cache, v_cache, block_tables, kv_lens, cu_seqlens_q)
+    p = _pointers(b"b3b3u3u3i2i1I1", *t)
+    if p.__class__ is int:
+        _refuse_at(p, b"b3b3u3u3i2i1I1", "q o k_cache v_cache block_tables kv_lens cu_seqlens_q", t)
+    dev, qp, rows, hq, d, op, rows2, hq2, d2, kc, blocks, hkv, page, vc, b2, h2, p2, table, S, width, kv, \
+        seqs, cu, seqs1 = p
+    if (rows2, hq2, d2) != (rows, hq, d) or (b2, h2, p2) != (blocks, hkv, page) or page != 9 * d or \
+            S != seqs or (rows if cu_seqlens_q is None else seqs1 - 1) != S:
+        raise ValueError("decode kv4: inconsistent shapes")
+    ws_ptr, ws_bytes = _scratch(workspace, dev)
+    if rows == 0:
+        return
+    status = _lib.rag_attn_decode_paged_kv4(
+        qp, kc, vc, op, table, kv, cu or None, S, int(max_seqlen_q), width, blocks, hq, hkv, d, 16,
+        float(softmax_scale), ws_ptr, ws_bytes, _raw_stream(stream, dev))
+    if status:
+        _check(status)
+
+
+def rag_draft_verify_workspace_size(num_rows, num_seqs, vocab) -> int:
+    return lib().rag_draft_verify_workspace_size(num_rows, num_seqs, vocab)
+
+
+def rag_draft_verify(logits, tokens, cu_seqlens_q, temperature, uniforms, kept, num_kept, next_token,
+                     parents=None, draft_probs=None, workspace=None, stream=None) -> None:
+    """logits [Tq, V] bf16 or fp32 and draft_probs fp32 [Tq, V] or None, contiguous but
+    for the step from row to row; tokens int32 [Tq]; parents int32 [Tq] or None (chains);
+    cu_seqlens_q int32 [S+1]; temperature fp32 [S]; uniforms fp32 [Tq]; kept int32
+    [S, max_kept], num_kept and next_token int32 [S] outputs; workspace a GPU tensor of
+    rag_draft_verify_workspace_size bytes, zero-filled once before its first use."""
+    t = (logits, tokens, cu_seqlens_q, temperature, uniforms, kept, num_kept, next_token, parents,
+         draft_probs)
+    p = _pointers(b"h2i1i1f1f1i2i1i1I1G2", *t)
+    if p.__class__ is int:
+        _refuse_at(p, b"h2i1i1f1f1i2i1i1I1G2", "logits tokens cu_seqlens_q temperature uniforms kept "
+                   "num_kept next_token parents draft_probs", t)
+    dev, lp, rows, vocab, step, wide, tok, rows2, cu, seqs1, heat, S, u, rows3, ke, S2, most, nk, S3, nt, S4, \
+        par, rows4, draft, rows5, vocab2, dstep = p
+    if not rows == rows2 == rows3 or not S == S2 == S3 == S4 == seqs1 - 1 or \
+            (parents is not None and rows4 != rows) or \
+            (draft_probs is not None and (rows5, vocab2) != (rows, vocab)):
+        raise ValueError("draft verify: inconsistent shapes")
+    ws_ptr, ws_bytes = _scratch(workspace, dev)
+    status = _lib.rag_draft_verify(
+        lp, wide, step, draft or None, dstep, tok, par or None, cu, heat, u, ke, nk, nt, rows, S, vocab,
+        most, ws_ptr, ws_bytes, _raw_stream(stream, dev))
     if status:
         _check(status)
 

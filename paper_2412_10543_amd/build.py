@@ -28,10 +28,11 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE,
 # them without AGPR copies.
 SOURCE_FLAGS = {"awq_gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 SOURCES = ["kernels.hip", "kv_cache.hip", "awq_gemm.hip", "decode_scratch.hip", "tree_decode.hip",
-           "ranges_prefill.hip", "kv_pages.hip", "api.cpp", "awq_api.cpp", "draft_api.cpp",
+           "ranges_prefill.hip", "kv_pages.hip", "rope_write.hip", "kv4_read.hip", "kv4_decode.hip",
+           "draft_verify.hip", "api.cpp", "awq_api.cpp", "draft_api.cpp", "serve_api.cpp",
            "planner.cpp"]
 HEADERS = ["common.h", "prefill_tile.h", "decode_unit.h", "launch.h", "errors.h", "awq.h",
-           "checks.h", "draft.h", "masked_tile.h"]
+           "checks.h", "draft.h", "masked_tile.h", "kv4.h", "serve.h"]
 
 
 PROBES = os.path.join(PKG, "libceiling_probes.so")

@@ -1,0 +1,219 @@
+// Between the projection of a batch of new tokens and their attention (gfx950):
+// the RMS norm of each head of Q and K, the rotation of both by the tokens'
+// positions, and the K and V rows' way into the paged cache, in bf16 or in 4 bits,
+// in one pass over the projection's output.
+//
+//   norm      y = x w / sqrt(mean(x^2) + eps), over the D channels of a head
+//   rotation  (a, b) -> (a cos - b sin, b cos + a sin) for the pairs of channels
+//             (i, i + R/2), or (2 i, 2 i + 1); channels from R on stay
+// Both in fp32, rounded once, to bf16; 4-bit codes (kv4.h) are made of the rounded
+// values, so that they are those of a bf16 cache.
+//
+// HBM-bound.  A wave holds 64 / (D/8) head rows at a time, 16 bytes a lane, and
+// walks over the heads of one token with its angles in registers.
+#include "common.h"
+#include "kv4.h"
+#include "serve.h"
+
+namespace rag {
+
+namespace {
+
+constexpr int kRpWaves = 4;
+
+__device__ __forceinline__ void unpack8(u32x4 x, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(x[i] << 16);
+    f[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+  }
+}
+
+template <int D>
+__device__ __forceinline__ u32x4 row_shuffle(u32x4 x, int lane) {
+  u32x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = __shfl(x[i], lane, kWave);
+  return y;
+}
+
+// Sum over the D/8 lanes of a row.
+template <int D>
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+  for (int m = D / 16; m >= 1; m >>= 1) x += wave_xor(x, m);
+  return x;
+}
+
+// Minimum over the 8 lanes of a group of 64 channels.
+__device__ __forceinline__ float group_min(float x) {
+#pragma unroll
+  for (int m = 4; m >= 1; m >>= 1) x = fminf(x, wave_xor(x, m));
+  return x;
+}
+
+// The lane's eight channels (chunk j of the row) of a token's K or V row, to its page.
+template <int D>
+__device__ __forceinline__ void store_kv4(u32x4 x, bool key, char* page, int token, int j) {
+  using P = Kv4Page<D>;
+  float f[8];
+  unpack8(x, f);
+  float lo = 0.f, hi = 0.f;
+  bool finite = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo = fminf(lo, f[i]);
+    hi = fminf(hi, -f[i]);
+    finite &= fabsf(f[i]) < INFINITY;
+  }
+  lo = group_min(lo);
+  hi = -group_min(hi);
+  finite = group_min(finite ? 1.f : 0.f) > 0.f;
+  const Kv4Scale sc(lo, hi, finite);
+  uint32_t c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = sc.code(f[i]);
+  if (key) {
+    const uint32_t even = c[0] | c[2] << 4 | c[4] << 8 | c[6] << 12;
+    const uint32_t odd = c[1] | c[3] << 4 | c[5] << 8 | c[7] << 12;
+    *reinterpret_cast<uint32_t*>(page + P::k_word(token, j)) = even | odd << 16;
+  } else {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      *reinterpret_cast<uint16_t*>(page + P::v_unit(token, 2 * (j % 8) + u, j / 8)) =
+          (uint16_t)(c[4 * u] | c[4 * u + 1] << 4 | c[4 * u + 2] << 8 | c[4 * u + 3] << 12);
+  }
+  if (j % 8 == 0) *reinterpret_cast<uint32_t*>(page + P::param(token, j / 8)) = sc.param();
+}
+
+// Workgroup: kRpWaves waves, each a token (x) and a share of its head rows (y).
+template <int D, bool kKv4>
+__global__ __launch_bounds__(64 * kRpWaves) void rope_kernel(RopeArgs a) {
+  constexpr int kLanes = D / 8, kRows = kWave / kLanes;
+  const int lane = threadIdx.x & 63, j = lane % kLanes;
+  const int64_t t = (int64_t)blockIdx.x * kRpWaves + wave_id();
+  if (t >= a.num_tokens) return;
+  const int slot = a.slots != nullptr ? a.slots[t] : 0;
+  if (slot < 0) return;                              // padding token
+  const int rows = (a.q != nullptr ? a.hq : 0) + 2 * a.hkv, q_rows = rows - 2 * a.hkv;
+
+  // the pair's other channel is in chunk `other`; angles of the lane's eight channels
+  const int half = a.rot / 16;                       // chunks of R/2 channels
+  const bool turned = a.positions != nullptr && j < a.rot / 8;
+  int other = j;
+  float c[8], s[8];
+  if (turned) {
+    // (a position outside the table is a broken precondition; it reads the last row)
+    const int pos = (int)min((uint32_t)a.positions[t], (uint32_t)(a.max_position - 1));
+    const float* row = a.cos_sin + (size_t)pos * a.rot;
+    if (a.interleaved) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        c[i] = row[4 * j + i / 2];
+        s[i] = row[a.rot / 2 + 4 * j + i / 2] * (i % 2 ? 1.f : -1.f);
+      }
+    } else {
+      other = j < half ? j + half : j - half;
+      const float* p = row + 8 * (j < half ? j : other);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        c[i] = p[i];
+        s[i] = p[a.rot / 2 + i] * (j < half ? -1.f : 1.f);
+      }
+    }
+  }
+
+  const int steps = (rows + kRows - 1) / kRows;
+  for (int it = blockIdx.y; it < steps; it += gridDim.y) {
+    const int r = it * kRows + lane / kLanes;
+    const bool is_q = r < q_rows, is_k = !is_q && r < q_rows + a.hkv;
+    const int h = is_q ? r : is_k ? r - q_rows : r - q_rows - a.hkv;
+    const bool has = r < rows;
+    const bf16_t* src = is_q   ? (const bf16_t*)a.q + t * a.q_stride
+                        : is_k ? (const bf16_t*)a.k + t * a.k_stride
+                               : (const bf16_t*)a.v + t * a.v_stride;
+    u32x4 x = {0, 0, 0, 0};
+    if (has) x = load16(src + (size_t)h * D + j * 8);
+    const u32x4 y = row_shuffle<D>(x, lane - j + other);
+    const bf16_t* w = (const bf16_t*)(is_q ? a.q_weight : is_k ? a.k_weight : nullptr);
+    float f[8], g[8];
+    unpack8(x, f);
+    unpack8(y, g);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
+    sum = row_sum<D>(sum);
+    if (w != nullptr) {
+      const float n = 1.f / sqrtf(sum * (1.f / D) + a.eps);
+      float wf[8], wg[8];
+      unpack8(load16(w + j * 8), wf);
+      unpack8(load16(w + other * 8), wg);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        f[i] = f[i] * n * wf[i];
+        g[i] = g[i] * n * wg[i];
+      }
+    }
+    if (turned && (is_q || is_k)) {
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = fmaf(f[i], c[i], (a.interleaved ? f[i ^ 1] : g[i]) * s[i]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = o[i];
+    }
+    if (w != nullptr || (turned && (is_q || is_k)))   // (others are copied bit by bit)
+      x = as_u32x4(to_bf16x8(f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]));
+    if (is_q && has) {
+      *reinterpret_cast<u32x4*>((bf16_t*)a.q_out + ((size_t)t * a.hq + h) * D + j * 8) = x;
+    }
+    if (!is_q && has) {
+      bf16_t* out = (bf16_t*)(is_k ? a.k_out : a.v_out);
+      if (out != nullptr)
+        *reinterpret_cast<u32x4*>(out + ((size_t)t * a.hkv + h) * D + j * 8) = x;
+    }
+    if (a.slots == nullptr) continue;
+    char* cache = (char*)(is_k ? a.k_cache : a.v_cache);
+    const size_t page = (size_t)(slot >> 4) * a.hkv + h;
+    if constexpr (kKv4) {
+      // (the 8 lanes of a group stand in one row: they take this together)
+      if (has && !is_q)
+        store_kv4<D>(x, is_k, cache + page * Kv4Page<D>::kBytes, slot & 15, j);
+    } else if (has && !is_q) {
+      *reinterpret_cast<u32x4*>((bf16_t*)cache + (page * 16 + (slot & 15)) * D + j * 8) = x;
+    }
+  }
+}
+
+int rope_steps(const RopeArgs& a) {
+  const int rows = (a.q != nullptr ? a.hq : 0) + 2 * a.hkv, per = kWave / (a.d / 8);
+  return (rows + per - 1) / per;
+}
+
+dim3 rope_dim(const RopeArgs& a) {
+  const unsigned x = (unsigned)((a.num_tokens + (int64_t)kRpWaves - 1) / kRpWaves);
+  const int steps = rope_steps(a);
+  int y = 1;
+  while (y < steps && (int64_t)x * y < 1024) ++y;
+  return dim3(x, (unsigned)std::min(y, 65535));
+}
+
+}  // namespace
+
+int64_t rope_grid(const RopeArgs& a) {
+  const dim3 g = rope_dim(a);
+  return (int64_t)g.x * g.y;
+}
+
+hipError_t launch_rope(const RopeArgs& a, bool kv4, hipStream_t stream) {
+  const dim3 grid = rope_dim(a), block(64 * kRpWaves);
+  if (grid.x == 0) return hipSuccess;
+  if (a.d == 64)
+    kv4 ? rope_kernel<64, true><<<grid, block, 0, stream>>>(a)
+        : rope_kernel<64, false><<<grid, block, 0, stream>>>(a);
+  else
+    kv4 ? rope_kernel<128, true><<<grid, block, 0, stream>>>(a)
+        : rope_kernel<128, false><<<grid, block, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace rag
