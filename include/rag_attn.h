@@ -684,7 +684,7 @@ rag_status rag_attn_decode_paged_kv4(
 
 /*
  * Bytes of workspace for rag_draft_verify calls of these sizes and of smaller ones; 0
- * for sizes that it does not take.  Library-internal layout: 65,536 int32 arrival
+ * for sizes that it does not take.  Library-internal layout: 32,768 int32 arrival
  * counters, then maxima and sums of parts of the rows.
  */
 size_t rag_draft_verify_workspace_size(int32_t num_rows, int32_t num_seqs,
@@ -739,7 +739,7 @@ size_t rag_draft_verify_workspace_size(int32_t num_rows, int32_t num_seqs,
  *
  * Returns RAG_OK (num_seqs == 0 is a no-op), RAG_ERR_INVALID_ARG (null, misaligned or
  * overlapping pointers, sizes, strides, max_kept 0), RAG_ERR_UNSUPPORTED (draft_probs with
- * parents, more than 49,152 rows, 8,192 sequences or 2^28 tokens), RAG_ERR_WORKSPACE or
+ * parents, more than 2^20 rows, 16,384 sequences or 2^28 tokens), RAG_ERR_WORKSPACE or
  * RAG_ERR_HIP.
  */
 rag_status rag_draft_verify(

@@ -11,146 +11,156 @@
 //
 // A draw by running sums turns on the sum of everything before the drawn token: with
 // 128,000 likely tokens, sums in fp32 would move one draw in ten.  Exponentials and sums
-// are therefore fp64 (the vector units' rate for it is that of fp32), and the exponential
-// is its power series, 2^x = 2^n sum (x - n)^k ln2^k / k!, |x - n| <= 1/2, to k = 11
-// (2^-47 relative).
+// are therefore fp64 (the vector units' rate for it is that of fp32).
 //
-// HBM-bound by the logits, which are read once: a workgroup takes kVChunk of a row and
-// leaves its maximum and sum; the last workgroup of a row to finish places the draw in a
-// chunk and reads that chunk again; the last row of a sequence walks.  With the
-// drafter's probabilities a second launch sums max(p - q, 0) for the one row a sequence.
+// First launch: a wave takes a segment of a row into its registers and leaves its maximum and
+// sum; the logits are read once.  Second launch, without the drafter's probabilities: a wave for
+// each row places the draw in a segment and reads that again; the last row of a sequence to finish
+// walks.  With them: workgroups for the one row a sequence whose next token is drawn find it
+// from the segments' sums, sum max(p - q, 0) in segments, and the last one draws.
 #include "common.h"
 #include "serve.h"
 
 #include <climits>
-#include <algorithm>
 
 namespace rag {
 
 namespace {
 
-constexpr int kVThreads = 256, kVWaves = kVThreads / kWave;
-constexpr int kVPer = 16;                       // logits of a thread
-constexpr int kVChunk = kVThreads * kVPer;
-constexpr int kVCounters = kVerifyMaxRows + 2 * kVerifyMaxSeqs;
+constexpr int kVWaves = 4, kVThreads = kVWaves * kWave;
+constexpr int kVStep = kWave * 8;               // logits of a wave's load
+constexpr int kVCounters = 2 * kVerifyMaxSeqs;
+constexpr int kVWalk = 1024;                    // nodes whose walk is in LDS
 
-// A chunk's maximum, sum of exp((x - maximum) / T) and first index of the maximum.
+// A segment's maximum and sum of exp((x - maximum) / T): kV loads of a wave.
 struct VStat {
   double sum;
   float top;
-  int arg;
-};
-// A row's.
-struct VRow {
-  double total;                 // sum of exp((x - top) / T)
-  float top;
-  int token;                    // drawn, or the first of the largest; with drafts: the latter
-  int accept;                   // with drafts: whether the next node is accepted
-  int pad;
+  int arg;                      // T = 0: the first index of the maximum
 };
 
 struct VWs {
-  int* rows;                    // [kVerifyMaxRows] arrivals
-  int* seqs;                    // [2][kVerifyMaxSeqs]
-  VStat* stats;                 // [num_rows][chunks]
-  VRow* row;                    // [num_rows]
-  double* rest;                 // [num_seqs][chunks]
+  int* seqs;                    // [2][kVerifyMaxSeqs] arrivals
+  VStat* stats;                 // [num_rows][segments]
+  int* drawn;                   // [num_rows]
+  double* rest;                 // [num_seqs][segments]
 };
 
-__host__ __device__ __forceinline__ int verify_chunks(int vocab) {
-  return (int)(((int64_t)vocab + kVChunk - 1) / kVChunk);
+// Segments of a row, of kV loads each.
+__host__ __device__ __forceinline__ int verify_segments(int vocab, int kv) {
+  return (int)(((int64_t)vocab + kv * kVStep - 1) / (kv * kVStep));
 }
 
 __host__ __device__ __forceinline__ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// (Sized for the shortest segments: calls of fewer rows have shorter ones.)
 __host__ __device__ __forceinline__ VWs verify_ws(char* base, int num_rows, int vocab) {
   VWs w;
-  const size_t chunks = (size_t)verify_chunks(vocab);
-  w.rows = reinterpret_cast<int*>(base);
-  w.seqs = w.rows + kVerifyMaxRows;
+  const size_t segs = (size_t)verify_segments(vocab, 1);
+  w.seqs = reinterpret_cast<int*>(base);
   base += up256(kVCounters * sizeof(int));
   w.stats = reinterpret_cast<VStat*>(base);
-  base += up256(num_rows * chunks * sizeof(VStat));
-  w.row = reinterpret_cast<VRow*>(base);
-  base += up256(num_rows * sizeof(VRow));
+  base += up256(num_rows * segs * sizeof(VStat));
+  w.drawn = reinterpret_cast<int*>(base);
+  base += up256(num_rows * sizeof(int));
   w.rest = reinterpret_cast<double*>(base);
   return w;
 }
 
-// ---- values that another XCD reads -------------------------------------------------
-template <class T>
-__device__ __forceinline__ void put(T* p, const T& v) {
-  static_assert(sizeof(T) % 8 == 0, "8-byte pieces");
-  uint64_t x[sizeof(T) / 8];
-  __builtin_memcpy(x, &v, sizeof(T));
+// exp((x - top) / T) for x <= top; what lies under 2^-1000 counts as 0, as NaN does, and where
+// top is infinite everything does.
+//   2^t = 2^n p(t - n), n the nearest whole number (from the low bits of t + 1.5 2^52), p(f) =
+//   1 + f r(f), r of degree 8 through (2^f - 1) / f at the Chebyshev nodes of [-1/2, 1/2]:
+//   2^-44 relative, and 1 at 0 (so that equal logits have equal sums).
+struct Heat {
+  double k, top;                // log2(e) / T
+  float cut;
+  __device__ __forceinline__ Heat(float top_, double k_) : k(k_), top(top_) {
+    const double low = top - 1000.0 / k;
+    cut = !(fabsf(top_) < INFINITY) ? INFINITY : low > -3.4028234663852886e38 ? (float)low : -3.4028234663852886e38f;
+  }
+  // Of N logits, step by step side by side (one's steps wait for each other).  kExact: 0 is 0
+  // (otherwise it may be as much as 2^-1022, which no sum notices).
+  template <bool kExact, int N>
+  __device__ __forceinline__ void weights(const float (&x)[N], double (&w)[N]) const {
+    constexpr double kRound = 6755399441055744.0;
+    constexpr double kP[10] = {1.0, 0.6931471805599453, 0.2402265069581299, 0.05550410866476082,
+                               0.009618129159402558, 0.0013333558178986627, 0.00015403455852453838,
+                               1.5252686876393043e-05, 1.3255224878668817e-06, 1.0203115707778471e-07};
+    double f[N], p[N];
+    uint32_t n[N];
 #pragma unroll
-  for (size_t i = 0; i < sizeof(T) / 8; ++i)
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(p) + i, x[i], __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-}
-template <class T>
-__device__ __forceinline__ T get(const T* p) {
-  uint64_t x[sizeof(T) / 8];
+    for (int i = 0; i < N; ++i) {
+      const double d = (double)x[i] - top;
+      const double m = __builtin_fma(d, k, kRound);
+      f[i] = __builtin_fma(d, k, kRound - m);
+      n[i] = (uint32_t)__builtin_bit_cast(uint64_t, m);
+      p[i] = kP[9];
+    }
 #pragma unroll
-  for (size_t i = 0; i < sizeof(T) / 8; ++i)
-    x[i] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p) + i, __ATOMIC_RELAXED,
-                             __HIP_MEMORY_SCOPE_AGENT);
-  T v;
-  __builtin_memcpy(&v, x, sizeof(T));
-  return v;
-}
-
-// 2^x for x <= 0 (and rounding above it); below -1100, and for NaN, 0.
-__device__ __forceinline__ double exp2_f64(double x) {
-  x = __builtin_fmax(x, -1100.0);
-  const double n = __builtin_rint(x), f = x - n;
-  constexpr double kL = 0.69314718055994530942;
-  double r = 1.0;
-  constexpr double c1 = kL, c2 = c1 * kL / 2, c3 = c2 * kL / 3, c4 = c3 * kL / 4, c5 = c4 * kL / 5,
-                   c6 = c5 * kL / 6, c7 = c6 * kL / 7, c8 = c7 * kL / 8, c9 = c8 * kL / 9,
-                   c10 = c9 * kL / 10, c11 = c10 * kL / 11;
-  r = __builtin_fma(c11, f, c10);
-  r = __builtin_fma(r, f, c9);
-  r = __builtin_fma(r, f, c8);
-  r = __builtin_fma(r, f, c7);
-  r = __builtin_fma(r, f, c6);
-  r = __builtin_fma(r, f, c5);
-  r = __builtin_fma(r, f, c4);
-  r = __builtin_fma(r, f, c3);
-  r = __builtin_fma(r, f, c2);
-  r = __builtin_fma(r, f, c1);
-  r = __builtin_fma(r, f, 1.0);
-  return __builtin_ldexp(r, (int)n);
-}
-
-// exp((x - top) / T), k = log2(e) / T; NaN and what lies at or below -inf count 0.
-__device__ __forceinline__ double weight(float x, float top, double k) {
-  return exp2_f64(((double)x - (double)top) * k);
-}
+    for (int j = 8; j >= 0; --j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = __builtin_fma(p[i], f[i], kP[j]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const u32x2 b = __builtin_bit_cast(u32x2, p[i]);
+      const bool some = x[i] >= cut;
+      const u32x2 r = {kExact && !some ? 0u : b[0], some ? b[1] + (n[i] << 20) : 0u};
+      w[i] = __builtin_bit_cast(double, r);
+    }
+  }
+  __device__ __forceinline__ double weight(float x) const {
+    const float one[1] = {x};
+    double w[1];
+    weights<true>(one, w);
+    return w[0];
+  }
+};
 
 // Eight logits of a row from element e on; -inf behind its end.  Rows may start at any
 // element: the loads are of 16 bytes at any even address.
 struct __attribute__((packed, aligned(2))) Any16 { u32x4 v; };
 struct __attribute__((packed, aligned(4))) Any16f { f32x4 v; };
 
+// Eight logits as they lie in memory.
+template <bool kWide>
+struct Raw8;
+template <>
+struct Raw8<false> {
+  u32x4 a;
+  __device__ __forceinline__ void load(const void* row, int e) {
+    a = reinterpret_cast<const Any16*>((const bf16_t*)row + e)->v;
+  }
+  __device__ __forceinline__ void unpack(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(a[i] << 16);
+      x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Raw8<true> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const void* row, int e) {
+    a = reinterpret_cast<const Any16f*>((const float*)row + e)->v;
+    b = reinterpret_cast<const Any16f*>((const float*)row + e + 4)->v;
+  }
+  __device__ __forceinline__ void unpack(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = a[i];
+      x[4 + i] = b[i];
+    }
+  }
+};
+
 template <bool kWide>
 __device__ __forceinline__ void load8(const void* row, int e, int vocab, float (&x)[8]) {
   if (e + 8 <= vocab) {
-    if constexpr (kWide) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const f32x4 y = reinterpret_cast<const Any16f*>((const float*)row + e + 4 * i)->v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j];
-      }
-    } else {
-      const u32x4 y = reinterpret_cast<const Any16*>((const bf16_t*)row + e)->v;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(y[i] << 16);
-        x[2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
-      }
-    }
+    Raw8<kWide> r;
+    r.load(row, e);
+    r.unpack(x);
     return;
   }
 #pragma unroll
@@ -162,380 +172,505 @@ __device__ __forceinline__ void load8(const void* row, int e, int vocab, float (
   }
 }
 
+// A lane's share of a segment, kV loads from element e on, kVStep apart; `whole`: the wave's
+// lie in the row (all are requested before the first is waited for).
+template <bool kWide, int kV>
+__device__ __forceinline__ void load_segment(const void* row, int e, int vocab, bool whole,
+                                             float (&x)[kV][8]) {
+  if (whole) {
+    Raw8<kWide> r[kV];
+#pragma unroll
+    for (int v = 0; v < kV; ++v) r[v].load(row, e + v * kVStep);
+#pragma unroll
+    for (int v = 0; v < kV; ++v) r[v].unpack(x[v]);
+  } else {
+#pragma unroll
+    for (int v = 0; v < kV; ++v) load8<kWide>(row, e + v * kVStep, vocab, x[v]);
+  }
+}
+
 template <bool kWide>
 __device__ __forceinline__ const void* logits_row(const VerifyArgs& a, int row) {
   return (const char*)a.logits + (size_t)row * a.logits_stride * (kWide ? 4 : 2);
 }
 
-// ---- sums and minima over the workgroup -----------------------------------------------
-struct VLds {
-  double d[kVWaves];
-  float f[kVWaves];
-  int i[kVWaves];
-  int at, flag;
-};
-
-__device__ __forceinline__ double block_sum(VLds& lds, double x) {
+// ---- over the wave ----------------------------------------------------------------------
+__device__ __forceinline__ double wave_sum(double x) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, kWave);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds.d[threadIdx.x >> 6] = x;
-  __syncthreads();
-  double s = 0;
-#pragma unroll
-  for (int w = 0; w < kVWaves; ++w) s += lds.d[w];
-  return s;
+  return x;
 }
-// Sum of the threads before this one, and of all.
-__device__ __forceinline__ double block_before(VLds& lds, double x, double& total) {
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x = fmaxf(x, wave_xor(x, m));
+  return x;
+}
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x = min(x, __shfl_xor(x, m, kWave));
+  return x;
+}
+// Sum of the lanes before this one, and of all.
+__device__ __forceinline__ double wave_before(double x, double& total) {
   double y = x;
 #pragma unroll
   for (int m = 1; m < kWave; m <<= 1) {
     const double z = __shfl_up(y, m, kWave);
     if ((int)(threadIdx.x & 63) >= m) y += z;
   }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) lds.d[threadIdx.x >> 6] = y;
-  __syncthreads();
-  double before = y - x;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kVWaves; ++w) {
-    if (w < (int)(threadIdx.x >> 6)) before += lds.d[w];
-    total += lds.d[w];
-  }
-  return before;
-}
-__device__ __forceinline__ float block_max(VLds& lds, float x) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x = fmaxf(x, wave_xor(x, m));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds.f[threadIdx.x >> 6] = x;
-  __syncthreads();
-  float s = lds.f[0];
-#pragma unroll
-  for (int w = 1; w < kVWaves; ++w) s = fmaxf(s, lds.f[w]);
-  return s;
-}
-__device__ __forceinline__ int block_min(VLds& lds, int x) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x = min(x, __shfl_xor(x, m, kWave));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds.i[threadIdx.x >> 6] = x;
-  __syncthreads();
-  int s = lds.i[0];
-#pragma unroll
-  for (int w = 1; w < kVWaves; ++w) s = min(s, lds.i[w]);
-  return s;
+  total = __shfl(y, kWave - 1, kWave);
+  return y - x;
 }
 
-// Counts one arrival of the workgroup, whose stores (put) have gone out before; true for
-// the last of n, for which the counter is cleared.
-__device__ __forceinline__ bool last_to_arrive(VLds& lds, int* counter, int n) {
+// Counts one arrival of the workgroup at a counter, its coherent stores before it; true for the
+// last of n, for which the counter is cleared.
+__device__ __forceinline__ bool last_to_arrive(int& flag, int* counter, int n) {
   wait_all_memory();
   __syncthreads();
   if (threadIdx.x == 0) {
-    lds.flag = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (lds.flag == n - 1)
-      __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    flag = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (flag == n - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  return lds.flag == n - 1;
+  return flag == n - 1;
 }
 
 // The sequence that owns row `row` (cu does not decrease and starts at 0): the number of
 // entries cu[1 .. num_seqs - 1] at or below it.
-__device__ __forceinline__ int sequence_of(VLds& lds, const VerifyArgs& a, int row) {
+__device__ __forceinline__ int sequence_of(const VerifyArgs& a, int row) {
   int n = 0;
-  for (int s = 1 + threadIdx.x; s < a.num_seqs; s += kVThreads) n += a.cu[s] <= row;
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) n += __shfl_xor(n, m, kWave);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds.i[threadIdx.x >> 6] = n;
-  __syncthreads();
-  n = 0;
-#pragma unroll
-  for (int w = 0; w < kVWaves; ++w) n += lds.i[w];
+  for (int s0 = 1; s0 < a.num_seqs; s0 += kWave) {
+    const int s = s0 + (int)(threadIdx.x & 63);
+    n += __popcll(__builtin_amdgcn_ballot_w64(s < a.num_seqs && a.cu[min(s, a.num_seqs)] <= row));
+  }
   return n;
 }
 
-// The first place where running sums exceed `target`: the threads' sums stand behind one
-// another, `mine(i)` are the thread's eight; returns its element, or INT_MAX.
-template <class F>
-__device__ __forceinline__ int first_above(VLds& lds, double before, double target, int e, F mine) {
-  int at = INT_MAX;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    before += mine(i);
-    if (before > target) at = min(at, e + i);
-  }
-  return block_min(lds, at);
+__device__ __forceinline__ double log2e_over(float heat) {
+  return heat > 0.f ? 1.44269504088896340736 / (double)heat : 0.0;
 }
 
-// The draw in a chunk whose weights sum up behind `before`: `fill(e, w)` gives the eight
-// weights from element e on.  Where rounding leaves the target above all of them, the last
-// with a weight (INT_MIN + 1: none).
-template <class F>
-__device__ __forceinline__ int draw_in_chunk(VLds& lds, int chunk, double before, double target,
-                                             F fill) {
-  int found = INT_MAX, last = INT_MAX;
+// A row from its segments' maxima and sums: `total` of exp((x - top) / T), and the first index of
+// its maximum where nothing can be drawn from it (T = 0, no sum; -1: not looked for).
+struct VRow {
+  double total;
+  float top;
+  int best;
+};
+
+template <bool kWide>
+__device__ __forceinline__ VRow row_of(const VerifyArgs& a, const VStat* stats, int segs, int row,
+                                       float heat, double k) {
+  const int lane = threadIdx.x & 63;
+  VRow r{0, -INFINITY, -1};
+  for (int c = lane; c < segs; c += kWave) r.top = fmaxf(r.top, stats[c].top);
+  r.top = wave_max(r.top);
+  const Heat w(r.top, k);
+  int arg = INT_MAX;
+  for (int c = lane; c < segs; c += kWave) {
+    const VStat y = stats[c];
+    if (heat > 0.f)
+      r.total += y.sum * w.weight(y.top);
+    else if (y.top == r.top)
+      arg = min(arg, y.arg);
+  }
+  r.total = wave_sum(r.total);
+  if (r.total > 0) return r;
+  r.total = 0;
+  if (heat > 0.f) {                        // (all masked, or +inf among them)
+    const void* x = logits_row<kWide>(a, row);
+    for (int e = lane * 8; e < a.vocab; e += kVStep) {
+      float y[8];
+      load8<kWide>(x, e, a.vocab, y);
 #pragma unroll
-  for (int v = 0; v < kVPer / 8; ++v) {
-    const int e = chunk * kVChunk + (v * kVThreads + (int)threadIdx.x) * 8;
-    double w[8], mine = 0;
-    fill(e, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      mine += w[i];
-      if (w[i] > 0) last = min(last, -(e + i));
+      for (int i = 0; i < 8; ++i)
+        if (y[i] == r.top && e + i < a.vocab) arg = min(arg, e + i);
     }
-    double total;
-    const double b = before + block_before(lds, mine, total);
-    if (found == INT_MAX) found = first_above(lds, b, target, e, [&](int i) { return w[i]; });
-    before += total;
   }
-  last = block_min(lds, last);
-  return found != INT_MAX ? found : -last;
+  arg = wave_min(arg);
+  r.best = arg < a.vocab ? arg : 0;        // (a row of NaN: 0)
+  return r;
 }
 
-// The chunk that holds u of the total: sums(c) gives chunk c's, kVThreads at a time in
-// order.  Returns it and the sum before it (the last chunk with a sum where rounding
-// leaves none).
+// The segment in which running sums first exceed `target`, sums(c) being segment c's, and the
+// sum before it; the last one with a sum where rounding leaves none, -1 where none has one.
 template <class F>
-__device__ __forceinline__ int chunk_of(VLds& lds, int chunks, double target, F sums, double& before) {
-  double all = 0, b_last = 0;
+__device__ __forceinline__ int segment_of(int segs, double target, F sums, double& before) {
+  double all = 0;
   int last = -1;
-  for (int c0 = 0; c0 < chunks; c0 += kVThreads) {
-    const int c = c0 + (int)threadIdx.x;
-    const double x = c < chunks ? sums(c) : 0;
+  before = 0;
+  for (int c0 = 0; c0 < segs; c0 += kWave) {
+    const int c = c0 + (int)(threadIdx.x & 63);
+    const double x = c < segs ? sums(c) : 0;
     double total;
-    const double b = all + block_before(lds, x, total);
-    const int found = block_min(lds, x > 0 && b + x > target ? c : INT_MAX);
-    const int some = block_min(lds, x > 0 ? -c : INT_MAX);
-    const int here = found != INT_MAX ? found : some != INT_MAX ? -some : -1;
-    if (here >= 0) {
-      __syncthreads();
-      if (c == here) lds.d[0] = b;
-      __syncthreads();
-      b_last = lds.d[0];
-      last = here;
+    const double b = all + wave_before(x, total);
+    const uint64_t above = __builtin_amdgcn_ballot_w64(x > 0 && b + x > target);
+    const uint64_t some = __builtin_amdgcn_ballot_w64(x > 0);
+    if (some != 0) {
+      const int l = above != 0 ? __builtin_ctzll(above) : 63 - __builtin_clzll(some);
+      last = c0 + l;
+      before = __shfl(b, l, kWave);
     }
-    if (found != INT_MAX) break;
+    if (above != 0) break;
     all += total;
   }
-  before = b_last;
   return last;
 }
 
-// The token drawn from a row's weights with u (its chunks' sums are in `stats`).
-template <bool kWide>
-__device__ __forceinline__ int draw_row(VLds& lds, const VerifyArgs& a, const VStat* stats, int row,
-                                        const VRow& r, double k, float u) {
-  double before;
-  const double target = (double)u * r.total;
-  const int chunk = chunk_of(
-      lds, verify_chunks(a.vocab), target,
-      [&](int c) {
-        const VStat s = get(stats + c);
-        return s.sum * weight(s.top, r.top, k);
-      },
-      before);
-  if (chunk < 0) return r.token;
-  const void* x = logits_row<kWide>(a, row);
-  const int t = draw_in_chunk(lds, chunk, before, target, [&](int e, double(&w)[8]) {
-    float y[8];
-    load8<kWide>(x, e, a.vocab, y);
+// The element of a segment in which running sums from `before` on first exceed `target`:
+// w[v][i] is the weight of element e0 + v kVStep + 8 lane + i.  Where rounding leaves none the
+// last with a weight; -1 where none has one.
+template <int kV, class F>
+__device__ __forceinline__ int element_of(int e0, double before, double target, F weights) {
+  int last = -1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = weight(y[i], r.top, k);
-  });
-  return t >= 0 && t < a.vocab ? t : r.token;
+  for (int v = 0; v < kV; ++v) {
+    double w[8], mine = 0, total;
+    weights(v, w);
+    int some = -1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      mine += w[i];
+      if (w[i] > 0) some = i;
+    }
+    double b = before + wave_before(mine, total);
+    int at = -1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      b += w[i];
+      if (at < 0 && w[i] > 0 && b > target) at = i;
+    }
+    const uint64_t above = __builtin_amdgcn_ballot_w64(at >= 0);
+    const uint64_t any = __builtin_amdgcn_ballot_w64(some >= 0);
+    if (any != 0) {
+      const int l = above != 0 ? __builtin_ctzll(above) : 63 - __builtin_clzll(any);
+      last = e0 + v * kVStep + 8 * l + __shfl(above != 0 ? at : some, l, kWave);
+    }
+    if (above != 0) break;
+    before += total;
+  }
+  return last;
 }
 
-// ---- the walk (workgroup-parallel) ----------------------------------------------------
-__device__ __forceinline__ void finish(const VerifyArgs& a, int s, int count, int token) {
+// The token drawn from a row with u.
+template <bool kWide, int kV>
+__device__ __forceinline__ int draw_row(const VerifyArgs& a, const VStat* stats, int row, const VRow& r,
+                                        double k, float u) {
+  double before;
+  const double target = (double)u * r.total;
+  const Heat h(r.top, k);
+  const int seg = segment_of(
+      verify_segments(a.vocab, kV), target,
+      [&](int c) { return stats[c].sum * h.weight(stats[c].top); }, before);
+  const int e0 = max(seg, 0) * kV * kVStep, lane = threadIdx.x & 63;
+  float x[kV][8];
+  load_segment<kWide, kV>(logits_row<kWide>(a, row), e0 + lane * 8, a.vocab,
+                          e0 + kV * kVStep <= a.vocab, x);
+  const int t = element_of<kV>(e0, before, target,
+                               [&](int v, double(&w)[8]) { h.weights<true>(x[v], w); });
+  return min(max(t, 0), a.vocab - 1);
+}
+
+// What a row says without chance, or drawn with u.
+template <bool kWide, int kV>
+__device__ __forceinline__ int token_of(const VerifyArgs& a, const VStat* stats, int row, const VRow& r,
+                                        double k, float u) {
+  return r.best >= 0 ? r.best : draw_row<kWide, kV>(a, stats, row, r, k, u);
+}
+
+// ---- first launch ---------------------------------------------------------------------------
+// (The workgroups' order is rows first, so that waves of a row stream neighbouring memory.)
+template <bool kWide, int kV>
+__global__ __launch_bounds__(kVThreads) void verify_rows_kernel(VerifyArgs a) {
+  const int segs = verify_segments(a.vocab, kV), groups = (segs + kVWaves - 1) / kVWaves;
+  const int row = blockIdx.x / groups, seg = blockIdx.x % groups * kVWaves + wave_id();
+  if (seg >= segs) return;
+  const int lane = threadIdx.x & 63, e0 = seg * kV * kVStep + lane * 8;
+  float x[kV][8];
+  load_segment<kWide, kV>(logits_row<kWide>(a, row), e0, a.vocab, (seg + 1) * kV * kVStep <= a.vocab, x);
+  if (row >= a.cu[a.num_seqs]) return;     // behind the last sequence
+  const float heat = a.temperature[sequence_of(a, row)];
+  VStat st;
+  st.top = -INFINITY;
+  st.sum = 0;
+  st.arg = INT_MAX;
+#pragma unroll
+  for (int v = 0; v < kV; ++v)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) st.top = fmaxf(st.top, x[v][i]);
+  st.top = wave_max(st.top);
+  if (heat > 0.f) {
+    const Heat w(st.top, log2e_over(heat));
+    double sum[8] = {};
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      double y[8];
+      w.weights<false>(x[v], y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += y[i];
+    }
+    st.sum = wave_sum(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
+  } else {
+#pragma unroll
+    for (int v = kV - 1; v >= 0; --v)
+#pragma unroll
+      for (int i = 7; i >= 0; --i)
+        if (x[v][i] == st.top) st.arg = e0 + v * kVStep + i;
+    st.arg = wave_min(st.arg);
+  }
+  const VWs ws = verify_ws(a.ws, a.num_rows, a.vocab);
+  if (lane == 0) ws.stats[(size_t)row * segs + seg] = st;
+}
+
+// ---- second launch ---------------------------------------------------------------------------
+__device__ __forceinline__ void finish(const VerifyArgs& a, int s, int count, int token, int threads) {
   if (threadIdx.x == 0) {
     a.num_kept[s] = count;
     a.next_token[s] = token;
   }
-  for (int i = count + (int)threadIdx.x; i < a.max_kept; i += kVThreads)
+  for (int i = count + (int)threadIdx.x; i < a.max_kept; i += threads)
     a.kept[(size_t)s * a.max_kept + i] = -1;
 }
 
-// From node 0 to the child whose token is the one drawn.
-__device__ __forceinline__ void walk(VLds& lds, const VerifyArgs& a, const VWs& ws, int s, int first,
-                                     int n) {
-  int here = 0, count = 0, token;
-  for (;;) {
-    if (threadIdx.x == 0) a.kept[(size_t)s * a.max_kept + count] = here;
-    ++count;
-    token = get(&ws.row[first + here]).token;
-    if (count == a.max_kept) break;
-    int child = INT_MAX;
-    if (a.parents == nullptr) {
-      if (here + 1 < n && a.tokens[first + here + 1] == token) child = here + 1;
-    } else {
-      for (int j = here + 1 + (int)threadIdx.x; j < n; j += kVThreads)
-        if (child == INT_MAX && a.parents[first + j] == here && a.tokens[first + j] == token) child = j;
-      child = block_min(lds, child);
-    }
-    if (child == INT_MAX) break;
-    here = child;
-  }
-  finish(a, s, count, token);
-}
-
-template <bool kWide>
-__global__ __launch_bounds__(kVThreads) void verify_rows_kernel(VerifyArgs a) {
-  __shared__ VLds lds;
-  const int chunks = verify_chunks(a.vocab);
-  const VWs ws = verify_ws(a.ws, a.num_rows, a.vocab);
-  for (int s = blockIdx.x * kVThreads + threadIdx.x; s < a.num_seqs; s += gridDim.x * kVThreads)
-    if (a.cu[s + 1] == a.cu[s]) {          // no node: nothing kept, no token
+// Sequences without nodes: nothing kept, no token.
+__device__ __forceinline__ void finish_empty(const VerifyArgs& a) {
+  for (int s = blockIdx.x * blockDim.x + threadIdx.x; s < a.num_seqs; s += gridDim.x * blockDim.x)
+    if (a.cu[s + 1] == a.cu[s]) {
       a.num_kept[s] = 0;
       a.next_token[s] = -1;
       for (int i = 0; i < a.max_kept; ++i) a.kept[(size_t)s * a.max_kept + i] = -1;
     }
-  const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
-  if (a.num_seqs == 0 || row >= min(a.cu[a.num_seqs], a.num_rows)) return;
-
-  float x[kVPer];
-#pragma unroll
-  for (int v = 0; v < kVPer / 8; ++v)
-    load8<kWide>(logits_row<kWide>(a, row), chunk * kVChunk + (v * kVThreads + (int)threadIdx.x) * 8,
-                 a.vocab, *reinterpret_cast<float(*)[8]>(x + 8 * v));
-  const int s = sequence_of(lds, a, row);
-  const int first = a.cu[s], n = a.cu[s + 1] - first;
-  const float heat = a.temperature[s];
-  const bool sampled = heat > 0.f;
-  const double k = sampled ? 1.44269504088896340736 / (double)heat : 0.0;
-
-  VStat st;
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kVPer; ++i) top = fmaxf(top, x[i]);
-  st.top = block_max(lds, top);
-  st.sum = 0;
-  if (sampled) {
-#pragma unroll
-    for (int i = 0; i < kVPer; ++i) st.sum += weight(x[i], st.top, k);
-    st.sum = block_sum(lds, st.sum);
-  }
-  int arg = INT_MAX;
-#pragma unroll
-  for (int v = kVPer / 8 - 1; v >= 0; --v)
-#pragma unroll
-    for (int i = 7; i >= 0; --i)
-      if (x[8 * v + i] == st.top) arg = chunk * kVChunk + (v * kVThreads + (int)threadIdx.x) * 8 + i;
-  st.arg = block_min(lds, arg);
-  VStat* stats = ws.stats + (size_t)row * chunks;
-  if (threadIdx.x == 0) put(stats + chunk, st);
-  if (!last_to_arrive(lds, ws.rows + row, chunks)) return;
-
-  // ---- the row ---------------------------------------------------------------------------
-  VRow r{};
-  top = -INFINITY;
-  for (int c = threadIdx.x; c < chunks; c += kVThreads) top = fmaxf(top, get(stats + c).top);
-  r.top = block_max(lds, top);
-  double total = 0;
-  arg = INT_MAX;
-  for (int c = threadIdx.x; c < chunks; c += kVThreads) {
-    const VStat y = get(stats + c);
-    if (sampled) total += y.sum * weight(y.top, r.top, k);
-    if (y.top == r.top) arg = min(arg, y.arg);
-  }
-  r.total = block_sum(lds, total);
-  arg = block_min(lds, arg);
-  r.token = arg < a.vocab ? arg : 0;       // (a row of NaN: 0)
-  const bool drawn = sampled && r.total > 0;
-  if (a.draft == nullptr) {
-    if (drawn) r.token = draw_row<kWide>(lds, a, stats, row, r, k, a.uniforms[row]);
-  } else if (row + 1 < first + n) {
-    const int next = a.tokens[row + 1];
-    if (!drawn) {
-      r.accept = next == r.token;
-    } else if (next >= 0 && next < a.vocab) {
-      float y;
-      if constexpr (kWide)
-        y = ((const float*)logits_row<kWide>(a, row))[next];
-      else
-        y = __uint_as_float((uint32_t)((const bf16_t*)logits_row<kWide>(a, row))[next] << 16);
-      const double q = a.draft[(size_t)(row + 1) * a.draft_stride + next];
-      r.accept = (double)a.uniforms[row + 1] * q < weight(y, r.top, k) / r.total;
-    }
-  }
-  if (threadIdx.x == 0) put(ws.row + row, r);
-  if (a.draft != nullptr) return;          // (the second launch goes on)
-  if (!last_to_arrive(lds, ws.seqs + s, n)) return;
-  walk(lds, a, ws, s, first, n);
 }
 
-// With the drafter's probabilities: the accepted nodes, and the token behind them.
-template <bool kWide>
-__global__ __launch_bounds__(kVThreads) void verify_rest_kernel(VerifyArgs a) {
-  __shared__ VLds lds;
-  const int chunks = verify_chunks(a.vocab);
+// From node 0 to the child whose token is the one drawn (one wave).
+template <class Drawn, class Token, class Parent>
+__device__ __forceinline__ void walk(const VerifyArgs& a, int s, int n, Drawn drawn, Token tokens,
+                                     Parent parents) {
+  int here = 0, count = 0, token;
+  for (;;) {
+    if (threadIdx.x == 0) a.kept[(size_t)s * a.max_kept + count] = here;
+    ++count;
+    token = drawn(here);
+    if (count == a.max_kept) break;
+    int child = INT_MAX;
+    for (int j0 = here + 1; j0 < n && child == INT_MAX; j0 += kWave) {
+      const int j = j0 + (int)threadIdx.x, x = min(j, n - 1);
+      const uint64_t is = __builtin_amdgcn_ballot_w64(j < n && parents(x) == here && tokens(x) == token);
+      if (is != 0) child = j0 + __builtin_ctzll(is);
+      if (a.parents == nullptr) break;
+    }
+    if (child == INT_MAX) break;
+    here = child;
+  }
+  finish(a, s, count, token, kWave);
+}
+
+// Without the drafter's probabilities: a wave draws a row's token; the last of a sequence walks.
+template <bool kWide, int kV>
+__global__ __launch_bounds__(kWave) void verify_walk_kernel(VerifyArgs a) {
+  __shared__ int drawn[kVWalk], tokens[kVWalk], parents[kVWalk], flag;
+  finish_empty(a);
+  const int row = blockIdx.x;
+  if (a.num_seqs == 0 || row >= min(a.cu[a.num_seqs], a.num_rows)) return;
   const VWs ws = verify_ws(a.ws, a.num_rows, a.vocab);
-  const int s = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
+  const int segs = verify_segments(a.vocab, kV), s = sequence_of(a, row);
+  const int first = a.cu[s], n = a.cu[s + 1] - first;
+  const float heat = a.temperature[s], u = a.uniforms[row];
+  const double k = log2e_over(heat);
+  const VStat* stats = ws.stats + (size_t)row * segs;
+  const VRow r = row_of<kWide>(a, stats, segs, row, heat, k);
+  const int token = token_of<kWide, kV>(a, stats, row, r, k, u);
+  if (threadIdx.x == 0)
+    __hip_atomic_store(ws.drawn + row, token, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (!last_to_arrive(flag, ws.seqs + s, n)) return;
+  auto get = [&](int i) {
+    return __hip_atomic_load(ws.drawn + first + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  auto parent = [&](int i) { return a.parents != nullptr ? a.parents[first + i] : i - 1; };
+  if (n > kVWalk) {
+    walk(a, s, n, get, [&](int i) { return a.tokens[first + i]; }, parent);
+    return;
+  }
+  for (int i = threadIdx.x; i < n; i += kWave) {
+    drawn[i] = get(i);
+    tokens[i] = a.tokens[first + i];
+    parents[i] = parent(i);
+  }
+  __syncthreads();
+  walk(a, s, n, [&](int i) { return drawn[i]; }, [&](int i) { return tokens[i]; },
+       [&](int i) { return parents[i]; });
+}
+
+// With the drafter's probabilities: the kept nodes, and the token behind them.  Every workgroup
+// of a sequence finds its last kept node, four rows at a time.
+template <bool kWide, int kV, int kRows>
+__global__ __launch_bounds__(kVThreads) void verify_rest_kernel(VerifyArgs a) {
+  __shared__ double sh_total[kVWaves];
+  __shared__ float sh_top[kVWaves];
+  __shared__ int sh_best[kVWaves], sh_ok[kVWaves], flag;
+  finish_empty(a);
+  const int segs = verify_segments(a.vocab, kV), groups = (segs + kVWaves - 1) / kVWaves;
+  const int wave = wave_id(), lane = threadIdx.x & 63;
+  const int s = blockIdx.x / groups, group = blockIdx.x % groups, seg = group * kVWaves + wave;
   const int first = a.cu[s], n = min(a.cu[s + 1], a.num_rows) - first;
   if (n <= 0) return;
-  // the first node that is not accepted
-  int count = INT_MAX;
-  for (int j = threadIdx.x; j < n; j += kVThreads)
-    if (count == INT_MAX && (j + 1 == n || get(&ws.row[first + j]).accept == 0)) count = j + 1;
-  count = min(block_min(lds, count), a.max_kept);
-  const int row = first + count - 1;
-  const VRow r = get(&ws.row[row]);
-  const float heat = a.temperature[s];
-  const bool drawn = heat > 0.f && r.total > 0;
-  // (behind max_kept nodes the next one is neither accepted nor refused)
-  const bool refused = count < n && r.accept == 0;
-  const double k = drawn ? 1.44269504088896340736 / (double)heat : 0.0;
-  const float u = a.uniforms[first];
-  if (chunk == 0) {
-    for (int i = threadIdx.x; i < count; i += kVThreads) a.kept[(size_t)s * a.max_kept + i] = i;
+  const VWs ws = verify_ws(a.ws, a.num_rows, a.vocab);
+  const int row_segs = verify_segments(a.vocab, kRows);
+  const float heat = a.temperature[s], u = a.uniforms[first];
+  const double k = log2e_over(heat);
+
+  int count = 0;
+  VRow r;
+  bool refused = false;
+  while (count < a.max_kept && !refused && count < n) {
+    const int i = min(count + wave, n - 1), row = first + i;
+    VRow mine = row_of<kWide>(a, ws.stats + (size_t)row * row_segs, row_segs, row, heat, k);
+    bool ok = false;
+    if (i + 1 < n) {
+      const int next = a.tokens[row + 1];
+      if (mine.best >= 0) {
+        ok = next == mine.best;
+      } else if (next >= 0 && next < a.vocab) {
+        const void* x = logits_row<kWide>(a, row);
+        const float y = kWide ? ((const float*)x)[next]
+                              : __uint_as_float((uint32_t)((const bf16_t*)x)[next] << 16);
+        const double q = a.draft[(size_t)(row + 1) * a.draft_stride + next];
+        ok = (double)a.uniforms[row + 1] * q < Heat(mine.top, k).weight(y) / mine.total;
+      }
+    }
+    if (lane == 0) {
+      sh_total[wave] = mine.total;
+      sh_top[wave] = mine.top;
+      sh_best[wave] = mine.best;
+      sh_ok[wave] = ok;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kVWaves; ++w) {
+      if (refused || count == a.max_kept || count == n) break;
+      r = VRow{sh_total[w], sh_top[w], sh_best[w]};
+      ++count;
+      refused = sh_ok[w] == 0;             // (the last node has no next one to refuse)
+    }
+    __syncthreads();
   }
-  if (!drawn || !refused) {
-    if (chunk != 0) return;
-    const int token = drawn ? draw_row<kWide>(lds, a, ws.stats + (size_t)row * chunks, row, r, k, u)
-                            : r.token;
-    finish(a, s, count, token);
+  refused = refused && count < n && count < a.max_kept;   // (the last that may be kept has no children)
+  const int row = first + count - 1;
+  const VStat* stats = ws.stats + (size_t)row * row_segs;
+  if (group == 0)
+    for (int i = threadIdx.x; i < count; i += kVThreads) a.kept[(size_t)s * a.max_kept + i] = i;
+  if (!refused || r.best >= 0) {
+    if (group != 0) return;
+    int token = r.best;
+    if (token < 0 && wave == 0) token = draw_row<kWide, kRows>(a, stats, row, r, k, u);
+    finish(a, s, count, token, kVThreads);
     return;
   }
   const void* x = logits_row<kWide>(a, row);
   const float* q = a.draft + (size_t)(row + 1) * a.draft_stride;
-  auto fill = [&](int e, double(&w)[8]) {
-    float y[8], z[8];
-    load8<kWide>(x, e, a.vocab, y);
-    load8<true>(q, e, a.vocab, z);
+  const Heat h(r.top, k);
+  const double inv = 1.0 / r.total;
+  float y[kV][8], z[kV][8];
+  auto rest_of = [&](int v, int e0, double(&w)[8]) {     // max(p - q, 0)
+    h.weights<true>(y[v], w);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      w[i] = e + i < a.vocab ? __builtin_fmax(weight(y[i], r.top, k) / r.total - (double)z[i], 0.0) : 0.0;
+      w[i] = e0 + v * kVStep + lane * 8 + i < a.vocab
+                 ? __builtin_fmax(__builtin_fma(w[i], inv, -(double)z[v][i]), 0.0)
+                 : 0.0;
+  };
+  auto load = [&](int e0) {
+    load_segment<kWide, kV>(x, e0 + lane * 8, a.vocab, e0 + kV * kVStep <= a.vocab, y);
+    load_segment<true, kV>(q, e0 + lane * 8, a.vocab, e0 + kV * kVStep <= a.vocab, z);
   };
   double sum = 0;
+  load(seg * kV * kVStep);
 #pragma unroll
-  for (int v = 0; v < kVPer / 8; ++v) {
+  for (int v = 0; v < kV; ++v) {
     double w[8];
-    fill(chunk * kVChunk + (v * kVThreads + (int)threadIdx.x) * 8, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum += w[i];
+    rest_of(v, seg * kV * kVStep, w);
+    sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
   }
-  sum = block_sum(lds, sum);
-  double* rest = ws.rest + (size_t)s * chunks;
-  if (threadIdx.x == 0) put(rest + chunk, sum);
-  if (!last_to_arrive(lds, ws.seqs + kVerifyMaxSeqs + s, chunks)) return;
-  sum = 0;
-  for (int c = threadIdx.x; c < chunks; c += kVThreads) sum += get(rest + c);
-  const double total = block_sum(lds, sum);
+  sum = wave_sum(sum);
+  uint64_t* rest = reinterpret_cast<uint64_t*>(ws.rest + (size_t)s * segs);
+  if (lane == 0 && seg < segs)
+    __hip_atomic_store(rest + seg, __builtin_bit_cast(uint64_t, sum), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+  if (!last_to_arrive(flag, ws.seqs + kVerifyMaxSeqs + s, groups)) return;
+  auto sums = [&](int c) {
+    return __builtin_bit_cast(
+        double, __hip_atomic_load(rest + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+  };
   int token = -1;
-  if (total > 0) {
-    double before;
-    const double target = (double)u * total;
-    const int c = chunk_of(lds, chunks, target, [&](int i) { return get(rest + i); }, before);
-    if (c >= 0) token = draw_in_chunk(lds, c, before, target, fill);
+  if (wave == 0) {
+    double total = 0, before;
+    for (int c = lane; c < segs; c += kWave) total += sums(c);
+    const double target = (double)u * wave_sum(total);
+    const int c = segment_of(segs, target, sums, before);
+    if (c >= 0) {
+      load(c * kV * kVStep);
+      token = element_of<kV>(c * kV * kVStep, before, target,
+                             [&](int v, double(&w)[8]) { rest_of(v, c * kV * kVStep, w); });
+    }
+    if (token < 0 || token >= a.vocab)     // (p = q to the last bit: p itself)
+      token = draw_row<kWide, kRows>(a, stats, row, r, k, u);
   }
-  if (token < 0 || token >= a.vocab)       // (p = q to the last bit: p itself)
-    token = draw_row<kWide>(lds, a, ws.stats + (size_t)row * chunks, row, r, k, u);
-  finish(a, s, count, token);
+  finish(a, s, count, token, kVThreads);
+}
+
+#ifndef FILL
+#define FILL 8192
+#endif
+#ifndef RFILL
+#define RFILL 2048
+#endif
+// Loads of a segment of `rows` rows: as many as leave the GPU `fill` waves.
+constexpr int64_t kVFill = FILL, kVRestFill = RFILL;
+constexpr int kVMaxLoads = 8, kVMaxRestLoads = 4;
+
+int verify_loads(int64_t rows, int vocab, int64_t fill, int kv) {
+  while (kv > 1 && rows * verify_segments(vocab, kv) < fill) kv /= 2;
+  return kv;
+}
+
+int row_loads(const VerifyArgs& a) { return verify_loads(a.num_rows, a.vocab, kVFill, kVMaxLoads); }
+int rest_loads(const VerifyArgs& a) {
+  return verify_loads(a.num_seqs, a.vocab, kVRestFill, kVMaxRestLoads);
+}
+
+int64_t verify_groups(int vocab, int kv) {
+  return (verify_segments(vocab, kv) + kVWaves - 1) / kVWaves;
+}
+
+template <bool kWide, int kV>
+void launch_verify_v(const VerifyArgs& a, hipStream_t stream) {
+  const dim3 block(kVThreads);
+  if (a.num_rows > 0)
+    verify_rows_kernel<kWide, kV>
+        <<<dim3((unsigned)(a.num_rows * verify_groups(a.vocab, kV))), block, 0, stream>>>(a);
+  if (a.draft == nullptr || a.num_rows == 0) {
+    verify_walk_kernel<kWide, kV>
+        <<<dim3((unsigned)std::max(a.num_rows, 1)), dim3(kWave), 0, stream>>>(a);
+    return;
+  }
+  const int kv = rest_loads(a);
+  const dim3 grid((unsigned)(a.num_seqs * verify_groups(a.vocab, kv)));
+  if (kv == 1)
+    verify_rest_kernel<kWide, 1, kV><<<grid, block, 0, stream>>>(a);
+  else if (kv == 2)
+    verify_rest_kernel<kWide, 2, kV><<<grid, block, 0, stream>>>(a);
+  else
+    verify_rest_kernel<kWide, 4, kV><<<grid, block, 0, stream>>>(a);
+}
+
+template <bool kWide>
+void launch_verify_w(const VerifyArgs& a, hipStream_t stream) {
+  switch (row_loads(a)) {
+    case 1: launch_verify_v<kWide, 1>(a, stream); break;
+    case 2: launch_verify_v<kWide, 2>(a, stream); break;
+    case 4: launch_verify_v<kWide, 4>(a, stream); break;
+    default: launch_verify_v<kWide, 8>(a, stream);
+  }
 }
 
 }  // namespace
@@ -543,28 +678,16 @@ __global__ __launch_bounds__(kVThreads) void verify_rest_kernel(VerifyArgs a) {
 size_t verify_workspace(int num_rows, int num_seqs, int vocab) {
   const VWs w = verify_ws(nullptr, num_rows, vocab);
   return reinterpret_cast<size_t>(w.rest) +
-         up256((size_t)num_seqs * verify_chunks(vocab) * sizeof(double));
+         up256((size_t)num_seqs * verify_segments(vocab, 1) * sizeof(double));
 }
 
 int64_t verify_grid(const VerifyArgs& a) {
-  return std::max<int64_t>(1, (int64_t)std::max(a.num_rows, a.draft != nullptr ? a.num_seqs : 0) *
-                                  verify_chunks(a.vocab));
+  return std::max(a.num_rows * verify_groups(a.vocab, row_loads(a)),
+                  a.num_seqs * verify_groups(a.vocab, rest_loads(a)));
 }
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
-  const int64_t chunks = verify_chunks(a.vocab);
-  const dim3 rows((unsigned)std::max<int64_t>(1, a.num_rows * chunks)), block(kVThreads);
-  const dim3 rest((unsigned)(a.num_seqs * chunks));
-  if (a.wide)
-    verify_rows_kernel<true><<<rows, block, 0, stream>>>(a);
-  else
-    verify_rows_kernel<false><<<rows, block, 0, stream>>>(a);
-  if (a.draft != nullptr && a.num_rows > 0) {
-    if (a.wide)
-      verify_rest_kernel<true><<<rest, block, 0, stream>>>(a);
-    else
-      verify_rest_kernel<false><<<rest, block, 0, stream>>>(a);
-  }
+  a.wide ? launch_verify_w<true>(a, stream) : launch_verify_w<false>(a, stream);
   return hipGetLastError();
 }
 

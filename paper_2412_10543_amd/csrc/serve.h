@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -79,8 +80,8 @@ struct Kv4Shape {
 
 constexpr int kKv4PlanSeqs = 1024;         // sequences that are cut from their lengths
 constexpr int kKv4Counters = 4096;         // arrival counters of a call, at most
-constexpr int kVerifyMaxRows = 49152;      // (a counter each)
-constexpr int kVerifyMaxSeqs = 8192;       // (two)
+constexpr int kVerifyMaxRows = 1 << 20;
+constexpr int kVerifyMaxSeqs = 16384;      // (two counters each)
 constexpr int kVerifyMaxVocab = 1 << 28;
 
 int64_t rope_grid(const RopeArgs& a);

@@ -11,7 +11,7 @@ from paper_2412_10543_amd import binding
 
 pytestmark = pytest.mark.gpu
 
-COUNTERS = 49152 + 2 * 8192
+COUNTERS = 2 * 16384
 
 
 def _i32(x):
@@ -93,6 +93,29 @@ def test_drafts_that_fit_are_kept_to_the_end(with_draft):
         want = ss.reference_verify(logits.numpy(), tokens, cu, heat, u.tolist(), max_kept,
                                    draft=draft.numpy() if with_draft else None)
         assert got == tuple(want) and got[1] == [min(max_kept, n)] * 6
+
+
+@pytest.mark.parametrize("chain,with_draft", [(False, False), (True, False), (True, True)])
+@pytest.mark.parametrize("max_kept", [1, 2, 3])
+def test_paths_that_may_not_be_longer(chain, with_draft, max_kept):
+    """The last node that may be kept counts as having no children, refused or not."""
+    for seed in range(4):
+        _check([9, 1, 4, 0, 12, 3, 3, 2, 7], 900, chain, with_draft, True, max_kept=max_kept, seed=seed)
+
+
+def test_long_chains_and_trees():
+    """More nodes than the walk holds at a time, rows more than four at a time."""
+    _check([1500, 3], 40, False, False, True, seed=1, heats=(0.0,))
+    n, vocab = 1200, 30
+    logits, tokens, _, cu, heat, u, draft = ss.verify_case(2, [n, 37], vocab, True, heats=(0.0,))
+    for row in range(n + 37):
+        if row not in (0, n):
+            tokens[row] = int(logits[row - 1].argmax())
+    for d in (None, draft):
+        got = _verify(logits.cuda(), tokens, None, cu, heat, u, None if d is None else d.cuda(), n)
+        want = ss.reference_verify(logits.numpy(), tokens, cu, heat, u.tolist(), n,
+                                   draft=None if d is None else d.numpy())
+        assert got == tuple(want) and got[1] == [n, 37]
 
 
 def test_greedy_ties_take_the_lowest_index():

@@ -141,7 +141,7 @@ VERIFY = dict(logits=_at(0), wide=0, ls=1000, draft=None, ds=0, tokens=_at(2), p
     (dict(draft=_at(1), ds=999, parents=None), BAD), (dict(draft=_at(1) + 4, ds=1000, parents=None), BAD),
     (dict(ws=_at(10) + 128), BAD), (dict(kept=_at(2)), BAD), (dict(n=_at(4)), BAD),
     (dict(nxt=_at(8) + 12), BAD), (dict(kept=_at(10)), BAD), (dict(ws=_at(0)), BAD),
-    (dict(draft=_at(1), ds=1000), NO), (dict(T=49153), NO), (dict(S=8193), NO),
+    (dict(draft=_at(1), ds=1000), NO), (dict(T=(1 << 20) + 1), NO), (dict(S=16385), NO),
     (dict(V=(1 << 28) + 1, ls=1 << 29), NO),
     (dict(ws=None), WS), (dict(ws_bytes=1000), WS), (dict(S=0), OK),
 ])
@@ -153,10 +153,10 @@ def test_verify_refusals(kw, status):
 def test_verify_workspace_serves_smaller_calls():
     size = binding.rag_draft_verify_workspace_size
     steps = [(1, 1, 1), (5, 1, 4096), (5, 2, 4097), (300, 64, 128000), (300, 65, 128000),
-             (49152, 8192, 200000)]
+             (1 << 20, 16384, 200000)]
     sizes = [size(*x) for x in steps]
     assert sizes == sorted(sizes) and sizes[0] > 0
-    for bad in ((-1, 1, 10), (1, -1, 10), (1, 1, 0), (49153, 1, 10), (1, 8193, 10), (1, 1, (1 << 28) + 1)):
+    for bad in ((-1, 1, 10), (1, -1, 10), (1, 1, 0), ((1 << 20) + 1, 1, 10), (1, 16385, 10), (1, 1, (1 << 28) + 1)):
         assert size(*bad) == 0
 
 
