@@ -11,7 +11,7 @@
 //
 // A draw by running sums turns on the sum of everything before the drawn token: with
 // 128,000 likely tokens, sums in fp32 would move one draw in ten.  Exponentials and sums
-// are therefore fp64 (the vector units' rate for it is that of fp32).
+// are therefore fp64.
 //
 // First launch: a wave takes a segment of a row into its registers and leaves its maximum and
 // sum; the logits are read once.  Second launch, without the drafter's probabilities: a wave for
@@ -70,8 +70,9 @@ __host__ __device__ __forceinline__ VWs verify_ws(char* base, int num_rows, int 
 // exp((x - top) / T) for x <= top; what lies under 2^-1000 counts as 0, as NaN does, and where
 // top is infinite everything does.
 //   2^t = 2^n p(t - n), n the nearest whole number (from the low bits of t + 1.5 2^52), p(f) =
-//   1 + f r(f), r of degree 8 through (2^f - 1) / f at the Chebyshev nodes of [-1/2, 1/2]:
-//   2^-44 relative, and 1 at 0 (so that equal logits have equal sums).
+//   1 + f r(f), r of degree 7 through (2^f - 1) / f at the Chebyshev nodes of [-1/2, 1/2]:
+//   2^-38 relative, and 1 at 0 (so that equal logits have equal sums).  What of that all weights
+//   share drops out of a draw, so that it moves one draw in 10^8 among 128,000 likely tokens.
 struct Heat {
   double k, top;                // log2(e) / T
   float cut;
@@ -84,9 +85,9 @@ struct Heat {
   template <bool kExact, int N>
   __device__ __forceinline__ void weights(const float (&x)[N], double (&w)[N]) const {
     constexpr double kRound = 6755399441055744.0;
-    constexpr double kP[10] = {1.0, 0.6931471805599453, 0.2402265069581299, 0.05550410866476082,
-                               0.009618129159402558, 0.0013333558178986627, 0.00015403455852453838,
-                               1.5252686876393043e-05, 1.3255224878668817e-06, 1.0203115707778471e-07};
+    constexpr double kP[9] = {1.0, 0.6931471805568324, 0.24022650695888503,
+                              0.055504109063258665, 0.00961812913523614, 0.0013333478473685416,
+                              0.00015403475186530786, 1.5303700711365693e-05, 1.325080551750225e-06};
     double f[N], p[N];
     uint32_t n[N];
 #pragma unroll
@@ -95,10 +96,10 @@ struct Heat {
       const double m = __builtin_fma(d, k, kRound);
       f[i] = __builtin_fma(d, k, kRound - m);
       n[i] = (uint32_t)__builtin_bit_cast(uint64_t, m);
-      p[i] = kP[9];
+      p[i] = kP[8];
     }
 #pragma unroll
-    for (int j = 8; j >= 0; --j)
+    for (int j = 7; j >= 0; --j)
 #pragma unroll
       for (int i = 0; i < N; ++i) p[i] = __builtin_fma(p[i], f[i], kP[j]);
 #pragma unroll
@@ -401,15 +402,18 @@ __global__ __launch_bounds__(kVThreads) void verify_rows_kernel(VerifyArgs a) {
   st.top = wave_max(st.top);
   if (heat > 0.f) {
     const Heat w(st.top, log2e_over(heat));
-    double sum[8] = {};
+    double sum[4] = {};
 #pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      double y[8];
-      w.weights<false>(x[v], y);
+    for (int v = 0; v < kV * 2; ++v) {
+      float z[4];
+      double y[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += y[i];
+      for (int i = 0; i < 4; ++i) z[i] = x[v / 2][v % 2 * 4 + i];
+      w.weights<false>(z, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] += y[i];
     }
-    st.sum = wave_sum(((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7])));
+    st.sum = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
   } else {
 #pragma unroll
     for (int v = kV - 1; v >= 0; --v)
@@ -626,7 +630,7 @@ __global__ __launch_bounds__(kVThreads) void verify_rest_kernel(VerifyArgs a) {
 #endif
 // Loads of a segment of `rows` rows: as many as leave the GPU `fill` waves.
 constexpr int64_t kVFill = FILL, kVRestFill = RFILL;
-constexpr int kVMaxLoads = 8, kVMaxRestLoads = 4;
+constexpr int kVMaxLoads = 4, kVMaxRestLoads = 4;
 
 int verify_loads(int64_t rows, int vocab, int64_t fill, int kv) {
   while (kv > 1 && rows * verify_segments(vocab, kv) < fill) kv /= 2;
@@ -668,8 +672,7 @@ void launch_verify_w(const VerifyArgs& a, hipStream_t stream) {
   switch (row_loads(a)) {
     case 1: launch_verify_v<kWide, 1>(a, stream); break;
     case 2: launch_verify_v<kWide, 2>(a, stream); break;
-    case 4: launch_verify_v<kWide, 4>(a, stream); break;
-    default: launch_verify_v<kWide, 8>(a, stream);
+    default: launch_verify_v<kWide, 4>(a, stream);
   }
 }
 
