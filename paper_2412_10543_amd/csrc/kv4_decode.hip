@@ -12,8 +12,10 @@
 // correction uses the rounded p', so that 128 cancels.
 //
 // A wave takes blocks of two pages (32 keys) straight into registers, one 16-byte load
-// for a page's K codes and one for its V codes; the workgroup's four waves take
-// every fourth block each and join their states through LDS.  As many workgroups as
+// for a page's K codes and one for its V codes, for 16 pairs.  A workgroup's four waves take
+// every fourth block each, for up to 16 pairs; every second, two and two, for 32; or all four
+// each block for 64, which then reaches them through the CU's cache.  They join their states
+// through LDS.  As many workgroups as
 // the chip takes at a time get even shares of all sequences' blocks; a sequence that is
 // cut writes partial outputs and log-sum-exps, which the last of its workgroups to
 // finish joins.
@@ -27,6 +29,7 @@ namespace {
 
 constexpr int kQWaves = 4;
 constexpr int kQKeys = 32;                 // keys of a block
+constexpr int kQPairs = 16 * kQWaves;      // pairs of a tile, at most
 constexpr int kQMinBlocks = 8;             // blocks of a share, at least
 constexpr int kQStart = 6;                 // blocks that the start of a tile counts for
 constexpr int kQMaxPieces = 64;            // of a tile (one lane each in the join)
@@ -45,7 +48,7 @@ struct Kv4Plan {
   int start[4], len[4], tiles[4], total, share;
 };
 
-template <int D, int T>
+template <int D>
 struct Kv4Lds {
   float o[kQWaves][16][D + 4];
   float m[kQWaves][16], l[kQWaves][16];
@@ -73,7 +76,7 @@ __device__ __forceinline__ int kv4_blocks(int kv_len) {
 }
 
 // The sequences' places in one row of all blocks, kQStart more in front of each tile.
-template <int C, class Lds>
+template <class Lds>
 __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& plan) {
   const int group = a.hq / a.hkv;
   int sum = 0, longest = 0;
@@ -84,7 +87,7 @@ __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& pl
     if (s < a.num_seqs) {
       int qb, rows, kv;
       kv4_sequence(a, s, qb, rows, kv);
-      plan.tiles[i] = (max(rows, 0) * group + C - 1) / C;
+      plan.tiles[i] = (max(rows, 0) * group + kQPairs - 1) / kQPairs;
       plan.len[i] = kv4_blocks(kv) + kQStart;
     }
     plan.start[i] = sum;
@@ -149,260 +152,213 @@ __device__ __forceinline__ Kv4Piece kv4_find(const Kv4Args& a, Lds& lds, const K
   return lds.piece;
 }
 
-// A page's codes and parameters, as a lane has them.
+// Half of a block (K or V) as a lane has it: of two pages the codes, words (g, w) of key l16 or V
+// units of keys 4 g4 .., and the parameters of keys 4 g4 .. 4 g4 + 3.
 template <int D>
-struct Kv4Regs {
-  static constexpr int kGroups = D / 64;
-  uint32_t k[2 * kGroups], v[2 * kGroups];   // words (g, w) of key l16; V units of keys 4 g4 ..
-  u32x4 kp[kGroups], vp[kGroups];            // of keys 4 g4 .. 4 g4 + 3
+struct Kv4Half {
+  uint32_t c[2][D / 32];
+  u32x4 p[2][D / 64];
+  __device__ __forceinline__ void load(int j, const char* page, int code_at, int g4) {
+    if constexpr (D == 128) {
+      const u32x4 y = load16_stream(page + code_at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[j][i] = y[i];
+    } else {
+      const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(page + code_at));
+      c[j][0] = y[0];
+      c[j][1] = y[1];
+    }
+#pragma unroll
+    for (int g = 0; g < D / 64; ++g) p[j][g] = load16(page + Kv4Page<D>::param(4 * g4, g));
+  }
 };
 
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&x)[N], const char* p) {
-  if constexpr (N == 4) {
-    const u32x4 y = load16_stream(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = y[i];
-  } else {
-    const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-    x[0] = y[0];
-    x[1] = y[1];
-  }
-}
-
-template <int D>
-__device__ __forceinline__ void kv4_load(Kv4Regs<D>& r, const char* kp, const char* vp, int lane) {
-  const int g4 = lane >> 4;
-  load_words(r.k, kp + (lane & 15) * (D / 2) + g4 * (D / 8));
-  load_words(r.v, vp + ((lane & 15) * 16 + 4 * g4) * (D / 32));
-#pragma unroll
-  for (int g = 0; g < D / 64; ++g) {
-    r.kp[g] = load16(kp + Kv4Page<D>::param(4 * g4, g));
-    r.vp[g] = load16(vp + Kv4Page<D>::param(4 * g4, g));
-  }
-}
-
-__device__ __forceinline__ bf16x8 kv4_operand(uint32_t w) {
-  const u32x4 x = {kv4_pair(w, 0), kv4_pair(w, 1), kv4_pair(w, 2), kv4_pair(w, 3)};
+__device__ __forceinline__ bf16x8 kv4_operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const u32x4 x = {a, b, c, d};
   return as_bf16x8(x);
 }
 
-// A wave's state of T column tiles of 16 (row, q head) pairs: O^T without its
-// corrections, the corrections (this lane's keys' share), the sum of weights and the
-// maximum that they refer to (scores times scale log2 e).
-template <int D, int T>
+// A wave's state of 16 (row, q head) pairs: O^T without its corrections, the corrections (this
+// lane's keys' share), the sum of weights and the maximum that they refer to (scores times
+// scale log2 e).
+template <int D>
 struct Kv4State {
-  f32x4 o[T][D / 16];           // [4 g + e]: channels 64 g + 4 (4 g4 + r) + e
-  float corr[T][D / 64], l[T], m[T];
+  f32x4 o[D / 16];              // [4 g + e]: channels 64 g + 4 (4 g4 + r) + e
+  float corr[D / 64], l, m;
 };
 
-// Blocks b0 + wave, + kQWaves, .. below b1.
-template <int D, int T>
-__device__ __forceinline__ void kv4_blocks_of_wave(const Kv4Args& a, const Kv4Piece& x, int h,
-                                                   Kv4State<D, T>& st) {
+// Pairs pair0 .. pair0 + 15 against blocks b, b + step, .. below b1.
+template <int D>
+__device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, int h, int pair0, int b,
+                                         int step, Kv4State<D>& st) {
   constexpr int kG = D / 64;
   using P = Kv4Page<D>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   const int group = a.hq / a.hkv, pairs = x.rows * group;
   const float c = a.scale * kLog2e;
 
-  bf16x8 q[T][2 * kG];
-  float qsum[T][kG];
-  int last[T];                             // the last key that the lane's column sees
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int pair = (x.tile * T + t) * 16 + l16, row = min(pair, pairs - 1) / group;
-    const bf16_t* src = (const bf16_t*)a.q +
-                        ((size_t)(x.qb + row) * a.hq + h * group + min(pair, pairs - 1) % group) * D;
-    last[t] = x.kv_len - x.rows + row;
-#pragma unroll
-    for (int g = 0; g < kG; ++g) {
-      qsum[t][g] = 0.f;
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const u32x4 y = load16(src + 64 * g + 16 * g4 + 8 * w);
-        q[t][2 * g + w] = as_bf16x8(y);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          qsum[t][g] += __uint_as_float(y[i] << 16) + __uint_as_float(y[i] & 0xffff0000u);
-      }
-      qsum[t][g] += wave_xor(qsum[t][g], 16);
-      qsum[t][g] += wave_xor(qsum[t][g], 32);
-      st.corr[t][g] = 0.f;
-    }
-    st.l[t] = 0.f;
-    st.m[t] = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) st.o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
   const int pages = (x.kv_len + 15) / 16;
   const int32_t* table = a.tables + (size_t)x.s * a.max_blocks;
   const size_t stride = (size_t)a.hkv * P::kBytes;
   const char* kc = (const char*)a.k_cache + (size_t)h * P::kBytes;
   const char* vc = (const char*)a.v_cache + (size_t)h * P::kBytes;
-  Kv4Regs<D> r[2];
-  auto load = [&](int b) {
+  const int k_at = l16 * (D / 2) + g4 * (D / 8), v_at = (l16 * 16 + 4 * g4) * (D / 32);
+  Kv4Half<D> k, v;
+  size_t id[2];
+  auto find = [&](int blk) {               // (behind the last page: that one again)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {          // (behind the last page: that one again)
-      const size_t id = (size_t)table[min(2 * b + j, pages - 1)] * stride;
-      kv4_load<D>(r[j], kc + id, vc + id, lane);
-    }
+    for (int j = 0; j < 2; ++j) id[j] = (size_t)table[min(2 * blk + j, pages - 1)] * stride;
   };
-  int b = x.b0 + wave_id();
-  if (b < x.b1) load(b);
-  for (; b < x.b1; b += kQWaves) {
+  auto load_k = [&] {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) k.load(j, kc + id[j], k_at, g4);
+  };
+  auto load_v = [&] {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) v.load(j, vc + id[j], v_at, g4);
+  };
+  if (b < x.b1) {
+    find(b);
+    load_k();
+    load_v();
+  }
+
+  const int pair = min(pair0 + l16, pairs - 1), row = pair / group;
+  const int last = x.kv_len - x.rows + row;        // the last key that the lane's column sees
+  const bf16_t* src = (const bf16_t*)a.q + ((size_t)(x.qb + row) * a.hq + h * group + pair % group) * D;
+  bf16x8 q[2 * kG];
+  float qsum[kG];
+#pragma unroll
+  for (int g = 0; g < kG; ++g) {
+    qsum[g] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const u32x4 y = load16(src + 64 * g + 16 * g4 + 8 * w);
+      q[2 * g + w] = as_bf16x8(y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        qsum[g] += __uint_as_float(y[i] << 16) + __uint_as_float(y[i] & 0xffff0000u);
+    }
+    qsum[g] += wave_xor(qsum[g], 16);
+    qsum[g] += wave_xor(qsum[g], 32);
+    st.corr[g] = 0.f;
+  }
+  st.l = 0.f;
+  st.m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (; b < x.b1; b += step) {
     const int key0 = kQKeys * b;
+    const bool more = b + step < x.b1;
+    if (more) find(b + step);
     // ---- S^T = K Q^T ---------------------------------------------------------------
-    f32x4 sc[T][2];
+    float sc[8];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int g = 0; g < kG; ++g) {
-        f32x4 acc[T];
-#pragma unroll
-        for (int t = 0; t < T; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          const bf16x8 k = kv4_operand(r[j].k[2 * g + w]);
-#pragma unroll
-          for (int t = 0; t < T; ++t) acc[t] = mfma16(k, q[t][2 * g + w], acc[t]);
+          const uint32_t y = k.c[j][2 * g + w];
+          acc = mfma16(kv4_operand(kv4_pair(y, 0), kv4_pair(y, 1), kv4_pair(y, 2), kv4_pair(y, 3)),
+                       q[2 * g + w], acc);
         }
 #pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float s = kv4_scale(r[j].kp[g][i]);
-            const float y = fmaf(-kv4_zero(r[j].kp[g][i]), qsum[t][g], acc[t][i]);
-            sc[t][j][i] = g == 0 ? s * y : fmaf(s, y, sc[t][j][i]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          const float s = kv4_scale(k.p[j][g][i]);
+          const float y = fmaf(-kv4_zero(k.p[j][g][i]), qsum[g], acc[i]);
+          sc[4 * j + i] = g == 0 ? s * y : fmaf(s, y, sc[4 * j + i]);
+        }
       }
-    // ---- values of this block, the next block's loads -------------------------------
-    uint32_t v[2][2 * kG];
-    u32x4 vp[2][kG];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-#pragma unroll
-      for (int i = 0; i < 2 * kG; ++i) v[j][i] = r[j].v[i];
-#pragma unroll
-      for (int g = 0; g < kG; ++g) vp[j][g] = r[j].vp[g];
-    }
-    if (b + kQWaves < x.b1) load(b + kQWaves);
+    if (more) load_k();
     // ---- masks: keys that a row does not see, and slots behind the last key -----------
     const bool masked = key0 + kQKeys > x.kv_len - x.rows + 1;
     if (masked) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int i = 0; i < 8; ++i) {
+        const int key = key0 + 16 * (i / 4) + 4 * g4 + i % 4;
+        if (key > last) {                  // (its parameters may be NaN)
+          sc[i] = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = key0 + 16 * j + 4 * g4 + i;
-#pragma unroll
-          for (int t = 0; t < T; ++t)
-            if (key > last[t]) sc[t][j][i] = -INFINITY;
-          if (key >= x.kv_len) {
-#pragma unroll
-            for (int g = 0; g < kG; ++g) vp[j][g][i] = 0;
-          }
+          for (int g = 0; g < kG; ++g) v.p[i / 4][g][i % 4] = 0;
         }
+      }
     }
     // ---- softmax ------------------------------------------------------------------------
-    bf16x8 pf[T][kG];
+    float top = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      float top = -INFINITY;
+    for (int i = 0; i < 8; ++i) {
+      sc[i] *= c;
+      top = fmaxf(top, sc[i]);
+    }
+    top = fmaxf(top, wave_xor(top, 16));
+    top = fmaxf(top, wave_xor(top, 32));
+    if (wave_any(top > st.m + kRescaleLog2)) {
+      const float m = fmaxf(st.m, top);
+      const float alpha = st.m == -INFINITY ? 0.f : fast_exp2(st.m - m);
+      st.l *= alpha;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int i = 0; i < D / 16; ++i) st.o[i] *= alpha;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sc[t][j][i] *= c;
-          top = fmaxf(top, sc[t][j][i]);
-        }
-      top = fmaxf(top, wave_xor(top, 16));
-      top = fmaxf(top, wave_xor(top, 32));
-      if (wave_any(top > st.m[t] + kRescaleLog2)) {
-        const float m = fmaxf(st.m[t], top);
-        const float alpha = st.m[t] == -INFINITY ? 0.f : fast_exp2(st.m[t] - m);
-        st.l[t] *= alpha;
+      for (int g = 0; g < kG; ++g) st.corr[g] *= alpha;
+      st.m = m;
+    }
+    const float ref = st.m == -INFINITY ? 0.f : st.m;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) st.o[t][i] *= alpha;
-#pragma unroll
-        for (int g = 0; g < kG; ++g) st.corr[t][g] *= alpha;
-        st.m[t] = m;
-      }
-      const float ref = st.m[t] == -INFINITY ? 0.f : st.m[t];
-      float p[8];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[4 * j + i] = fast_exp2(sc[t][j][i] - ref);
-          st.l[t] += p[4 * j + i];
-        }
-#pragma unroll
-      for (int g = 0; g < kG; ++g) {
-        float y[8], zz[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y[i] = p[i] * kv4_scale(vp[i / 4][g][i % 4]);
-          zz[i] = kv4_zero(vp[i / 4][g][i % 4]);
-        }
-        if (masked) {                      // (parameters of a key not seen may be NaN)
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (key0 + 16 * (i / 4) + 4 * g4 + i % 4 > last[t]) y[i] = zz[i] = 0.f;
-        }
-        pf[t][g] = to_bf16x8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
-        const u32x4 bits = as_u32x4(pf[t][g]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float rounded = __uint_as_float(i % 2 ? bits[i / 2] & 0xffff0000u : bits[i / 2] << 16);
-          st.corr[t][g] = fmaf(rounded, zz[i], st.corr[t][g]);
-        }
-      }
+    for (int i = 0; i < 8; ++i) {
+      sc[i] = fast_exp2(sc[i] - ref);
+      st.l += sc[i];
     }
     // ---- O^T += V^T P^T ---------------------------------------------------------------------
 #pragma unroll
     for (int g = 0; g < kG; ++g) {
-      uint32_t y[4];                       // two keys' units of group g each
+      float y[8];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int i = 0; i < 8; ++i) y[i] = sc[i] * kv4_scale(v.p[i / 4][g][i % 4]);
+      const bf16x8 pf = to_bf16x8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
+      const u32x4 bits = as_u32x4(pf);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if constexpr (kG == 1)
-            y[2 * j + i] = v[j][i];
-          else
-            y[2 * j + i] = __builtin_amdgcn_perm(v[j][2 * i + 1], v[j][2 * i],
-                                                 g == 0 ? 0x05040100u : 0x07060302u);
-        }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const u32x4 w = {kv4_pair(y[0], e), kv4_pair(y[1], e), kv4_pair(y[2], e), kv4_pair(y[3], e)};
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-          st.o[t][4 * g + e] = mfma16(as_bf16x8(w), pf[t][g], st.o[t][4 * g + e]);
+      for (int i = 0; i < 8; ++i) {
+        const float rounded = __uint_as_float(i % 2 ? bits[i / 2] & 0xffff0000u : bits[i / 2] << 16);
+        st.corr[g] = fmaf(rounded, kv4_zero(v.p[i / 4][g][i % 4]), st.corr[g]);
       }
+      uint32_t w[4];                       // two keys' units of group g each
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kG == 1)
+          w[i] = v.c[i / 2][i % 2];
+        else
+          w[i] = __builtin_amdgcn_perm(v.c[i / 2][i % 2 * 2 + 1], v.c[i / 2][i % 2 * 2],
+                                       g == 0 ? 0x05040100u : 0x07060302u);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        st.o[4 * g + e] = mfma16(kv4_operand(kv4_pair(w[0], e), kv4_pair(w[1], e), kv4_pair(w[2], e),
+                                             kv4_pair(w[3], e)),
+                                 pf, st.o[4 * g + e]);
     }
+    if (more) load_v();
   }
+  st.l += wave_xor(st.l, 16);
+  st.l += wave_xor(st.l, 32);
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    st.l[t] += wave_xor(st.l[t], 16);
-    st.l[t] += wave_xor(st.l[t], 32);
+  for (int g = 0; g < kG; ++g) {
+    st.corr[g] += wave_xor(st.corr[g], 16);
+    st.corr[g] += wave_xor(st.corr[g], 32);
 #pragma unroll
-    for (int g = 0; g < kG; ++g) {
-      st.corr[t][g] += wave_xor(st.corr[t][g], 16);
-      st.corr[t][g] += wave_xor(st.corr[t][g], 32);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) st.o[t][4 * g + e] -= st.corr[t][g];
-    }
+    for (int e = 0; e < 4; ++e) st.o[4 * g + e] -= st.corr[g];
   }
 }
 
 // Join of a cut tile's pieces: piece p's partials are at place 2 (first + p), + 1 for p = 0.
-template <int D, int C>
+template <int D>
 __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, int h) {
+  const int C = a.cols;
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
-  const int have = min(C, x.rows * group - x.tile * C);
+  const int have = min(kQPairs, x.rows * group - x.tile * kQPairs);
   auto place = [&](int p) { return ((size_t)(2 * (x.first + p) + (p == 0)) * a.hkv + h) * C; };
   for (int i = threadIdx.x >> 6; i < have; i += kQWaves) {
     const float lse = lane < x.n ? load_coherent(a.part_lse + place(lane) + i) : -INFINITY;
@@ -422,7 +378,7 @@ __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, in
       for (int e = 0; e < kPer; ++e) acc[e] += wp == 0.f ? 0.f : wp * y[e];
     }
     const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
-    const int pair = x.tile * C + i;
+    const int pair = x.tile * kQPairs + i;
     bf16_t* o = (bf16_t*)a.o + ((size_t)(x.qb + pair / group) * a.hq + h * group + pair % group) * D;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
@@ -432,59 +388,55 @@ __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, in
   }
 }
 
-template <int D, int T, class Lds>
-__device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, int h, Lds& lds) {
-  constexpr int kPer = D / 64, C = 16 * T;
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = threadIdx.x >> 6;
-  const int group = a.hq / a.hkv, pairs = x.rows * group;
-  Kv4State<D, T> st;
-  kv4_blocks_of_wave<D, T>(a, x, h, st);
-#pragma unroll
-  for (int t = 0; t < T; ++t) {            // the waves' states, a column tile at a time
-    if ((x.tile * T + t) * 16 >= pairs) break;
-    __syncthreads();
+template <int D>
+__device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, int h, Kv4Lds<D>& lds) {
+  constexpr int kPer = D / 64;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
+  const int group = a.hq / a.hkv, pair0 = x.tile * kQPairs, have = min(x.rows * group - pair0, kQPairs);
+  // the waves: `side` column tiles of 16 pairs beside each other
+  const int side = have <= 16 ? 1 : have <= 32 ? 2 : 4, mine = wave % side;
+  if (16 * mine < have) {
+    Kv4State<D> st;
+    kv4_wave<D>(a, x, h, pair0 + 16 * mine, x.b0 + wave / side, kQWaves / side, st);
+    // (the last piece's readers are behind kv4_find's barrier)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        lds.o[wave][l16][64 * (i / 4) + 4 * (4 * g4 + r) + i % 4] = st.o[t][i][r];
+        lds.o[wave][l16][64 * (i / 4) + 4 * (4 * g4 + r) + i % 4] = st.o[i][r];
     if (g4 == 0) {
-      lds.m[wave][l16] = st.m[t];
-      lds.l[wave][l16] = st.l[t];
+      lds.m[wave][l16] = st.m;
+      lds.l[wave][l16] = st.l;
     }
-    __syncthreads();
-    for (int i = wave; i < 16; i += kQWaves) {
-      const int pair = (x.tile * T + t) * 16 + i;
-      if (pair >= pairs) break;
-      float top = -INFINITY, sum = 0.f, acc[kPer] = {};
+  }
+  __syncthreads();
+  for (int i = wave; i < have; i += kQWaves) {
+    const int pair = pair0 + i, row = i % 16;
+    float top = -INFINITY, sum = 0.f, acc[kPer] = {};
+    for (int w = i / 16; w < kQWaves; w += side) top = fmaxf(top, lds.m[w][row]);
+    for (int w = i / 16; w < kQWaves; w += side) {
+      const float m = lds.m[w][row], f = m == -INFINITY ? 0.f : fast_exp2(m - top);
+      sum += m == -INFINITY ? lds.l[w][row] : f * lds.l[w][row];
 #pragma unroll
-      for (int w = 0; w < kQWaves; ++w) top = fmaxf(top, lds.m[w][i]);
+      for (int e = 0; e < kPer; ++e) acc[e] += f * lds.o[w][row][lane * kPer + e];
+    }
+    // (a sum that is NaN, from keys that are, stays: the row is NaN)
+    const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+    if (x.n == 1) {
+      bf16_t* o = (bf16_t*)a.o + ((size_t)(x.qb + pair / group) * a.hq + h * group + pair % group) * D;
 #pragma unroll
-      for (int w = 0; w < kQWaves; ++w) {
-        const float f = lds.m[w][i] == -INFINITY ? 0.f : fast_exp2(lds.m[w][i] - top);
-        sum += lds.m[w][i] == -INFINITY ? lds.l[w][i] : f * lds.l[w][i];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] += f * lds.o[w][i][lane * kPer + e];
+      for (int e = 0; e < kPer; ++e) {
+        const __bf16 y = (__bf16)(acc[e] * inv);
+        o[lane * kPer + e] = __builtin_bit_cast(bf16_t, y);
       }
-      // (a sum that is NaN, from keys that are, stays: the row is NaN)
-      const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
-      if (x.n == 1) {
-        bf16_t* o = (bf16_t*)a.o +
-                    ((size_t)(x.qb + pair / group) * a.hq + h * group + pair % group) * D;
+    } else {
+      const size_t at = ((size_t)(2 * (x.first + x.p) + (x.p == 0)) * a.hkv + h) * a.cols + i;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          const __bf16 y = (__bf16)(acc[e] * inv);
-          o[lane * kPer + e] = __builtin_bit_cast(bf16_t, y);
-        }
-      } else {
-        const size_t at = ((size_t)(2 * (x.first + x.p) + (x.p == 0)) * a.hkv + h) * C + 16 * t + i;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) store_coherent(a.part_o + at * D + lane * kPer + e, acc[e] * inv);
-        if (lane == 0)
-          store_coherent(a.part_lse + at, sum > 0.f   ? top + __log2f(sum)
-                                          : sum == sum ? -INFINITY
-                                                       : sum);
-      }
+      for (int e = 0; e < kPer; ++e) store_coherent(a.part_o + at * D + lane * kPer + e, acc[e] * inv);
+      if (lane == 0)
+        store_coherent(a.part_lse + at, sum > 0.f   ? top + __log2f(sum)
+                                        : sum == sum ? -INFINITY
+                                                     : sum);
     }
   }
   if (x.n == 1) return;
@@ -497,33 +449,34 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
     lds.flag = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (lds.flag != x.n - 1) return;
-  kv4_join<D, C>(a, x, h);
+  kv4_join<D>(a, x, h);
   if (threadIdx.x == 0) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-template <int D, int T>
-__global__ __launch_bounds__(64 * kQWaves, T > 2 ? 1 : 2) void kv4_decode_kernel(Kv4Args a) {
-  __shared__ Kv4Lds<D, T> lds;
-  constexpr int C = 16 * T;
+#ifndef OCC
+#define OCC 2
+#endif
+template <int D>
+__global__ __launch_bounds__(64 * kQWaves, OCC) void kv4_decode_kernel(Kv4Args a) {
+  __shared__ Kv4Lds<D> lds;
+  const int h = blockIdx.x % a.hkv, unit = blockIdx.x / a.hkv;
   if (a.units == 0) {                      // a workgroup for each tile
-    const int h = blockIdx.x % a.hkv, u = blockIdx.x / a.hkv;
     Kv4Piece x{};
-    x.s = u / a.tiles;
-    x.tile = u % a.tiles;
+    x.s = unit / a.tiles;
+    x.tile = unit % a.tiles;
     kv4_sequence(a, x.s, x.qb, x.rows, x.kv_len);
-    if (x.tile * C >= x.rows * (a.hq / a.hkv)) return;
+    if (x.tile * kQPairs >= x.rows * (a.hq / a.hkv)) return;
     x.b1 = kv4_blocks(x.kv_len);
     x.n = 1;
-    kv4_piece<D, T>(a, x, h, lds);
+    kv4_piece<D>(a, x, h, lds);
     return;
   }
-  const int h = blockIdx.x % a.hkv, unit = blockIdx.x / a.hkv;
   Kv4Plan plan;
-  kv4_plan<C>(a, lds, plan);
+  kv4_plan(a, lds, plan);
   for (int at = 0;;) {
     const Kv4Piece x = kv4_find(a, lds, plan, unit, at);
     if (x.s < 0) return;
-    kv4_piece<D, T>(a, x, h, lds);
+    kv4_piece<D>(a, x, h, lds);
     at = x.next;
   }
 }
@@ -533,8 +486,8 @@ __global__ __launch_bounds__(64 * kQWaves, T > 2 ? 1 : 2) void kv4_decode_kernel
 Kv4Shape kv4_shape(int num_seqs, int max_rows, int hq, int hkv, int max_blocks) {
   const int64_t pairs = (int64_t)max_rows * (hq / hkv);
   Kv4Shape t;
-  t.cols = pairs <= 16 ? 16 : pairs <= 32 ? 32 : 64;
-  t.tiles = (int)((pairs + t.cols - 1) / t.cols);
+  t.cols = (int)std::min<int64_t>(pairs, kQPairs);
+  t.tiles = (int)((pairs + kQPairs - 1) / kQPairs);
   t.units = num_seqs <= kKv4PlanSeqs ? std::max(kQWorkgroups / hkv, 1) : 0;
   // (counters; places among all blocks are counted in 32 bits)
   if ((int64_t)t.units * hkv > kKv4Counters ||
@@ -547,26 +500,12 @@ int64_t kv4_grid(const Kv4Shape& t, int num_seqs, int hkv) {
   return t.units > 0 ? (int64_t)t.units * hkv : (int64_t)num_seqs * t.tiles * hkv;
 }
 
-namespace {
-
-template <int D>
-void launch_kv4_d(const Kv4Args& a, const Kv4Shape& t, hipStream_t stream) {
-  const dim3 grid((unsigned)kv4_grid(t, a.num_seqs, a.hkv)), block(64 * kQWaves);
-  if (t.cols == 16)
-    kv4_decode_kernel<D, 1><<<grid, block, 0, stream>>>(a);
-  else if (t.cols == 32)
-    kv4_decode_kernel<D, 2><<<grid, block, 0, stream>>>(a);
-  else
-    kv4_decode_kernel<D, 4><<<grid, block, 0, stream>>>(a);
-}
-
-}  // namespace
-
 hipError_t launch_kv4(const Kv4Args& a, const Kv4Shape& t, hipStream_t stream) {
+  const dim3 grid((unsigned)kv4_grid(t, a.num_seqs, a.hkv)), block(64 * kQWaves);
   if (a.d == 64)
-    launch_kv4_d<64>(a, t, stream);
+    kv4_decode_kernel<64><<<grid, block, 0, stream>>>(a);
   else
-    launch_kv4_d<128>(a, t, stream);
+    kv4_decode_kernel<128><<<grid, block, 0, stream>>>(a);
   return hipGetLastError();
 }
 

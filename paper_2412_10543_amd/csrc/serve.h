@@ -50,10 +50,10 @@ struct Kv4Args {
   const int32_t* cu_q;          // null: one row a sequence
   int num_seqs, max_rows, max_blocks, hq, hkv, d;
   float scale;
-  int tiles = 1;                // row tiles of a sequence and kv head, at most
+  int cols = 0, tiles = 1;      // pairs of a tile, row tiles of a sequence and kv head, at most
   int units = 0;                // workgroups of a kv head that share all keys; 0: nothing is cut
-  float* part_o = nullptr;      // [2 units][hkv][rows of a tile][d]
-  float* part_lse = nullptr;    // [2 units][hkv][rows of a tile]
+  float* part_o = nullptr;      // [2 units][hkv][cols][d]
+  float* part_lse = nullptr;    // [2 units][hkv][cols]
   int* arrivals = nullptr;      // [units][hkv]
 };
 

@@ -361,6 +361,7 @@ rag_status rag_attn_decode_paged_kv4(const void* q, const void* k_cache, const v
   rag::Kv4Args a{q,        k_cache,      v_cache,            o,           block_tables,
                  kv_lens,  cu_seqlens_q, num_seqs,           max_seqlen_q, max_blocks_per_seq,
                  num_q_heads, num_kv_heads, head_dim,        softmax_scale};
+  a.cols = t.cols;
   a.tiles = t.tiles;
   a.units = t.units;
   if (rag::kv4_grid(t, num_seqs, num_kv_heads) > INT_MAX)
