@@ -47,6 +47,15 @@ __device__ __forceinline__ float kv4_zero(uint32_t p) { return __uint_as_float(p
 __device__ __forceinline__ uint32_t kv4_pair(uint32_t w, int p) {
   return ((w >> (4 * p)) & kKv4Ones) | kKv4Magic;
 }
+// The same as a shift and one v_and_or_b32, for loops: that takes one constant from a scalar
+// register, so that the other one has to be in a vector register.
+struct Kv4Unpack {
+  uint32_t ones = kKv4Ones, magic = kKv4Magic;
+  __device__ __forceinline__ Kv4Unpack() { asm("" : "+s"(ones), "+v"(magic)); }
+  __device__ __forceinline__ uint32_t operator()(uint32_t w, int p) const {
+    return ((w >> (4 * p)) & ones) | magic;
+  }
+};
 
 // Scale and zero point of a group from its lowest and highest value (0 counted in):
 // s = (hi - lo) / 15 rounded to bf16 (formed from halves, which do not overflow),

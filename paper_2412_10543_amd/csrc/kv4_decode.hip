@@ -7,12 +7,16 @@
 // so that both products take the codes as they are (the bf16 numbers 128 + c, two
 // by one shift and one and-or), on v_mfma_f32_16x16x32_bf16: S^T = K Q^T with the
 // (row, q head) pairs of a kv head as the 16 columns, then O^T = V^T P^T, whose B
-// operand the lanes hold already.  Sums, maxima and the corrections are fp32; p' is
-// rounded to bf16 for the matrix unit, as P is in the bf16 cache's kernels, and the
-// correction uses the rounded p', so that 128 cancels.
+// operand the lanes hold already.  The corrections are products too: 128 + z is a bf16
+// number, sum q three of them (24 bits), and the second is the same P^T under one more
+// row.  Sums and maxima are fp32; p' is rounded to bf16 for the matrix unit, as P is in the
+// bf16 cache's kernels, and the correction uses the rounded p', so that 128 cancels.
 //
-// A wave takes blocks of two pages (32 keys) straight into registers, one 16-byte load
-// for a page's K codes and one for its V codes, for 16 pairs.  A workgroup's four waves take
+// A wave takes blocks of two pages (32 keys), two blocks ahead, straight into registers, one
+// 16-byte load for a page's K codes and one for its V codes, for 16 pairs.  Parameters come
+// with one load of their lines and reach the lanes that need them through LDS: loads of a line
+// that is still on its way hold up all loads behind them (64 sequences of 2.6k to 10.3k keys:
+// 113 us with the lines read where they are needed).  A workgroup's four waves take
 // every fourth block each, for up to 16 pairs; every second, two and two, for 32; or all four
 // each block for 64, which then reaches them through the CU's cache.  They join their states
 // through LDS.  As many workgroups as
@@ -22,6 +26,8 @@
 #include "common.h"
 #include "kv4.h"
 #include "serve.h"
+
+#include <type_traits>
 
 namespace rag {
 
@@ -43,15 +49,17 @@ struct Kv4Piece {
   int next;                     // where in the unit's share the next piece starts
 };
 
-// What all sequences have: each thread four of them, in order.
+// All sequences' blocks and the workgroups' shares of them.
 struct Kv4Plan {
-  int start[4], len[4], tiles[4], total, share;
+  int total, share;
 };
 
 template <int D>
 struct Kv4Lds {
   float o[kQWaves][16][D + 4];
   float m[kQWaves][16], l[kQWaves][16];
+  uint32_t params[kQWaves][D];
+  int start[kKv4PlanSeqs], span[kKv4PlanSeqs], len[kKv4PlanSeqs];   // (a thread's own four each)
   int wave_sum[kQWaves], longest[kQWaves], flag;
   Kv4Piece piece;
 };
@@ -83,16 +91,18 @@ __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& pl
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int s = threadIdx.x * 4 + i;
-    plan.len[i] = plan.tiles[i] = 0;
+    int tiles = 0, len = 0;
     if (s < a.num_seqs) {
       int qb, rows, kv;
       kv4_sequence(a, s, qb, rows, kv);
-      plan.tiles[i] = (max(rows, 0) * group + kQPairs - 1) / kQPairs;
-      plan.len[i] = kv4_blocks(kv) + kQStart;
+      tiles = (max(rows, 0) * group + kQPairs - 1) / kQPairs;
+      len = kv4_blocks(kv) + kQStart;
     }
-    plan.start[i] = sum;
-    sum += plan.tiles[i] * plan.len[i];
-    if (plan.tiles[i] > 0) longest = max(longest, plan.len[i]);
+    lds.start[s] = sum;
+    lds.span[s] = tiles * len;
+    lds.len[s] = len;
+    sum += tiles * len;
+    if (tiles > 0) longest = max(longest, len);
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int upto = wave_scan(sum);
@@ -113,7 +123,7 @@ __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& pl
     longest = max(longest, lds.longest[w]);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) plan.start[i] += before;
+  for (int i = 0; i < 4; ++i) lds.start[threadIdx.x * 4 + i] += before;
   // (a tile is cut into at most kQMaxPieces)
   plan.share = max(max((plan.total + a.units - 1) / a.units, kQMinBlocks),
                    (longest + kQMaxPieces - 3) / (kQMaxPieces - 2));
@@ -132,12 +142,12 @@ __device__ __forceinline__ Kv4Piece kv4_find(const Kv4Args& a, Lds& lds, const K
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int off = g - plan.start[i];
-    if (off >= 0 && off < plan.tiles[i] * plan.len[i]) {
+    const int s = threadIdx.x * 4 + i, off = g - lds.start[s];
+    if (off >= 0 && off < lds.span[s]) {
       Kv4Piece x;
-      x.s = threadIdx.x * 4 + i;
-      x.tile = off / plan.len[i];
-      const int t0 = plan.start[i] + x.tile * plan.len[i], t1 = t0 + plan.len[i];
+      x.s = s;
+      x.tile = off / lds.len[s];
+      const int t0 = lds.start[s] + x.tile * lds.len[s], t1 = t0 + lds.len[s];
       x.b0 = max(g - t0 - kQStart, 0);
       x.b1 = max(min(to, t1) - t0 - kQStart, 0);
       x.first = t0 / plan.share;
@@ -149,53 +159,79 @@ __device__ __forceinline__ Kv4Piece kv4_find(const Kv4Args& a, Lds& lds, const K
     }
   }
   __syncthreads();
-  return lds.piece;
+  // (the same for all lanes, which the compiler is to know: scalar registers and loads)
+  Kv4Piece x;
+  const int* src = reinterpret_cast<const int*>(&lds.piece);
+  int* dst = reinterpret_cast<int*>(&x);
+#pragma unroll
+  for (size_t i = 0; i < sizeof(x) / sizeof(int); ++i) dst[i] = __builtin_amdgcn_readfirstlane(src[i]);
+  return x;
 }
 
-// Half of a block (K or V) as a lane has it: of two pages the codes, words (g, w) of key l16 or V
-// units of keys 4 g4 .., and the parameters of keys 4 g4 .. 4 g4 + 3.
+// A block on its way, as a lane has it: of two pages the words (g, w) of key l16 (K), the units of
+// keys 4 g4 .. (V), and a share of the parameters.
 template <int D>
-struct Kv4Half {
-  uint32_t c[2][D / 32];
-  u32x4 p[2][D / 64];
-  __device__ __forceinline__ void load(int j, const char* page, int code_at, int g4) {
-    if constexpr (D == 128) {
-      const u32x4 y = load16_stream(page + code_at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c[j][i] = y[i];
-    } else {
-      const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(page + code_at));
-      c[j][0] = y[0];
-      c[j][1] = y[1];
-    }
-#pragma unroll
-    for (int g = 0; g < D / 64; ++g) p[j][g] = load16(page + Kv4Page<D>::param(4 * g4, g));
-  }
+struct Kv4Block {
+  uint32_t k[2][D / 32], v[2][D / 32], p[D / 64];
 };
+
+template <int N>
+__device__ __forceinline__ void kv4_load(uint32_t (&x)[N], const char* p) {
+  if constexpr (N == 4) {
+    const u32x4 y = load16_stream(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = y[i];
+  } else {
+    const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+    x[0] = y[0];
+    x[1] = y[1];
+  }
+}
+
+// Parameters of a block in LDS: [page][K, V][group][token].
+template <int D>
+__device__ __forceinline__ constexpr int kv4_place(int j, int values, int g) {
+  return ((2 * j + values) * (D / 64) + g) * 16;
+}
 
 __device__ __forceinline__ bf16x8 kv4_operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   const u32x4 x = {a, b, c, d};
   return as_bf16x8(x);
 }
 
-// A wave's state of 16 (row, q head) pairs: O^T without its corrections, the corrections (this
-// lane's keys' share), the sum of weights and the maximum that they refer to (scores times
-// scale log2 e).
+// p[i], i the same for the wave, of memory that the kernel does not write.
+__device__ __forceinline__ int kv4_uniform(const int32_t* p, int i) {
+  typedef __attribute__((address_space(4))) const int32_t const_i32;
+  return ((const_i32*)p)[i];
+}
+
+// A wave's state of 16 (row, q head) pairs: O^T without its corrections, the corrections, the
+// sum of weights (this lane's keys' share) and the maximum that they refer to.
 template <int D>
 struct Kv4State {
   f32x4 o[D / 16];              // [4 g + e]: channels 64 g + 4 (4 g4 + r) + e
-  float corr[D / 64], l, m;
+  f32x4 corr[D / 64];           // (the same in all rows)
+  float l, m;
 };
+
+// Maximum over the four lanes of a column (lanes l16 + 16 g4).
+__device__ __forceinline__ float column_max(float x) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
 
 // Pairs pair0 .. pair0 + 15 against blocks b, b + step, .. below b1.
 template <int D>
 __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, int h, int pair0, int b,
-                                         int step, Kv4State<D>& st) {
+                                         int step, uint32_t* params, Kv4State<D>& st) {
   constexpr int kG = D / 64;
   using P = Kv4Page<D>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
   const int group = a.hq / a.hkv, pairs = x.rows * group;
-  const float c = a.scale * kLog2e;
+  const float c = a.scale * kLog2e, tau = kRescaleLog2 / c;
+  const Kv4Unpack unpack;
 
   const int pages = (x.kv_len + 15) / 16;
   const int32_t* table = a.tables + (size_t)x.s * a.max_blocks;
@@ -203,101 +239,134 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
   const char* kc = (const char*)a.k_cache + (size_t)h * P::kBytes;
   const char* vc = (const char*)a.v_cache + (size_t)h * P::kBytes;
   const int k_at = l16 * (D / 2) + g4 * (D / 8), v_at = (l16 * 16 + 4 * g4) * (D / 32);
-  Kv4Half<D> k, v;
+  Kv4Block<D> buf[2];
+  // Behind the wave's last block that one is requested again (and found in the caches), so that
+  // the loop has no branches around its loads.  Page ids come through the scalar cache, a block
+  // before they are used: a vector load of theirs would wait for all loads before it.
+  const int end = x.b1 > b ? b + (x.b1 - 1 - b) / step * step : b;
+  int next[2];
   size_t id[2];
   auto find = [&](int blk) {               // (behind the last page: that one again)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) id[j] = (size_t)table[min(2 * blk + j, pages - 1)] * stride;
+    for (int j = 0; j < 2; ++j) next[j] = kv4_uniform(table, min(2 * min(blk, end) + j, pages - 1));
   };
-  auto load_k = [&] {
+  auto found = [&] {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) k.load(j, kc + id[j], k_at, g4);
+    for (int j = 0; j < 2; ++j) id[j] = (size_t)next[j] * stride;
   };
-  auto load_v = [&] {
+  // the lane's parameters: word lane (and 64 + lane) of [page][K, V][group][token]
+  const char* pc = (lane / (16 * kG) % 2 ? vc : kc) + P::kParams + lane % (16 * kG) * 4;
+  auto load_k = [&](Kv4Block<D>& r) {
+    if constexpr (kG == 2) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) v.load(j, vc + id[j], v_at, g4);
+      for (int j = 0; j < 2; ++j) r.p[j] = *reinterpret_cast<const uint32_t*>(pc + id[j]);
+    } else {
+      r.p[0] = *reinterpret_cast<const uint32_t*>(pc + (lane < 32 ? id[0] : id[1]));
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) kv4_load(r.k[j], kc + id[j] + k_at);
+  };
+  auto load_v = [&](Kv4Block<D>& r) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) kv4_load(r.v[j], vc + id[j] + v_at);
   };
   if (b < x.b1) {
-    find(b);
-    load_k();
-    load_v();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      find(b + i * step);
+      found();
+      load_k(buf[i]);
+      load_v(buf[i]);
+    }
+    find(b + 2 * step);
   }
 
   const int pair = min(pair0 + l16, pairs - 1), row = pair / group;
   const int last = x.kv_len - x.rows + row;        // the last key that the lane's column sees
   const bf16_t* src = (const bf16_t*)a.q + ((size_t)(x.qb + row) * a.hq + h * group + pair % group) * D;
   bf16x8 q[2 * kG];
-  float qsum[kG];
+  bf16x8 qz[kG];                           // minus the sum of q, in three parts
 #pragma unroll
   for (int g = 0; g < kG; ++g) {
-    qsum[g] = 0.f;
+    float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       const u32x4 y = load16(src + 64 * g + 16 * g4 + 8 * w);
       q[2 * g + w] = as_bf16x8(y);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        qsum[g] += __uint_as_float(y[i] << 16) + __uint_as_float(y[i] & 0xffff0000u);
+        sum += __uint_as_float(y[i] << 16) + __uint_as_float(y[i] & 0xffff0000u);
     }
-    qsum[g] += wave_xor(qsum[g], 16);
-    qsum[g] += wave_xor(qsum[g], 32);
-    st.corr[g] = 0.f;
+    sum += wave_xor(sum, 16);
+    sum += wave_xor(sum, 32);
+    const float part0 = (float)(__bf16)-sum, part1 = (float)(__bf16)(-sum - part0);
+    const float on = g4 == 0 ? 1.f : 0.f;
+    qz[g] = to_bf16x8(part0 * on, part1 * on, (-sum - part0 - part1) * on, 0.f, 0.f, 0.f, 0.f, 0.f);
+    st.corr[g] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   st.l = 0.f;
   st.m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  for (; b < x.b1; b += step) {
+  auto block = [&](Kv4Block<D>& r, auto masked_t) {
+    constexpr bool masked = decltype(masked_t)::value;
     const int key0 = kQKeys * b;
-    const bool more = b + step < x.b1;
-    if (more) find(b + step);
+    found();
+    find(b + 3 * step);
+#pragma unroll
+    for (int i = 0; i < kG; ++i) params[64 * i + lane] = r.p[i];
+    wave_lds_sync();
     // ---- S^T = K Q^T ---------------------------------------------------------------
     float sc[8];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int g = 0; g < kG; ++g) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        const uint32_t kz = params[kv4_place<D>(j, 0, g) + l16];
+        const uint32_t zz = __builtin_amdgcn_perm(kz, kz, 0x01000100u);
+        f32x4 acc = mfma16(kv4_operand(zz, zz, zz, zz), qz[g], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          const uint32_t y = k.c[j][2 * g + w];
-          acc = mfma16(kv4_operand(kv4_pair(y, 0), kv4_pair(y, 1), kv4_pair(y, 2), kv4_pair(y, 3)),
+          const uint32_t y = r.k[j][2 * g + w];
+          acc = mfma16(kv4_operand(unpack(y, 0), unpack(y, 1), unpack(y, 2), unpack(y, 3)),
                        q[2 * g + w], acc);
         }
+        const u32x4 kp = *reinterpret_cast<const u32x4*>(params + kv4_place<D>(j, 0, g) + 4 * g4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float s = kv4_scale(k.p[j][g][i]);
-          const float y = fmaf(-kv4_zero(k.p[j][g][i]), qsum[g], acc[i]);
-          sc[4 * j + i] = g == 0 ? s * y : fmaf(s, y, sc[4 * j + i]);
+          const float s = kv4_scale(kp[i]);
+          sc[4 * j + i] = g == 0 ? s * acc[i] : fmaf(s, acc[i], sc[4 * j + i]);
         }
       }
-    if (more) load_k();
+    u32x4 vp[2][kG];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int g = 0; g < kG; ++g)
+        vp[j][g] = *reinterpret_cast<const u32x4*>(params + kv4_place<D>(j, 1, g) + 4 * g4);
+    load_k(r);
     // ---- masks: keys that a row does not see, and slots behind the last key -----------
-    const bool masked = key0 + kQKeys > x.kv_len - x.rows + 1;
-    if (masked) {
+    if constexpr (masked) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = key0 + 16 * (i / 4) + 4 * g4 + i % 4;
-        if (key > last) {                  // (its parameters may be NaN)
-          sc[i] = -INFINITY;
+        if (key > last) sc[i] = -INFINITY;
 #pragma unroll
-          for (int g = 0; g < kG; ++g) v.p[i / 4][g][i % 4] = 0;
+        for (int g = 0; g < kG; ++g) {     // (zero points alike for all columns: none that is NaN)
+          const uint32_t y = key < x.kv_len ? vp[i / 4][g][i % 4] : 0;
+          vp[i / 4][g][i % 4] = (y & 0x7f80u) == 0x7f80u ? y & 0xffff0000u : y;
         }
       }
     }
     // ---- softmax ------------------------------------------------------------------------
-    float top = -INFINITY;
+    float top = sc[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sc[i] *= c;
-      top = fmaxf(top, sc[i]);
-    }
-    top = fmaxf(top, wave_xor(top, 16));
-    top = fmaxf(top, wave_xor(top, 32));
-    if (wave_any(top > st.m + kRescaleLog2)) {
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
+    top = column_max(top);
+    if (wave_any(top > st.m + tau)) {
       const float m = fmaxf(st.m, top);
-      const float alpha = st.m == -INFINITY ? 0.f : fast_exp2(st.m - m);
+      const float alpha = st.m == -INFINITY ? 0.f : fast_exp2((st.m - m) * c);
       st.l *= alpha;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) st.o[i] *= alpha;
@@ -305,10 +374,10 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
       for (int g = 0; g < kG; ++g) st.corr[g] *= alpha;
       st.m = m;
     }
-    const float ref = st.m == -INFINITY ? 0.f : st.m;
+    const float ref = st.m == -INFINITY ? 0.f : -st.m * c;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      sc[i] = fast_exp2(sc[i] - ref);
+      sc[i] = fast_exp2(fmaf(sc[i], c, ref));
       st.l += sc[i];
     }
     // ---- O^T += V^T P^T ---------------------------------------------------------------------
@@ -316,40 +385,60 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
     for (int g = 0; g < kG; ++g) {
       float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = sc[i] * kv4_scale(v.p[i / 4][g][i % 4]);
-      const bf16x8 pf = to_bf16x8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
-      const u32x4 bits = as_u32x4(pf);
+      for (int i = 0; i < 8; ++i) y[i] = sc[i] * kv4_scale(vp[i / 4][g][i % 4]);
+      if constexpr (masked) {              // (the scale of a key not seen may be NaN)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float rounded = __uint_as_float(i % 2 ? bits[i / 2] & 0xffff0000u : bits[i / 2] << 16);
-        st.corr[g] = fmaf(rounded, kv4_zero(v.p[i / 4][g][i % 4]), st.corr[g]);
+        for (int i = 0; i < 8; ++i)
+          if (key0 + 16 * (i / 4) + 4 * g4 + i % 4 > last) y[i] = 0.f;
       }
-      uint32_t w[4];                       // two keys' units of group g each
+      const bf16x8 pf = to_bf16x8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
+      uint32_t w[4], zz[4];                // two keys' units of group g, and their zero points
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        const u32x4 pr = vp[i / 2][g];
+        zz[i] = __builtin_amdgcn_perm(pr[i % 2 * 2 + 1], pr[i % 2 * 2], 0x05040100u);
         if constexpr (kG == 1)
-          w[i] = v.c[i / 2][i % 2];
+          w[i] = r.v[i / 2][i % 2];
         else
-          w[i] = __builtin_amdgcn_perm(v.c[i / 2][i % 2 * 2 + 1], v.c[i / 2][i % 2 * 2],
+          w[i] = __builtin_amdgcn_perm(r.v[i / 2][i % 2 * 2 + 1], r.v[i / 2][i % 2 * 2],
                                        g == 0 ? 0x05040100u : 0x07060302u);
       }
+      st.corr[g] = mfma16(kv4_operand(zz[0], zz[1], zz[2], zz[3]), pf, st.corr[g]);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        st.o[4 * g + e] = mfma16(kv4_operand(kv4_pair(w[0], e), kv4_pair(w[1], e), kv4_pair(w[2], e),
-                                             kv4_pair(w[3], e)),
+        st.o[4 * g + e] = mfma16(kv4_operand(unpack(w[0], e), unpack(w[1], e), unpack(w[2], e),
+                                             unpack(w[3], e)),
                                  pf, st.o[4 * g + e]);
     }
-    if (more) load_v();
+    load_v(r);
+    wave_lds_sync();                       // (the next block's parameters take the place of these)
+    b += step;
+  };
+  const int open = (x.kv_len - x.rows + 1) / kQKeys;     // blocks that all rows see whole
+  // (two loops: the compiler would make one of two variants in a loop, with the codes of a
+  // block unpacked before it knows which)
+  const int whole = min(x.b1, open);
+  while (b < whole) {
+    block(buf[0], std::false_type());
+    if (b >= whole) {
+      const Kv4Block<D> t = buf[0];
+      buf[0] = buf[1];
+      buf[1] = t;
+      break;
+    }
+    block(buf[1], std::false_type());
+  }
+  while (b < x.b1) {
+    block(buf[0], std::true_type());
+    if (b >= x.b1) break;
+    block(buf[1], std::true_type());
   }
   st.l += wave_xor(st.l, 16);
   st.l += wave_xor(st.l, 32);
 #pragma unroll
-  for (int g = 0; g < kG; ++g) {
-    st.corr[g] += wave_xor(st.corr[g], 16);
-    st.corr[g] += wave_xor(st.corr[g], 32);
+  for (int g = 0; g < kG; ++g)
 #pragma unroll
     for (int e = 0; e < 4; ++e) st.o[4 * g + e] -= st.corr[g];
-  }
 }
 
 // Join of a cut tile's pieces: piece p's partials are at place 2 (first + p), + 1 for p = 0.
@@ -395,9 +484,10 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
   const int group = a.hq / a.hkv, pair0 = x.tile * kQPairs, have = min(x.rows * group - pair0, kQPairs);
   // the waves: `side` column tiles of 16 pairs beside each other
   const int side = have <= 16 ? 1 : have <= 32 ? 2 : 4, mine = wave % side;
+  const float c = a.scale * kLog2e;
   if (16 * mine < have) {
     Kv4State<D> st;
-    kv4_wave<D>(a, x, h, pair0 + 16 * mine, x.b0 + wave / side, kQWaves / side, st);
+    kv4_wave<D>(a, x, h, pair0 + 16 * mine, x.b0 + wave / side, kQWaves / side, lds.params[wave], st);
     // (the last piece's readers are behind kv4_find's barrier)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
@@ -415,7 +505,7 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
     float top = -INFINITY, sum = 0.f, acc[kPer] = {};
     for (int w = i / 16; w < kQWaves; w += side) top = fmaxf(top, lds.m[w][row]);
     for (int w = i / 16; w < kQWaves; w += side) {
-      const float m = lds.m[w][row], f = m == -INFINITY ? 0.f : fast_exp2(m - top);
+      const float m = lds.m[w][row], f = m == -INFINITY ? 0.f : fast_exp2((m - top) * c);
       sum += m == -INFINITY ? lds.l[w][row] : f * lds.l[w][row];
 #pragma unroll
       for (int e = 0; e < kPer; ++e) acc[e] += f * lds.o[w][row][lane * kPer + e];
@@ -434,7 +524,7 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
 #pragma unroll
       for (int e = 0; e < kPer; ++e) store_coherent(a.part_o + at * D + lane * kPer + e, acc[e] * inv);
       if (lane == 0)
-        store_coherent(a.part_lse + at, sum > 0.f   ? top + __log2f(sum)
+        store_coherent(a.part_lse + at, sum > 0.f   ? top * c + __log2f(sum)
                                         : sum == sum ? -INFINITY
                                                      : sum);
     }
@@ -460,24 +550,25 @@ template <int D>
 __global__ __launch_bounds__(64 * kQWaves, OCC) void kv4_decode_kernel(Kv4Args a) {
   __shared__ Kv4Lds<D> lds;
   const int h = blockIdx.x % a.hkv, unit = blockIdx.x / a.hkv;
-  if (a.units == 0) {                      // a workgroup for each tile
-    Kv4Piece x{};
-    x.s = unit / a.tiles;
-    x.tile = unit % a.tiles;
-    kv4_sequence(a, x.s, x.qb, x.rows, x.kv_len);
-    if (x.tile * kQPairs >= x.rows * (a.hq / a.hkv)) return;
-    x.b1 = kv4_blocks(x.kv_len);
-    x.n = 1;
-    kv4_piece<D>(a, x, h, lds);
-    return;
-  }
   Kv4Plan plan;
-  kv4_plan(a, lds, plan);
+  if (a.units > 0) kv4_plan(a, lds, plan);
   for (int at = 0;;) {
-    const Kv4Piece x = kv4_find(a, lds, plan, unit, at);
-    if (x.s < 0) return;
+    Kv4Piece x;
+    if (a.units > 0) {
+      x = kv4_find(a, lds, plan, unit, at);
+      if (x.s < 0) return;
+      at = x.next;
+    } else {                               // a workgroup for each tile
+      x.s = unit / a.tiles;
+      x.tile = unit % a.tiles;
+      kv4_sequence(a, x.s, x.qb, x.rows, x.kv_len);
+      if (x.tile * kQPairs >= x.rows * (a.hq / a.hkv)) return;
+      x.b0 = x.p = x.first = 0;
+      x.b1 = kv4_blocks(x.kv_len);
+      x.n = 1;
+    }
     kv4_piece<D>(a, x, h, lds);
-    at = x.next;
+    if (a.units == 0) return;
   }
 }
 
