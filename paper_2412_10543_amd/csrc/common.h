@@ -162,6 +162,23 @@ __device__ __forceinline__ void dma16(const void* src, bf16_t* lds_dst) {
       : "memory");
 }
 
+// The same copy of 4 bytes per lane (global_load_lds_dword): lane l's land at lds_dst + 4*l.
+__device__ __forceinline__ void dma4(const void* src, void* lds_dst) {
+  typedef __attribute__((address_space(3))) char lds_char;
+  const uint32_t base =
+      __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char*)lds_dst);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, off\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(src), "s"(base)
+      : "memory");
+}
+
 // The same copy with a wave-uniform 64-bit base in SGPRs plus a per-lane
 // 32-bit byte offset (the global instruction's SADDR form): no per-lane 64-bit
 // address arithmetic.  (The instruction's immediate offset would move the LDS

@@ -12,17 +12,16 @@
 // row.  Sums and maxima are fp32; p' is rounded to bf16 for the matrix unit, as P is in the
 // bf16 cache's kernels, and the correction uses the rounded p', so that 128 cancels.
 //
-// A wave takes blocks of two pages (32 keys), two blocks ahead, straight into registers, one
-// 16-byte load for a page's K codes and one for its V codes, for 16 pairs.  Parameters come
-// with one load of their lines and reach the lanes that need them through LDS: loads of a line
-// that is still on its way hold up all loads behind them (64 sequences of 2.6k to 10.3k keys:
-// 113 us with the lines read where they are needed).  A workgroup's four waves take
-// every fourth block each, for up to 16 pairs; every second, two and two, for 32; or all four
-// each block for 64, which then reaches them through the CU's cache.  They join their states
-// through LDS.  As many workgroups as
-// the chip takes at a time get even shares of all sequences' blocks; a sequence that is
-// cut writes partial outputs and log-sum-exps, which the last of its workgroups to
-// finish joins.
+// Blocks of two pages (32 keys) are copied straight into LDS, kQStages - 1 of them ahead, with
+// 16 bytes a lane and lanes in the pages' order, parameters with a load of their lines: a load that
+// finds a line still on its way holds up all behind it (64 sequences of 2.6k to 10.3k keys: 98 us
+// with the codes loaded as the matrix operands have them, 113 with the parameters' lines read
+// where they are needed).  Each of a workgroup's four waves copies every fourth block.  Up to 16
+// pairs, each attends the blocks that it has copied; for up to 32, two and two do with 16 pairs
+// each every second block; for up to 64 all four do every block.  They join their states through
+// LDS.  As many workgroups as the chip takes at a time get even shares of all sequences' blocks;
+// a sequence that is cut writes partial outputs and log-sum-exps, which the last of its
+// workgroups to finish joins.
 #include "common.h"
 #include "kv4.h"
 #include "serve.h"
@@ -54,11 +53,26 @@ struct Kv4Plan {
   int total, share;
 };
 
+#ifndef STAGES
+#define STAGES 3
+#endif
+constexpr int kQStages = STAGES;
+
+// A block in LDS: K codes of its two pages, V codes, parameters [page][K, V][group][token].
+template <int D>
+struct Kv4Block {
+  char k[16 * D], v[16 * D];
+  uint32_t p[D];
+  static constexpr int kOps = D == 128 ? 6 : 3;      // loads that fill one
+};
+
 template <int D>
 struct Kv4Lds {
-  float o[kQWaves][16][D + 4];
+  union {
+    Kv4Block<D> ring[kQStages][kQWaves];
+    float o[kQWaves][16][D + 4];
+  };
   float m[kQWaves][16], l[kQWaves][16];
-  uint32_t params[kQWaves][D];
   int start[kKv4PlanSeqs], span[kKv4PlanSeqs], len[kKv4PlanSeqs];   // (a thread's own four each)
   int wave_sum[kQWaves], longest[kQWaves], flag;
   Kv4Piece piece;
@@ -168,30 +182,23 @@ __device__ __forceinline__ Kv4Piece kv4_find(const Kv4Args& a, Lds& lds, const K
   return x;
 }
 
-// A block on its way, as a lane has it: of two pages the words (g, w) of key l16 (K), the units of
-// keys 4 g4 .. (V), and a share of the parameters.
-template <int D>
-struct Kv4Block {
-  uint32_t k[2][D / 32], v[2][D / 32], p[D / 64];
-};
-
-template <int N>
-__device__ __forceinline__ void kv4_load(uint32_t (&x)[N], const char* p) {
-  if constexpr (N == 4) {
-    const u32x4 y = load16_stream(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = y[i];
-  } else {
-    const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-    x[0] = y[0];
-    x[1] = y[1];
-  }
-}
-
-// Parameters of a block in LDS: [page][K, V][group][token].
+// Where the parameters of a page and group stand in a block.
 template <int D>
 __device__ __forceinline__ constexpr int kv4_place(int j, int values, int g) {
   return ((2 * j + values) * (D / 64) + g) * 16;
+}
+
+template <int N>
+__device__ __forceinline__ void kv4_read(uint32_t (&x)[N], const char* p) {
+  if constexpr (N == 4) {
+    const u32x4 y = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = y[i];
+  } else {
+    const u32x2 y = *reinterpret_cast<const u32x2*>(p);
+    x[0] = y[0];
+    x[1] = y[1];
+  }
 }
 
 __device__ __forceinline__ bf16x8 kv4_operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -222,63 +229,62 @@ __device__ __forceinline__ float column_max(float x) {
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
-// Pairs pair0 .. pair0 + 15 against blocks b, b + step, .. below b1.
+// Memory and the waits around it, in the order that they are written in.
+__device__ __forceinline__ void kv4_fence() { asm volatile("" ::: "memory"); }
+
+// The wave's 16 pairs (pair0 on) against the piece's blocks, `side` waves beside each other on each
+// of them; a wave whose pairs are none copies its blocks for the others.
 template <int D>
-__device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, int h, int pair0, int b,
-                                         int step, uint32_t* params, Kv4State<D>& st) {
+__device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, int h, int pair0, int side,
+                                         Kv4Lds<D>& lds, Kv4State<D>& st) {
   constexpr int kG = D / 64;
   using P = Kv4Page<D>;
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
   const int group = a.hq / a.hkv, pairs = x.rows * group;
   const float c = a.scale * kLog2e, tau = kRescaleLog2 / c;
   const Kv4Unpack unpack;
 
+  // ---- copies ---------------------------------------------------------------------------------
   const int pages = (x.kv_len + 15) / 16;
   const int32_t* table = a.tables + (size_t)x.s * a.max_blocks;
   const size_t stride = (size_t)a.hkv * P::kBytes;
   const char* kc = (const char*)a.k_cache + (size_t)h * P::kBytes;
   const char* vc = (const char*)a.v_cache + (size_t)h * P::kBytes;
-  const int k_at = l16 * (D / 2) + g4 * (D / 8), v_at = (l16 * 16 + 4 * g4) * (D / 32);
-  Kv4Block<D> buf[2];
-  // Behind the wave's last block that one is requested again (and found in the caches), so that
-  // the loop has no branches around its loads.  Page ids come through the scalar cache, a block
-  // before they are used: a vector load of theirs would wait for all loads before it.
-  const int end = x.b1 > b ? b + (x.b1 - 1 - b) / step * step : b;
+  // The lane's 16 bytes of a page (two pages where D = 64).  D = 128: each four lanes' in an order
+  // of their own, so that 16 lanes that read every fourth piece find them in all banks.
+  const int piece = kG == 2 ? 16 * ((lane & ~3) | ((lane - g4) & 3)) : 16 * (lane & 31);
+  const char* pc = (lane / (16 * kG) % 2 ? vc : kc) + P::kParams + lane % (16 * kG) * 4;
+  // Behind the last block that one is copied again, so that the number of loads on their way is
+  // known.  Page ids come through the scalar cache, a block before they are used.
   int next[2];
-  size_t id[2];
   auto find = [&](int blk) {               // (behind the last page: that one again)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) next[j] = kv4_uniform(table, min(2 * min(blk, end) + j, pages - 1));
+    for (int j = 0; j < 2; ++j) next[j] = kv4_uniform(table, min(2 * min(blk, x.b1 - 1) + j, pages - 1));
   };
-  auto found = [&] {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) id[j] = (size_t)next[j] * stride;
-  };
-  // the lane's parameters: word lane (and 64 + lane) of [page][K, V][group][token]
-  const char* pc = (lane / (16 * kG) % 2 ? vc : kc) + P::kParams + lane % (16 * kG) * 4;
-  auto load_k = [&](Kv4Block<D>& r) {
+  auto copy = [&](int stage) {
+    Kv4Block<D>& to = lds.ring[stage][wave];
+    const size_t id0 = (size_t)next[0] * stride, id1 = (size_t)next[1] * stride;
     if constexpr (kG == 2) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) r.p[j] = *reinterpret_cast<const uint32_t*>(pc + id[j]);
+      dma16(kc + id0 + piece, (bf16_t*)to.k);
+      dma16(kc + id1 + piece, (bf16_t*)(to.k + 8 * D));
+      dma4(pc + id0, to.p);
+      dma4(pc + id1, to.p + 64);
+      dma16(vc + id0 + piece, (bf16_t*)to.v);
+      dma16(vc + id1 + piece, (bf16_t*)(to.v + 8 * D));
     } else {
-      r.p[0] = *reinterpret_cast<const uint32_t*>(pc + (lane < 32 ? id[0] : id[1]));
+      const size_t id = lane < 32 ? id0 : id1;
+      dma16(kc + id + piece, (bf16_t*)to.k);
+      dma4(pc + id, to.p);
+      dma16(vc + id + piece, (bf16_t*)to.v);
     }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) kv4_load(r.k[j], kc + id[j] + k_at);
   };
-  auto load_v = [&](Kv4Block<D>& r) {
+  if (x.b0 < x.b1) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) kv4_load(r.v[j], vc + id[j] + v_at);
-  };
-  if (b < x.b1) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      find(b + i * step);
-      found();
-      load_k(buf[i]);
-      load_v(buf[i]);
+    for (int i = 0; i < kQStages - 1; ++i) {
+      find(x.b0 + i * kQWaves + wave);
+      copy(i);
     }
-    find(b + 2 * step);
+    find(x.b0 + (kQStages - 1) * kQWaves + wave);
   }
 
   const int pair = min(pair0 + l16, pairs - 1), row = pair / group;
@@ -309,18 +315,18 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto block = [&](Kv4Block<D>& r, auto masked_t) {
+  // where the lane's operands stand in a page's codes
+  const int at = kG == 2 ? 16 * (4 * l16 + ((g4 + (l16 >> 2)) & 3)) : 8 * (4 * l16 + g4);
+  auto block = [&](const Kv4Block<D>& r, int b, auto masked_t) {
     constexpr bool masked = decltype(masked_t)::value;
     const int key0 = kQKeys * b;
-    found();
-    find(b + 3 * step);
-#pragma unroll
-    for (int i = 0; i < kG; ++i) params[64 * i + lane] = r.p[i];
-    wave_lds_sync();
+    const uint32_t* params = r.p;
     // ---- S^T = K Q^T ---------------------------------------------------------------
     float sc[8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+      uint32_t code[2 * kG];
+      kv4_read(code, r.k + 8 * D * j + at);
 #pragma unroll
       for (int g = 0; g < kG; ++g) {
         const uint32_t kz = params[kv4_place<D>(j, 0, g) + l16];
@@ -328,7 +334,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
         f32x4 acc = mfma16(kv4_operand(zz, zz, zz, zz), qz[g], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          const uint32_t y = r.k[j][2 * g + w];
+          const uint32_t y = code[2 * g + w];
           acc = mfma16(kv4_operand(unpack(y, 0), unpack(y, 1), unpack(y, 2), unpack(y, 3)),
                        q[2 * g + w], acc);
         }
@@ -339,13 +345,16 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
           sc[4 * j + i] = g == 0 ? s * acc[i] : fmaf(s, acc[i], sc[4 * j + i]);
         }
       }
+    }
     u32x4 vp[2][kG];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int g = 0; g < kG; ++g)
         vp[j][g] = *reinterpret_cast<const u32x4*>(params + kv4_place<D>(j, 1, g) + 4 * g4);
-    load_k(r);
+    uint32_t v[2][2 * kG];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) kv4_read(v[j], r.v + 8 * D * j + at);
     // ---- masks: keys that a row does not see, and slots behind the last key -----------
     if constexpr (masked) {
 #pragma unroll
@@ -398,9 +407,9 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
         const u32x4 pr = vp[i / 2][g];
         zz[i] = __builtin_amdgcn_perm(pr[i % 2 * 2 + 1], pr[i % 2 * 2], 0x05040100u);
         if constexpr (kG == 1)
-          w[i] = r.v[i / 2][i % 2];
+          w[i] = v[i / 2][i % 2];
         else
-          w[i] = __builtin_amdgcn_perm(r.v[i / 2][i % 2 * 2 + 1], r.v[i / 2][i % 2 * 2],
+          w[i] = __builtin_amdgcn_perm(v[i / 2][i % 2 * 2 + 1], v[i / 2][i % 2 * 2],
                                        g == 0 ? 0x05040100u : 0x07060302u);
       }
       st.corr[g] = mfma16(kv4_operand(zz[0], zz[1], zz[2], zz[3]), pf, st.corr[g]);
@@ -410,29 +419,40 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
                                              unpack(w[3], e)),
                                  pf, st.o[4 * g + e]);
     }
-    load_v(r);
-    wave_lds_sync();                       // (the next block's parameters take the place of these)
-    b += step;
   };
+  // Blocks base .. base + 3 stand in stage `stage`.  Waits for the wave's own copies (and, where waves
+  // share blocks, for the others'), then starts those of the stage that all are done with.
+  int stage = 0;
+  auto turn = [&] {
+    kv4_fence();
+    __builtin_amdgcn_s_waitcnt(0x0070 | (Kv4Block<D>::kOps * (kQStages - 2)));   // and lgkmcnt(0)
+    if (side > 1) __builtin_amdgcn_s_barrier();
+    kv4_fence();
+  };
+  auto refill = [&](int base) {
+    copy(stage == 0 ? kQStages - 1 : stage - 1);
+    find(base + kQStages * kQWaves + wave);
+  };
+  const bool active = pair0 < pairs;
   const int open = (x.kv_len - x.rows + 1) / kQKeys;     // blocks that all rows see whole
+  auto blocks = [&](int& base, int to, auto masked_t) {
+    for (; base < to; base += kQWaves) {
+      turn();
+      refill(base);
+      if (active)
+        for (int j = wave / side; j < kQWaves && base + j < x.b1; j += kQWaves / side)
+          block(lds.ring[stage][j], base + j, masked_t);
+      stage = stage == kQStages - 1 ? 0 : stage + 1;
+    }
+  };
   // (two loops: the compiler would make one of two variants in a loop, with the codes of a
   // block unpacked before it knows which)
-  const int whole = min(x.b1, open);
-  while (b < whole) {
-    block(buf[0], std::false_type());
-    if (b >= whole) {
-      const Kv4Block<D> t = buf[0];
-      buf[0] = buf[1];
-      buf[1] = t;
-      break;
-    }
-    block(buf[1], std::false_type());
-  }
-  while (b < x.b1) {
-    block(buf[0], std::true_type());
-    if (b >= x.b1) break;
-    block(buf[1], std::true_type());
-  }
+  int base = x.b0;
+  blocks(base, min(x.b1, open) - kQWaves + 1, std::false_type());
+  blocks(base, x.b1, std::true_type());
+  kv4_fence();
+  __builtin_amdgcn_s_waitcnt(0);           // (copies that nobody waited for)
+  kv4_fence();
   st.l += wave_xor(st.l, 16);
   st.l += wave_xor(st.l, 32);
 #pragma unroll
@@ -485,18 +505,20 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
   // the waves: `side` column tiles of 16 pairs beside each other
   const int side = have <= 16 ? 1 : have <= 32 ? 2 : 4, mine = wave % side;
   const float c = a.scale * kLog2e;
-  if (16 * mine < have) {
+  {
     Kv4State<D> st;
-    kv4_wave<D>(a, x, h, pair0 + 16 * mine, x.b0 + wave / side, kQWaves / side, lds.params[wave], st);
-    // (the last piece's readers are behind kv4_find's barrier)
+    kv4_wave<D>(a, x, h, pair0 + 16 * mine, side, lds, st);
+    __syncthreads();                       // (the blocks make room for the states)
+    if (16 * mine < have) {
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i)
+      for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        lds.o[wave][l16][64 * (i / 4) + 4 * (4 * g4 + r) + i % 4] = st.o[i][r];
-    if (g4 == 0) {
-      lds.m[wave][l16] = st.m;
-      lds.l[wave][l16] = st.l;
+        for (int r = 0; r < 4; ++r)
+          lds.o[wave][l16][64 * (i / 4) + 4 * (4 * g4 + r) + i % 4] = st.o[i][r];
+      if (g4 == 0) {
+        lds.m[wave][l16] = st.m;
+        lds.l[wave][l16] = st.l;
+      }
     }
   }
   __syncthreads();
