@@ -60,20 +60,29 @@ constexpr int kQStages = STAGES;
 
 // A block in LDS: K codes of its two pages, V codes, parameters [page][K, V][group][token].
 template <int D>
-struct Kv4Block {
+struct alignas(16) Kv4Block {
   char k[16 * D], v[16 * D];
   uint32_t p[D];
   static constexpr int kOps = D == 128 ? 6 : 3;      // loads that fill one
 };
 
+// Up to 8 pairs: what a wave has of four pages.
 template <int D>
+struct alignas(16) Kv4Four {
+  char k[32 * D], v[32 * D];
+  uint32_t kp[D], vp[D];                   // [page][group][token]
+  static constexpr int kOps = D == 128 ? 12 : 6;     // loads that fill one
+};
+
+template <int D, int R>
 struct Kv4Lds {
   union {
-    Kv4Block<D> ring[kQStages][kQWaves];
-    float o[kQWaves][16][D + 4];
+    Kv4Block<D> ring[R == 1 ? kQStages : 0][kQWaves];
+    Kv4Four<D> four[R == 1 ? 0 : kQWaves][2];
+    float o[kQWaves][16 / R][D + 4];
   };
   float m[kQWaves][16], l[kQWaves][16];
-  int start[kKv4PlanSeqs], span[kKv4PlanSeqs], len[kKv4PlanSeqs];   // (a thread's own four each)
+  int start[kKv4PlanSeqs + 1];
   int wave_sum[kQWaves], longest[kQWaves], flag;
   Kv4Piece piece;
 };
@@ -101,7 +110,7 @@ __device__ __forceinline__ int kv4_blocks(int kv_len) {
 template <class Lds>
 __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& plan) {
   const int group = a.hq / a.hkv;
-  int sum = 0, longest = 0;
+  int sum = 0, longest = 0, start[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int s = threadIdx.x * 4 + i;
@@ -112,9 +121,7 @@ __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& pl
       tiles = (max(rows, 0) * group + kQPairs - 1) / kQPairs;
       len = kv4_blocks(kv) + kQStart;
     }
-    lds.start[s] = sum;
-    lds.span[s] = tiles * len;
-    lds.len[s] = len;
+    start[i] = sum;
     sum += tiles * len;
     if (tiles > 0) longest = max(longest, len);
   }
@@ -137,7 +144,8 @@ __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& pl
     longest = max(longest, lds.longest[w]);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) lds.start[threadIdx.x * 4 + i] += before;
+  for (int i = 0; i < 4; ++i) lds.start[threadIdx.x * 4 + i] = start[i] + before;
+  if (threadIdx.x == 0) lds.start[kKv4PlanSeqs] = plan.total;
   // (a tile is cut into at most kQMaxPieces)
   plan.share = max(max((plan.total + a.units - 1) / a.units, kQMinBlocks),
                    (longest + kQMaxPieces - 3) / (kQMaxPieces - 2));
@@ -157,18 +165,19 @@ __device__ __forceinline__ Kv4Piece kv4_find(const Kv4Args& a, Lds& lds, const K
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int s = threadIdx.x * 4 + i, off = g - lds.start[s];
-    if (off >= 0 && off < lds.span[s]) {
+    if (off >= 0 && g < lds.start[s + 1]) {
       Kv4Piece x;
       x.s = s;
-      x.tile = off / lds.len[s];
-      const int t0 = lds.start[s] + x.tile * lds.len[s], t1 = t0 + lds.len[s];
+      kv4_sequence(a, x.s, x.qb, x.rows, x.kv_len);
+      const int len = kv4_blocks(x.kv_len) + kQStart;
+      x.tile = off / len;
+      const int t0 = lds.start[s] + x.tile * len, t1 = t0 + len;
       x.b0 = max(g - t0 - kQStart, 0);
       x.b1 = max(min(to, t1) - t0 - kQStart, 0);
       x.first = t0 / plan.share;
       x.n = (t1 - 1) / plan.share - x.first + 1;
       x.p = unit - x.first;
       x.next = min(to, t1) - from;
-      kv4_sequence(a, x.s, x.qb, x.rows, x.kv_len);
       lds.piece = x;
     }
   }
@@ -236,7 +245,7 @@ __device__ __forceinline__ void kv4_fence() { asm volatile("" ::: "memory"); }
 // of them; a wave whose pairs are none copies its blocks for the others.
 template <int D>
 __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, int h, int pair0, int side,
-                                         Kv4Lds<D>& lds, Kv4State<D>& st) {
+                                         Kv4Lds<D, 1>& lds, Kv4State<D>& st) {
   constexpr int kG = D / 64;
   using P = Kv4Page<D>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
@@ -461,6 +470,255 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
     for (int e = 0; e < 4; ++e) st.o[4 * g + e] -= st.corr[g];
 }
 
+// x of the lanes 4 (R = 4) or 8 (R = 2, 4) before this one in its 16, around.
+template <int kBy>
+__device__ __forceinline__ float kv4_turned(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x120 + kBy, 0xf, 0xf, false));
+}
+template <int R>
+__device__ __forceinline__ float kv4_class_sum(float x) {
+  if constexpr (R == 4) x += kv4_turned<4>(x);
+  return x + kv4_turned<8>(x);
+}
+
+// Up to 16 / R pairs (R = 2, 4) against the blocks from x.b0 + 2 wave on, two of every eight.  Of the 16
+// columns R each are a pair's: class jl = l16 / (16 / R) of them has the scores of pages jl, jl + R, ..
+// (of the four that the wave has at a time; the matrix unit gives all columns all pages' scores, of
+// which a lane takes its own), so that softmax works on no score twice, and columns of O^T that hold
+// their classes' shares.  While four pages are worked on, the wave's next four are on their way.
+template <int D, int R>
+__device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x, int h,
+                                             Kv4Four<D>* lds, Kv4State<D>& st) {
+  constexpr int kG = D / 64, kTurns = 4 / R, kCols = 16 / R;
+  using P = Kv4Page<D>;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
+  const int jl = l16 / kCols;
+  const int group = a.hq / a.hkv, pairs = x.rows * group;
+  const float c = a.scale * kLog2e, tau = kRescaleLog2 / c;
+  const Kv4Unpack unpack;
+
+  // ---- copies ---------------------------------------------------------------------------------
+  const int pages = min((x.kv_len + 15) / 16, 2 * x.b1);
+  const int32_t* table = a.tables + (size_t)x.s * a.max_blocks;
+  const size_t stride = (size_t)a.hkv * P::kBytes;
+  const char* kc = (const char*)a.k_cache + (size_t)h * P::kBytes;
+  const char* vc = (const char*)a.v_cache + (size_t)h * P::kBytes;
+  const int piece = kG == 2 ? 16 * ((lane & ~3) | ((lane - g4) & 3)) : 16 * (lane & 31);
+  const int param = P::kParams + lane % (16 * kG) * 4;
+  int next[4];
+  auto find = [&](int page) {              // (behind the last page: that one again)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) next[j] = kv4_uniform(table, min(page + j, pages - 1));
+  };
+  auto pick = [](bool first, size_t a, size_t b) { return first ? a : b; };
+  auto copy = [&](Kv4Four<D>& to) {
+    size_t id[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) id[j] = (size_t)next[j] * stride;
+#pragma unroll
+    for (int values = 0; values < 2; ++values) {
+      const char* cache = values ? vc : kc;
+      char* codes = values ? to.v : to.k;
+      uint32_t* params = values ? to.vp : to.kp;
+      if constexpr (kG == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dma16(cache + id[j] + piece, (bf16_t*)(codes + 8 * D * j));
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          dma4(cache + pick(lane < 32, id[2 * j], id[2 * j + 1]) + param, params + 64 * j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          dma16(cache + pick(lane < 32, id[2 * j], id[2 * j + 1]) + piece, (bf16_t*)(codes + 16 * D * j));
+        dma4(cache + pick(lane < 32, pick(lane < 16, id[0], id[1]), pick(lane < 48, id[2], id[3])) + param,
+             params);
+      }
+    }
+  };
+  int page = 2 * x.b0 + 4 * wave;
+  const int end = 2 * x.b1;
+  if (page < end) {
+    find(page);
+    copy(lds[0]);
+    find(page + 4 * kQWaves);
+    copy(lds[1]);
+    find(page + 8 * kQWaves);
+  }
+
+  const int pair = min(l16 % kCols, pairs - 1), row = pair / group;
+  const int last = min(x.kv_len - x.rows + row, kQKeys * x.b1 - 1);   // the last key of the lane's column
+  const bf16_t* src = (const bf16_t*)a.q + ((size_t)(x.qb + row) * a.hq + h * group + pair % group) * D;
+  bf16x8 q[2 * kG];
+  bf16x8 qz[kG];                           // minus the sum of q, in three parts
+#pragma unroll
+  for (int g = 0; g < kG; ++g) {
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const u32x4 y = load16(src + 64 * g + 16 * g4 + 8 * w);
+      q[2 * g + w] = as_bf16x8(y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sum += __uint_as_float(y[i] << 16) + __uint_as_float(y[i] & 0xffff0000u);
+    }
+    sum += wave_xor(sum, 16);
+    sum += wave_xor(sum, 32);
+    const float part0 = (float)(__bf16)-sum, part1 = (float)(__bf16)(-sum - part0);
+    const float on = g4 == 0 ? 1.f : 0.f;
+    qz[g] = to_bf16x8(part0 * on, part1 * on, (-sum - part0 - part1) * on, 0.f, 0.f, 0.f, 0.f, 0.f);
+    st.corr[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  st.l = 0.f;
+  st.m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int at = kG == 2 ? 16 * (4 * l16 + ((g4 + (l16 >> 2)) & 3)) : 8 * (4 * l16 + g4);
+
+  auto four = [&](Kv4Four<D>& r, auto masked_t) {
+    constexpr bool masked = decltype(masked_t)::value;
+    kv4_fence();
+    __builtin_amdgcn_s_waitcnt(0x0F70 | Kv4Four<D>::kOps);     // (those of the next four may be out)
+    kv4_fence();
+    // ---- S^T = K Q^T -------------------------------------------------------------------------
+    float sc[kTurns][4];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t)
+#pragma unroll
+      for (int g = 0; g < kG; ++g) {
+        f32x4 mine = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          const int pg = t * R + j;
+          uint32_t code[2];
+          kv4_read(code, r.k + 8 * D * pg + at + 8 * g);
+          const uint32_t z = r.kp[(pg * kG + g) * 16 + l16], zz = __builtin_amdgcn_perm(z, z, 0x01000100u);
+          f32x4 acc = mfma16(kv4_operand(zz, zz, zz, zz), qz[g], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t y = code[w];
+            acc = mfma16(kv4_operand(unpack(y, 0), unpack(y, 1), unpack(y, 2), unpack(y, 3)),
+                         q[2 * g + w], acc);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mine[i] = j == 0 || jl == j ? acc[i] : mine[i];
+        }
+        const u32x4 kp = *reinterpret_cast<const u32x4*>(r.kp + ((t * R + jl) * kG + g) * 16 + 4 * g4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float s = kv4_scale(kp[i]);
+          sc[t][i] = g == 0 ? s * mine[i] : fmaf(s, mine[i], sc[t][i]);
+        }
+      }
+    // ---- softmax -------------------------------------------------------------------------------
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (masked && 16 * (page + t * R + jl) + 4 * g4 + i > last) sc[t][i] = -INFINITY;
+        top = fmaxf(top, sc[t][i]);
+      }
+    if constexpr (R == 4) top = fmaxf(top, kv4_turned<4>(top));
+    top = fmaxf(top, kv4_turned<8>(top));
+    top = column_max(top);
+    if (wave_any(top > st.m + tau)) {
+      const float m = fmaxf(st.m, top);
+      const float alpha = st.m == -INFINITY ? 0.f : fast_exp2((st.m - m) * c);
+      st.l *= alpha;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) st.o[i] *= alpha;
+#pragma unroll
+      for (int g = 0; g < kG; ++g) st.corr[g] *= alpha;
+      st.m = m;
+    }
+    const float ref = st.m == -INFINITY ? 0.f : -st.m * c;
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[t][i] = fast_exp2(fmaf(sc[t][i], c, ref));
+        st.l += sc[t][i];
+      }
+    // ---- O^T += V^T P^T ------------------------------------------------------------------------
+#pragma unroll
+    for (int g = 0; g < kG; ++g) {
+      u32x2 p[kTurns];                     // p', four keys of the lane's page
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        const u32x4 vp = *reinterpret_cast<const u32x4*>(r.vp + ((t * R + jl) * kG + g) * 16 + 4 * g4);
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[i] = sc[t][i] * kv4_scale(vp[i]);
+          // (the scale of a key not seen may be NaN)
+          if (masked && 16 * (page + t * R + jl) + 4 * g4 + i > last) y[i] = 0.f;
+        }
+        p[t] = __builtin_bit_cast(u32x2, to_bf16x4(y[0], y[1], y[2], y[3]));
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {        // pages 2 m and 2 m + 1
+        u32x4 b;
+        uint32_t w[4], zz[4];              // two keys' units of group g, and their zero points
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int j = 2 * m + i;
+          const u32x4 vz = *reinterpret_cast<const u32x4*>(r.vp + (j * kG + g) * 16 + 4 * g4);
+          uint32_t v[2 * kG];
+          kv4_read(v, r.v + 8 * D * j + at);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            b[2 * i + e] = jl == j % R ? p[j / R][e] : 0;
+            uint32_t z0 = vz[2 * e], z1 = vz[2 * e + 1];
+            if (masked) {                  // (zero points alike for all columns: none that is NaN)
+              const int key = 16 * (page + j) + 4 * g4 + 2 * e;
+              if (key >= x.kv_len || (z0 & 0x7f80u) == 0x7f80u) z0 = 0;
+              if (key + 1 >= x.kv_len || (z1 & 0x7f80u) == 0x7f80u) z1 = 0;
+            }
+            zz[2 * i + e] = __builtin_amdgcn_perm(z1, z0, 0x05040100u);
+            if constexpr (kG == 1)
+              w[2 * i + e] = v[e];
+            else
+              w[2 * i + e] = __builtin_amdgcn_perm(v[2 * e + 1], v[2 * e],
+                                                   g == 0 ? 0x05040100u : 0x07060302u);
+          }
+        }
+        const bf16x8 pf = as_bf16x8(b);
+        st.corr[g] = mfma16(kv4_operand(zz[0], zz[1], zz[2], zz[3]), pf, st.corr[g]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          st.o[4 * g + e] = mfma16(kv4_operand(unpack(w[0], e), unpack(w[1], e), unpack(w[2], e),
+                                               unpack(w[3], e)),
+                                   pf, st.o[4 * g + e]);
+      }
+    }
+    // what was read is in registers: the place is filled again
+    kv4_fence();
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    kv4_fence();
+    copy(r);
+    page += 4 * kQWaves;
+    find(page + 8 * kQWaves);
+  };
+  // pages that all rows see whole, and that are the piece's
+  const int whole = min((x.kv_len - x.rows + 1) / 16, end);
+  int stage = 1;
+  while (page + 4 <= whole) four(lds[stage ^= 1], std::false_type());
+  while (page < end) four(lds[stage ^= 1], std::true_type());
+  kv4_fence();
+  __builtin_amdgcn_s_waitcnt(0);           // (copies that nobody waited for)
+  kv4_fence();
+  st.l = kv4_class_sum<R>(st.l);
+  st.l += wave_xor(st.l, 16);
+  st.l += wave_xor(st.l, 32);
+#pragma unroll
+  for (int g = 0; g < kG; ++g)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        st.o[4 * g + e][r] = kv4_class_sum<R>(st.o[4 * g + e][r] - st.corr[g][r]);
+}
+
 // Join of a cut tile's pieces: piece p's partials are at place 2 (first + p), + 1 for p = 0.
 template <int D>
 __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, int h) {
@@ -497,8 +755,8 @@ __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, in
   }
 }
 
-template <int D>
-__device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, int h, Kv4Lds<D>& lds) {
+template <int D, int R>
+__device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, int h, Kv4Lds<D, R>& lds) {
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
   const int group = a.hq / a.hkv, pair0 = x.tile * kQPairs, have = min(x.rows * group - pair0, kQPairs);
@@ -507,9 +765,12 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
   const float c = a.scale * kLog2e;
   {
     Kv4State<D> st;
-    kv4_wave<D>(a, x, h, pair0 + 16 * mine, side, lds, st);
+    if constexpr (R == 1)
+      kv4_wave<D>(a, x, h, pair0 + 16 * mine, side, lds, st);
+    else
+      kv4_wave_few<D, R>(a, x, h, lds.four[wave], st);
     __syncthreads();                       // (the blocks make room for the states)
-    if (16 * mine < have) {
+    if (16 * mine < have && l16 < 16 / R) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -568,9 +829,10 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
 #ifndef OCC
 #define OCC 2
 #endif
-template <int D>
-__global__ __launch_bounds__(64 * kQWaves, OCC) void kv4_decode_kernel(Kv4Args a) {
-  __shared__ Kv4Lds<D> lds;
+// R: 16 / R pairs a sequence at most (R = 1: any number).
+template <int D, int R>
+__global__ __launch_bounds__(64 * kQWaves, R == 1 ? 2 : OCC) void kv4_decode_kernel(Kv4Args a) {
+  __shared__ Kv4Lds<D, R> lds;
   const int h = blockIdx.x % a.hkv, unit = blockIdx.x / a.hkv;
   Kv4Plan plan;
   if (a.units > 0) kv4_plan(a, lds, plan);
@@ -589,7 +851,7 @@ __global__ __launch_bounds__(64 * kQWaves, OCC) void kv4_decode_kernel(Kv4Args a
       x.b1 = kv4_blocks(x.kv_len);
       x.n = 1;
     }
-    kv4_piece<D>(a, x, h, lds);
+    kv4_piece<D, R>(a, x, h, lds);
     if (a.units == 0) return;
   }
 }
@@ -613,12 +875,23 @@ int64_t kv4_grid(const Kv4Shape& t, int num_seqs, int hkv) {
   return t.units > 0 ? (int64_t)t.units * hkv : (int64_t)num_seqs * t.tiles * hkv;
 }
 
-hipError_t launch_kv4(const Kv4Args& a, const Kv4Shape& t, hipStream_t stream) {
+namespace {
+
+template <int D>
+void launch_kv4_d(const Kv4Args& a, const Kv4Shape& t, hipStream_t stream) {
   const dim3 grid((unsigned)kv4_grid(t, a.num_seqs, a.hkv)), block(64 * kQWaves);
-  if (a.d == 64)
-    kv4_decode_kernel<64><<<grid, block, 0, stream>>>(a);
+  if (t.cols <= 4)
+    kv4_decode_kernel<D, 4><<<grid, block, 0, stream>>>(a);
+  else if (t.cols <= 8)
+    kv4_decode_kernel<D, 2><<<grid, block, 0, stream>>>(a);
   else
-    kv4_decode_kernel<128><<<grid, block, 0, stream>>>(a);
+    kv4_decode_kernel<D, 1><<<grid, block, 0, stream>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_kv4(const Kv4Args& a, const Kv4Shape& t, hipStream_t stream) {
+  a.d == 64 ? launch_kv4_d<64>(a, t, stream) : launch_kv4_d<128>(a, t, stream);
   return hipGetLastError();
 }
 
