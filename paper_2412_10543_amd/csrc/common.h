@@ -162,8 +162,8 @@ __device__ __forceinline__ void dma16(const void* src, bf16_t* lds_dst) {
       : "memory");
 }
 
-// The same copy of 4 bytes per lane (global_load_lds_dword): lane l's land at lds_dst + 4*l.
-__device__ __forceinline__ void dma4(const void* src, void* lds_dst) {
+// The same copy with the non-temporal hint: data read once.
+__device__ __forceinline__ void dma16_stream(const void* src, void* lds_dst) {
   typedef __attribute__((address_space(3))) char lds_char;
   const uint32_t base =
       __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char*)lds_dst);
@@ -172,7 +172,23 @@ __device__ __forceinline__ void dma4(const void* src, void* lds_dst) {
       "s_mov_b32 %0, m0\n\t"
       "s_mov_b32 m0, %2\n\t"
       "s_nop 0\n\t"
-      "global_load_lds_dword %1, off\n\t"
+      "global_load_lds_dwordx4 %1, off nt\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(src), "s"(base)
+      : "memory");
+}
+// And of 4 bytes per lane: lane l's land at lds_dst + 4*l.
+__device__ __forceinline__ void dma4_stream(const void* src, void* lds_dst) {
+  typedef __attribute__((address_space(3))) char lds_char;
+  const uint32_t base =
+      __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char*)lds_dst);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, off nt\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)
       : "v"(src), "s"(base)

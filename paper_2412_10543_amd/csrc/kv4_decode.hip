@@ -274,17 +274,17 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
     Kv4Block<D>& to = lds.ring[stage][wave];
     const size_t id0 = (size_t)next[0] * stride, id1 = (size_t)next[1] * stride;
     if constexpr (kG == 2) {
-      dma16(kc + id0 + piece, (bf16_t*)to.k);
-      dma16(kc + id1 + piece, (bf16_t*)(to.k + 8 * D));
-      dma4(pc + id0, to.p);
-      dma4(pc + id1, to.p + 64);
-      dma16(vc + id0 + piece, (bf16_t*)to.v);
-      dma16(vc + id1 + piece, (bf16_t*)(to.v + 8 * D));
+      dma16_stream(kc + id0 + piece, to.k);
+      dma16_stream(kc + id1 + piece, to.k + 8 * D);
+      dma4_stream(pc + id0, to.p);
+      dma4_stream(pc + id1, to.p + 64);
+      dma16_stream(vc + id0 + piece, to.v);
+      dma16_stream(vc + id1 + piece, to.v + 8 * D);
     } else {
       const size_t id = lane < 32 ? id0 : id1;
-      dma16(kc + id + piece, (bf16_t*)to.k);
-      dma4(pc + id, to.p);
-      dma16(vc + id + piece, (bf16_t*)to.v);
+      dma16_stream(kc + id + piece, to.k);
+      dma4_stream(pc + id, to.p);
+      dma16_stream(vc + id + piece, to.v);
     }
   };
   if (x.b0 < x.b1) {
@@ -511,37 +511,33 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
     for (int j = 0; j < 4; ++j) next[j] = kv4_uniform(table, min(page + j, pages - 1));
   };
   auto pick = [](bool first, size_t a, size_t b) { return first ? a : b; };
-  auto copy = [&](Kv4Four<D>& to) {
+  auto copy = [&](const char* cache, char* codes, uint32_t* params) {
     size_t id[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) id[j] = (size_t)next[j] * stride;
+    if constexpr (kG == 2) {
 #pragma unroll
-    for (int values = 0; values < 2; ++values) {
-      const char* cache = values ? vc : kc;
-      char* codes = values ? to.v : to.k;
-      uint32_t* params = values ? to.vp : to.kp;
-      if constexpr (kG == 2) {
+      for (int j = 0; j < 4; ++j) dma16_stream(cache + id[j] + piece, codes + 8 * D * j);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dma16(cache + id[j] + piece, (bf16_t*)(codes + 8 * D * j));
+      for (int j = 0; j < 2; ++j)
+        dma4_stream(cache + pick(lane < 32, id[2 * j], id[2 * j + 1]) + param, params + 64 * j);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          dma4(cache + pick(lane < 32, id[2 * j], id[2 * j + 1]) + param, params + 64 * j);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          dma16(cache + pick(lane < 32, id[2 * j], id[2 * j + 1]) + piece, (bf16_t*)(codes + 16 * D * j));
-        dma4(cache + pick(lane < 32, pick(lane < 16, id[0], id[1]), pick(lane < 48, id[2], id[3])) + param,
-             params);
-      }
+      for (int j = 0; j < 2; ++j)
+        dma16_stream(cache + pick(lane < 32, id[2 * j], id[2 * j + 1]) + piece, codes + 16 * D * j);
+      dma4_stream(cache + pick(lane < 32, pick(lane < 16, id[0], id[1]), pick(lane < 48, id[2], id[3])) +
+                      param, params);
     }
   };
   int page = 2 * x.b0 + 4 * wave;
   const int end = 2 * x.b1;
   if (page < end) {
     find(page);
-    copy(lds[0]);
+    copy(kc, lds[0].k, lds[0].kp);
+    copy(vc, lds[0].v, lds[0].vp);
     find(page + 4 * kQWaves);
-    copy(lds[1]);
+    copy(kc, lds[1].k, lds[1].kp);
+    copy(vc, lds[1].v, lds[1].vp);
     find(page + 8 * kQWaves);
   }
 
@@ -574,6 +570,11 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
   for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int at = kG == 2 ? 16 * (4 * l16 + ((g4 + (l16 >> 2)) & 3)) : 8 * (4 * l16 + g4);
 
+  auto taken = [&] {                       // what was read from LDS is in registers: it is filled again
+    kv4_fence();
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    kv4_fence();
+  };
   auto four = [&](Kv4Four<D>& r, auto masked_t) {
     constexpr bool masked = decltype(masked_t)::value;
     kv4_fence();
@@ -609,6 +610,8 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
           sc[t][i] = g == 0 ? s * mine[i] : fmaf(s, mine[i], sc[t][i]);
         }
       }
+    taken();
+    copy(kc, r.k, r.kp);
     // ---- softmax -------------------------------------------------------------------------------
     float top = -INFINITY;
 #pragma unroll
@@ -691,11 +694,8 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
                                    pf, st.o[4 * g + e]);
       }
     }
-    // what was read is in registers: the place is filled again
-    kv4_fence();
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    kv4_fence();
-    copy(r);
+    taken();
+    copy(vc, r.v, r.vp);
     page += 4 * kQWaves;
     find(page + 8 * kQWaves);
   };
