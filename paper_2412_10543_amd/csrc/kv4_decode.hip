@@ -35,10 +35,16 @@ namespace {
 constexpr int kQWaves = 4;
 constexpr int kQKeys = 32;                 // keys of a block
 constexpr int kQPairs = 16 * kQWaves;      // pairs of a tile, at most
-constexpr int kQMinBlocks = 8;             // blocks of a share, at least
-constexpr int kQStart = 6;                 // blocks that the start of a tile counts for
+// Blocks of a share, at least.  One sequence of 4,782 keys, 32 q / 8 kv heads: 13.9 us; cut down to 4
+// blocks 16.8 (more partials to join), to 16 14.0.
+constexpr int kQMinBlocks = 8;
+// Blocks that the start of a tile counts for (32 chains of 3 to 9 rows, 700 to 10,304 keys: 66 us;
+// with 20 67.7).
+constexpr int kQStart = 12;
 constexpr int kQMaxPieces = 64;            // of a tile (one lane each in the join)
-constexpr int kQWorkgroups = 512;          // about two a CU
+// Workgroups: two a CU, as many as there is LDS for (1024: 64 sequences of 2.6k to 10.3k keys 104 us
+// against 92).
+constexpr int kQWorkgroups = 512;
 
 // One row tile's piece of work: blocks [b0, b1) of its n.
 struct Kv4Piece {
@@ -53,10 +59,7 @@ struct Kv4Plan {
   int total, share;
 };
 
-#ifndef STAGES
-#define STAGES 3
-#endif
-constexpr int kQStages = STAGES;
+constexpr int kQStages = 3;
 
 // A block in LDS: K codes of its two pages, V codes, parameters [page][K, V][group][token].
 template <int D>
@@ -102,11 +105,19 @@ __device__ __forceinline__ void kv4_sequence(const Kv4Args& a, int s, int& qb, i
   kv = min(a.kv_lens[s], a.max_blocks * 16);
 }
 
+// Waves beside each other on a block, for this many pairs.
+__device__ __forceinline__ int kv4_side(int pairs) { return pairs <= 16 ? 1 : pairs <= 32 ? 2 : 4; }
+// A block's work: what waves beside each other add to it is about half of what the block takes
+// (32 chains of 3 to 9 rows: 66 us; counted as 1 : 1 : 1 70, 1 : 2 : 4 75, 2 : 3 : 3 72, 3 : 4 : 5 71).
+__device__ __forceinline__ int kv4_weight(int pairs) { return pairs <= 16 ? 2 : pairs <= 32 ? 3 : 4; }
+constexpr int kQMaxWeight = 4;
+
 __device__ __forceinline__ int kv4_blocks(int kv_len) {
   return (max(kv_len, 0) + kQKeys - 1) / kQKeys;
 }
 
-// The sequences' places in one row of all blocks, kQStart more in front of each tile.
+// The sequences' places in one row of all blocks, kQStart more in front of each tile, each counted
+// by its work.
 template <class Lds>
 __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& plan) {
   const int group = a.hq / a.hkv;
@@ -119,7 +130,7 @@ __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& pl
       int qb, rows, kv;
       kv4_sequence(a, s, qb, rows, kv);
       tiles = (max(rows, 0) * group + kQPairs - 1) / kQPairs;
-      len = kv4_blocks(kv) + kQStart;
+      len = (kv4_blocks(kv) + kQStart) * kv4_weight(max(rows, 0) * group);
     }
     start[i] = sum;
     sum += tiles * len;
@@ -147,7 +158,7 @@ __device__ __forceinline__ void kv4_plan(const Kv4Args& a, Lds& lds, Kv4Plan& pl
   for (int i = 0; i < 4; ++i) lds.start[threadIdx.x * 4 + i] = start[i] + before;
   if (threadIdx.x == 0) lds.start[kKv4PlanSeqs] = plan.total;
   // (a tile is cut into at most kQMaxPieces)
-  plan.share = max(max((plan.total + a.units - 1) / a.units, kQMinBlocks),
+  plan.share = max(max((plan.total + a.units - 1) / a.units, kQMinBlocks * kv4_weight(1)),
                    (longest + kQMaxPieces - 3) / (kQMaxPieces - 2));
 }
 
@@ -169,11 +180,12 @@ __device__ __forceinline__ Kv4Piece kv4_find(const Kv4Args& a, Lds& lds, const K
       Kv4Piece x;
       x.s = s;
       kv4_sequence(a, x.s, x.qb, x.rows, x.kv_len);
-      const int len = kv4_blocks(x.kv_len) + kQStart;
+      const int weight = kv4_weight(x.rows * (a.hq / a.hkv));
+      const int len = (kv4_blocks(x.kv_len) + kQStart) * weight;
       x.tile = off / len;
       const int t0 = lds.start[s] + x.tile * len, t1 = t0 + len;
-      x.b0 = max(g - t0 - kQStart, 0);
-      x.b1 = max(min(to, t1) - t0 - kQStart, 0);
+      x.b0 = max((g - t0) / weight - kQStart, 0);
+      x.b1 = max((min(to, t1) - t0) / weight - kQStart, 0);
       x.first = t0 / plan.share;
       x.n = (t1 - 1) / plan.share - x.first + 1;
       x.p = unit - x.first;
@@ -593,6 +605,8 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
           uint32_t code[2];
           kv4_read(code, r.k + 8 * D * pg + at + 8 * g);
           const uint32_t z = r.kp[(pg * kG + g) * 16 + l16], zz = __builtin_amdgcn_perm(z, z, 0x01000100u);
+          // (a product of 16 channels would do, but accumulators that pass from that shape to
+          // the other at once have given wrong sums)
           f32x4 acc = mfma16(kv4_operand(zz, zz, zz, zz), qz[g], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
@@ -728,7 +742,15 @@ __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, in
   const int have = min(kQPairs, x.rows * group - x.tile * kQPairs);
   auto place = [&](int p) { return ((size_t)(2 * (x.first + p) + (p == 0)) * a.hkv + h) * C; };
   for (int i = threadIdx.x >> 6; i < have; i += kQWaves) {
+    // (eight pieces' rows are requested at a time, the first beside the log-sum-exps)
+    float y[8][kPer];
+    auto request = [&](int p0) {
+#pragma unroll
+      for (int p = 0; p < 8; ++p)
+        load_coherent_vec<kPer>(a.part_o + (place(min(p0 + p, x.n - 1)) + i) * D + lane * kPer, y[p]);
+    };
     const float lse = lane < x.n ? load_coherent(a.part_lse + place(lane) + i) : -INFINITY;
+    request(0);
     float top = lse;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, wave_xor(top, m));
@@ -737,12 +759,15 @@ __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, in
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) sum += wave_xor(sum, m);
     float acc[kPer] = {};
-    for (int p = 0; p < x.n; ++p) {
-      float y[kPer];
-      load_coherent_vec<kPer>(a.part_o + (place(p) + i) * D + lane * kPer, y);
-      const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
+    for (int p0 = 0; p0 < x.n; p0 += 8) {
+      if (p0 > 0) request(p0);
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] += wp == 0.f ? 0.f : wp * y[e];
+      for (int p = 0; p < 8; ++p) {
+        const float wp = __uint_as_float(
+            __builtin_amdgcn_readlane(__float_as_uint(w), min(p0 + p, kWave - 1)));
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] += p0 + p >= x.n || wp == 0.f ? 0.f : wp * y[p][e];
+      }
     }
     const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
     const int pair = x.tile * kQPairs + i;
@@ -761,7 +786,7 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
   const int group = a.hq / a.hkv, pair0 = x.tile * kQPairs, have = min(x.rows * group - pair0, kQPairs);
   // the waves: `side` column tiles of 16 pairs beside each other
-  const int side = have <= 16 ? 1 : have <= 32 ? 2 : 4, mine = wave % side;
+  const int side = kv4_side(have), mine = wave % side;
   const float c = a.scale * kLog2e;
   {
     Kv4State<D> st;
@@ -826,12 +851,9 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
   if (threadIdx.x == 0) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-#ifndef OCC
-#define OCC 2
-#endif
 // R: 16 / R pairs a sequence at most (R = 1: any number).
 template <int D, int R>
-__global__ __launch_bounds__(64 * kQWaves, R == 1 ? 2 : OCC) void kv4_decode_kernel(Kv4Args a) {
+__global__ __launch_bounds__(64 * kQWaves, 2) void kv4_decode_kernel(Kv4Args a) {
   __shared__ Kv4Lds<D, R> lds;
   const int h = blockIdx.x % a.hkv, unit = blockIdx.x / a.hkv;
   Kv4Plan plan;
@@ -866,7 +888,7 @@ Kv4Shape kv4_shape(int num_seqs, int max_rows, int hq, int hkv, int max_blocks) 
   t.units = num_seqs <= kKv4PlanSeqs ? std::max(kQWorkgroups / hkv, 1) : 0;
   // (counters; places among all blocks are counted in 32 bits)
   if ((int64_t)t.units * hkv > kKv4Counters ||
-      (double)num_seqs * t.tiles * (max_blocks / 2 + 1 + kQStart) > 1e9)
+      (double)num_seqs * t.tiles * (max_blocks / 2 + 1 + kQStart) * kQMaxWeight > 1e9)
     t.units = 0;
   return t;
 }
