@@ -66,17 +66,29 @@ struct Kv4Scale {
   __device__ __forceinline__ Kv4Scale(float lo, float hi, bool finite) {
     s = (float)(__bf16)((0.5f * hi - 0.5f * lo) / 7.5f);
     z = s > 0.f ? fminf(__builtin_rintf(-lo / s), 15.f) : 0.f;
-    if (!finite) s = __builtin_nanf("");
+    if (!finite) {
+      s = __builtin_nanf("");
+      z = 0.f;
+    }
   }
   __device__ __forceinline__ uint32_t param() const {
     const uint32_t zz = __float_as_uint(128.f + z) >> 16;
     return (__float_as_uint(s) & 0xffff0000u) | zz;
   }
-  // x / s is rounded to fp32 before it is rounded to a whole number.  Both are bf16,
-  // so that a quotient that is no tie is at least 2^-10 away from one.
-  __device__ __forceinline__ uint32_t code(float x) const {
-    if (!(s > 0.f)) return 0;
-    return (uint32_t)fminf(fmaxf(__builtin_rintf(x / s) + z, 0.f), 15.f);
+  // Codes of N values, as whole floats.  x / s is rounded to fp32 before it is rounded to a whole
+  // number; both are bf16, so that a quotient that is no tie is at least 2^-10 away from one, and
+  // one that is comes out exact (x times 1 / s and one step that makes good what is left of x).
+  template <int N>
+  __device__ __forceinline__ void codes(const float (&x)[N], float (&c)[N]) const {
+    const bool near = s > 1e-30f && s < 1e30f;       // (the reciprocal and the step in range)
+    const float r = 1.f / s;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float q = x[i] * r;
+      q = __builtin_fmaf(__builtin_fmaf(-q, s, x[i]), r, q);
+      if (!near) q = s > 0.f ? x[i] / s : 0.f;
+      c[i] = __builtin_amdgcn_fmed3f(__builtin_rintf(q) + z, 0.f, 15.f);
+    }
   }
 };
 
