@@ -79,6 +79,9 @@ struct Heat {
   __device__ __forceinline__ Heat(float top_, double k_) : k(k_), top(top_) {
     const double low = top - 1000.0 / k;
     cut = !(fabsf(top_) < INFINITY) ? INFINITY : low > -3.4028234663852886e38 ? (float)low : -3.4028234663852886e38f;
+    // (never below: at small T a logit's last place is hundreds of powers of 2, which the exponent
+    // has no room for)
+    if ((double)cut < low) cut = nextafterf(cut, INFINITY);
   }
   // Of N logits, step by step side by side (one's steps wait for each other).  kExact: 0 is 0
   // (otherwise it may be as much as 2^-1022, which no sum notices).

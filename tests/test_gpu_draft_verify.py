@@ -205,6 +205,20 @@ def test_drafter_that_equals_the_model():
     assert got == tuple(want)
 
 
+def test_temperatures_near_a_logit_s_last_place():
+    """Neighbouring logits that lie hundreds to thousands of powers of 2 apart: the largest ones alone
+    are drawn, as likely as each other."""
+    heat = [1e-9, 3e-9, 6e-9, 7e-9, 8e-9, 9e-9, 1e-8, 1.05e-8, 1.1e-8, 2e-8, 1e-7, 1e-6] * 4
+    g = torch.Generator().manual_seed(8)
+    x = 100 - 2.0 ** -17 * torch.randint(0, 4, (48, 5000), generator=g)
+    x[:, 70] = 100
+    u, cu = torch.rand(48, generator=g), list(range(49))
+    got = _verify(x.cuda(), [0] * 48, None, cu, heat, u, None, 1)
+    assert all(x[i, t] == 100 for i, t in enumerate(got[2][:36]))
+    heat = torch.tensor(heat, dtype=torch.float32).tolist()
+    assert got == tuple(ss.reference_verify(x.numpy(), [0] * 48, cu, heat, u.tolist(), 1))
+
+
 def test_large_vocabulary_flat_logits():
     """Every one of 150,001 tokens is as likely as the others up to a little: a draw turns on
     the sixth digit of the sums."""
