@@ -262,7 +262,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
   using P = Kv4Page<D>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
   const int group = a.hq / a.hkv, pairs = x.rows * group;
-  const float c = a.scale * kLog2e, tau = kRescaleLog2 / c;
+  const float c = a.scale * kLog2e, tau = fminf(kRescaleLog2 / c, 1e30f);   // (finite at any scale)
   const Kv4Unpack unpack;
 
   // ---- copies ---------------------------------------------------------------------------------
@@ -506,7 +506,7 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
   const int jl = l16 / kCols;
   const int group = a.hq / a.hkv, pairs = x.rows * group;
-  const float c = a.scale * kLog2e, tau = kRescaleLog2 / c;
+  const float c = a.scale * kLog2e, tau = fminf(kRescaleLog2 / c, 1e30f);   // (finite at any scale)
   const Kv4Unpack unpack;
 
   // ---- copies ---------------------------------------------------------------------------------

@@ -79,6 +79,18 @@ def test_peaked_scores(k_scale):
     _check([900, 40, 3000], [1, 3, 2], 8, 2, 128, 5, k_scale)
 
 
+@pytest.mark.parametrize("hq", [8, 20])
+def test_scale_so_small_that_all_keys_are_alike(hq):
+    """The least scale above 0: the mean of the values."""
+    kv = [40, 700]
+    q, kc, vc, table = _case(kv, [1, 1], hq, 2, 128, 9)
+    o, ws = torch.full_like(q, math.nan), _workspace(2, 1, hq, 2, 128)
+    binding.rag_attn_decode_paged_kv4(q, kc, vc, o, table, _i32(kv), 2.0 ** -149, workspace=ws)
+    torch.cuda.synchronize()
+    want, bound = ss.reference_kv4(q, kc, vc, table.cpu(), kv, [1, 1], 2.0 ** -149)
+    within(o, want, bound, "mean")
+
+
 def test_sequences_without_keys_or_rows():
     """kv 0 with a row each gives 0; sequences without rows are passed over; rows behind the
     last sequence stay."""
