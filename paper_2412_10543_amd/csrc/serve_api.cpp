@@ -24,6 +24,8 @@ using rag::ok;
 
 // Page ids fit in int32 slots (page * 16 + offset), table widths in int32 keys.
 constexpr int32_t kMaxPages = 1 << 27;
+// Workgroups of a launch, of 256 threads at most: it takes less than 2^32 threads.
+constexpr int64_t kMaxGroups = (1 << 24) - 1;
 
 rag_status check_shape(const char* who, int32_t hq, int32_t hkv, int32_t d) {
   if (hkv <= 0 || hq < 0)
@@ -169,7 +171,7 @@ rag_status rope(const char* who, rag::RopeArgs a, bool kv4, int32_t block_size, 
         return st;
   }
   if (check_mode() && (st = check_tokens(who, a, num_blocks, stream)) != RAG_OK) return st;
-  if (rag::rope_grid(a) > INT_MAX) return fail(RAG_ERR_UNSUPPORTED, "%s: too many tokens", who);
+  if (rag::rope_grid(a) > kMaxGroups) return fail(RAG_ERR_UNSUPPORTED, "%s: too many tokens", who);
   if (rag::launch_rope(a, kv4, stream) != hipSuccess)
     return fail(RAG_ERR_HIP, "%s: kernel launch failed", who);
   return ok();
@@ -311,7 +313,7 @@ rag_status rag_kv4_read(const void* k_cache, const void* v_cache, const int32_t*
   const rag::Kv4ReadArgs a{k_cache,  v_cache,  block_tables,       cu_seqlens_k, k,       v,
                            num_rows, num_seqs, max_blocks_per_seq, num_kv_heads, head_dim};
   if (check_mode() && (st = check_read(a, num_blocks, stream)) != RAG_OK) return st;
-  if (rag::kv4_read_grid(a) > INT_MAX) return fail(RAG_ERR_UNSUPPORTED, "kv4 read: too many rows");
+  if (rag::kv4_read_grid(a) > kMaxGroups) return fail(RAG_ERR_UNSUPPORTED, "kv4 read: too many rows");
   if (rag::launch_kv4_read(a, stream) != hipSuccess)
     return fail(RAG_ERR_HIP, "kv4 read: kernel launch failed");
   return ok();
@@ -364,7 +366,7 @@ rag_status rag_attn_decode_paged_kv4(const void* q, const void* k_cache, const v
   a.cols = t.cols;
   a.tiles = t.tiles;
   a.units = t.units;
-  if (rag::kv4_grid(t, num_seqs, num_kv_heads) > INT_MAX)
+  if (rag::kv4_grid(t, num_seqs, num_kv_heads) > kMaxGroups)
     return fail(RAG_ERR_UNSUPPORTED, "decode kv4: too many sequences");
   const Kv4Ws ws = kv4_workspace(t, num_kv_heads, head_dim);
   if (ws.bytes > 0) {
@@ -454,7 +456,7 @@ rag_status rag_draft_verify(const void* logits, int32_t logits_fp32, int64_t log
     for (int j = i + 1; j < 11; ++j)
       if ((st = check_apart("draft verify", spans[i], spans[j])) != RAG_OK) return st;
   if (check_mode() && (st = check_verify(a, stream)) != RAG_OK) return st;
-  if (rag::verify_grid(a) > INT_MAX)
+  if (rag::verify_grid(a) > kMaxGroups)
     return fail(RAG_ERR_UNSUPPORTED, "draft verify: too many rows of %d tokens", vocab);
   if (rag::launch_verify(a, stream) != hipSuccess)
     return fail(RAG_ERR_HIP, "draft verify: kernel launch failed");

@@ -112,6 +112,24 @@ def test_attention_refusals(kw, status):
 
 
 @needs_lib
+def test_launches_of_too_many_threads_are_refused():
+    """A launch takes less than 2^32 threads: 2^24 workgroups of 256."""
+    L = binding.lib()
+    most = (1 << 31) - 1
+    kw = dict(ROPE, hq=1, hkv=1, d=64, rot=64, qs=64, ks=64, vs=64, T=most)
+    for i, name in enumerate(("q", "k", "v", "qo", "ko", "vo", "kc", "vc")):
+        kw[name] = FAKE + i * (1 << 40)
+    _says(L.rag_qkv_rope_write(*kw.values(), None), NO)
+    _says(L.rag_kv4_read(*dict(READ, T=most, hkv=8).values(), None), NO)
+    kw = dict(ATTN, S=1 << 19, hkv=32, cu=None)
+    _says(L.rag_attn_decode_paged_kv4(*kw.values(), None), NO)
+    kw = dict(VERIFY, T=1 << 20, V=1 << 20, ls=1 << 20, parents=None, ws_bytes=1 << 60)
+    for i, name in enumerate(("logits", "tokens", "cu", "heat", "u", "kept", "n", "nxt", "ws")):
+        kw[name] = FAKE + i * (1 << 44)
+    _says(L.rag_draft_verify(*kw.values(), None), NO)
+
+
+@needs_lib
 def test_attention_workspace_serves_smaller_calls():
     size = binding.rag_attn_decode_kv4_workspace_size
     for hq, hkv, d in ((32, 8, 128), (64, 8, 128), (14, 2, 64), (512, 512, 128)):
