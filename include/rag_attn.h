@@ -645,7 +645,8 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
  * step, or a chain of drafted tokens judged in one step (rag_draft_verify).  K and V of
  * the rows are in the cache already (rag_qkv_rope_write_kv4).
  *
- *   q, o     device [Tq, num_q_heads, head_dim]; o is output, written in full
+ *   q, o     device [Tq, num_q_heads, head_dim]; o is output, written up to row
+ *            cu[num_seqs]
  *   k_cache, v_cache  as in rag_qkv_rope_write_kv4
  *   block_tables, num_blocks, block_size  as in rag_attn_decode_paged
  *   kv_lens  device int32 [num_seqs]: keys of sequence s, counting those of its rows
