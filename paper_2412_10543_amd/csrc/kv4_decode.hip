@@ -12,16 +12,26 @@
 // row.  Sums and maxima are fp32; p' is rounded to bf16 for the matrix unit, as P is in the
 // bf16 cache's kernels, and the correction uses the rounded p', so that 128 cancels.
 //
-// Blocks of two pages (32 keys) are copied straight into LDS, kQStages - 1 of them ahead, with
-// 16 bytes a lane and lanes in the pages' order, parameters with a load of their lines: a load that
-// finds a line still on its way holds up all behind it (64 sequences of 2.6k to 10.3k keys: 98 us
-// with the codes loaded as the matrix operands have them, 113 with the parameters' lines read
-// where they are needed).  Each of a workgroup's four waves copies every fourth block.  Up to 16
-// pairs, each attends the blocks that it has copied; for up to 32, two and two do with 16 pairs
-// each every second block; for up to 64 all four do every block.  They join their states through
-// LDS.  As many workgroups as the chip takes at a time get even shares of all sequences' blocks;
-// a sequence that is cut writes partial outputs and log-sum-exps, which the last of its
-// workgroups to finish joins.
+// HBM-bound where each sequence has few pairs (64 sequences of 2.6k to 10.3k keys, 32 q / 8 kv heads of
+// 128: 88 us, 4.8 TB/s); with 16 to 64 pairs a sequence bound by the chains of product, softmax and
+// product of the two waves that a SIMD has room for (32 chains of 3 to 9 rows, 700 to 10,304 keys: 61 us,
+// vector units 43% busy, matrix units 11%).
+//
+// Pages are copied straight into LDS with 16 bytes a lane and lanes in the pages' order, parameters with
+// a load of their lines: a load that finds a line still on its way holds up all behind it (the 64
+// sequences: 98 us with the codes loaded as the matrix operands have them, 113 with the parameters'
+// lines read where they are needed).
+//   up to 8 pairs   kv4_wave_few: a wave has four pages at a time, and spreads them over the matrix
+//                   unit's columns that no pair needs
+//   up to 64        kv4_wave: blocks of two pages, kQStages - 1 of them ahead, of which each of the four
+//                   waves copies every fourth.  Up to 32 pairs a wave attends the blocks that it has
+//                   copied, with one or two tiles of 16 pairs (the codes are unpacked once: 61 us for the
+//                   32 chains, 64 with a tile a wave and two waves beside each other); for up to 64 two
+//                   and two waves have half of the pairs each and every second block.
+//   more            tiles of 64 pairs
+// The waves join their states through LDS.  As many workgroups as the chip takes at a time get even shares
+// of all sequences' blocks; a sequence that is cut writes partial outputs and log-sum-exps, which
+// the last of its workgroups to finish joins.
 #include "common.h"
 #include "kv4.h"
 #include "serve.h"
@@ -35,15 +45,15 @@ namespace {
 constexpr int kQWaves = 4;
 constexpr int kQKeys = 32;                 // keys of a block
 constexpr int kQPairs = 16 * kQWaves;      // pairs of a tile, at most
-// Blocks of a share, at least.  One sequence of 4,782 keys, 32 q / 8 kv heads: 13.9 us; cut down to 4
-// blocks 16.8 (more partials to join), to 16 14.0.
+// Blocks of a share, at least.  One sequence of 4,782 keys, 32 q / 8 kv heads: 13.6 us; cut down to 4
+// blocks 2.9 more (more partials to join), to 16 0.1 more.
 constexpr int kQMinBlocks = 8;
-// Blocks that the start of a tile counts for (32 chains of 3 to 9 rows, 700 to 10,304 keys: 66 us;
-// with 20 67.7).
-constexpr int kQStart = 12;
+// Blocks that the start of a tile counts for: a workgroup's second piece costs 10 to 20 us more than its
+// blocks (plan, first loads, states, partials; the 32 chains: 61 us; with 18 62.5, 32 63.8).
+constexpr int kQStart = 24;
 constexpr int kQMaxPieces = 64;            // of a tile (one lane each in the join)
-// Workgroups: two a CU, as many as there is LDS for (1024: 64 sequences of 2.6k to 10.3k keys 104 us
-// against 92).
+// Workgroups: two a CU, as many as there is LDS for (1024: 64 sequences of 2.6k to 10.3k keys 12 us
+// more).
 constexpr int kQWorkgroups = 512;
 
 // One row tile's piece of work: blocks [b0, b1) of its n.
@@ -77,14 +87,14 @@ struct alignas(16) Kv4Four {
   static constexpr int kOps = D == 128 ? 12 : 6;     // loads that fill one
 };
 
-template <int D, int R>
+template <int D, int R, int C>
 struct Kv4Lds {
   union {
     Kv4Block<D> ring[R == 1 ? kQStages : 0][kQWaves];
     Kv4Four<D> four[R == 1 ? 0 : kQWaves][2];
-    float o[kQWaves][16 / R][D + 4];
+    float o[kQWaves][16 * C / R][D + 4];
   };
-  float m[kQWaves][16], l[kQWaves][16];
+  float m[kQWaves][16 * C], l[kQWaves][16 * C];
   int start[kKv4PlanSeqs + 1];
   int wave_sum[kQWaves], longest[kQWaves], flag;
   Kv4Piece piece;
@@ -106,9 +116,8 @@ __device__ __forceinline__ void kv4_sequence(const Kv4Args& a, int s, int& qb, i
 }
 
 // Waves beside each other on a block, for this many pairs.
-__device__ __forceinline__ int kv4_side(int pairs) { return pairs <= 16 ? 1 : pairs <= 32 ? 2 : 4; }
-// A block's work: what waves beside each other add to it is about half of what the block takes
-// (32 chains of 3 to 9 rows: 66 us; counted as 1 : 1 : 1 70, 1 : 2 : 4 75, 2 : 3 : 3 72, 3 : 4 : 5 71).
+__device__ __forceinline__ int kv4_side(int pairs) { return pairs <= 32 ? 1 : 2; }
+// A block's work.  (The 32 chains: 61 us; with 3 : 4 : 7 61.3, 2 : 3 : 5 and 3 : 4 : 6 62.)
 __device__ __forceinline__ int kv4_weight(int pairs) { return pairs <= 16 ? 2 : pairs <= 32 ? 3 : 4; }
 constexpr int kQMaxWeight = 4;
 
@@ -186,7 +195,8 @@ __device__ __forceinline__ Kv4Piece kv4_find(const Kv4Args& a, Lds& lds, const K
       const int t0 = lds.start[s] + x.tile * len, t1 = t0 + len;
       x.b0 = max((g - t0) / weight - kQStart, 0);
       x.b1 = max((min(to, t1) - t0) / weight - kQStart, 0);
-      x.first = t0 / plan.share;
+      // (a unit whose share ends before the tile's first block has no piece of it)
+      x.first = min(t0 + kQStart * weight, t1 - 1) / plan.share;
       x.n = (t1 - 1) / plan.share - x.first + 1;
       x.p = unit - x.first;
       x.next = min(to, t1) - from;
@@ -253,11 +263,11 @@ __device__ __forceinline__ float column_max(float x) {
 // Memory and the waits around it, in the order that they are written in.
 __device__ __forceinline__ void kv4_fence() { asm volatile("" ::: "memory"); }
 
-// The wave's 16 pairs (pair0 on) against the piece's blocks, `side` waves beside each other on each
-// of them; a wave whose pairs are none copies its blocks for the others.
-template <int D>
+// The wave's 16 C pairs (pair0 on) against the piece's blocks, `side` waves beside each other on each
+// of them.  With C = 2 both tiles of pairs take the codes as they were unpacked once.
+template <int D, int C, class Lds>
 __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, int h, int pair0, int side,
-                                         Kv4Lds<D, 1>& lds, Kv4State<D>& st) {
+                                         Lds& lds, Kv4State<D> (&st)[C]) {
   constexpr int kG = D / 64;
   using P = Kv4Page<D>;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
@@ -308,33 +318,38 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
     find(x.b0 + (kQStages - 1) * kQWaves + wave);
   }
 
-  const int pair = min(pair0 + l16, pairs - 1), row = pair / group;
-  const int last = x.kv_len - x.rows + row;        // the last key that the lane's column sees
-  const bf16_t* src = (const bf16_t*)a.q + ((size_t)(x.qb + row) * a.hq + h * group + pair % group) * D;
-  bf16x8 q[2 * kG];
-  bf16x8 qz[kG];                           // minus the sum of q, in three parts
+  int last[C];                             // the last key that the lane's column sees
+  bf16x8 q[C][2 * kG];
+  bf16x8 qz[C][kG];                        // minus the sum of q, in three parts
 #pragma unroll
-  for (int g = 0; g < kG; ++g) {
-    float sum = 0.f;
+  for (int t = 0; t < C; ++t) {
+    const int pair = min(pair0 + 16 * t + l16, pairs - 1), row = pair / group;
+    last[t] = x.kv_len - x.rows + row;
+    const bf16_t* src = (const bf16_t*)a.q + ((size_t)(x.qb + row) * a.hq + h * group + pair % group) * D;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const u32x4 y = load16(src + 64 * g + 16 * g4 + 8 * w);
-      q[2 * g + w] = as_bf16x8(y);
+    for (int g = 0; g < kG; ++g) {
+      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        sum += __uint_as_float(y[i] << 16) + __uint_as_float(y[i] & 0xffff0000u);
+      for (int w = 0; w < 2; ++w) {
+        const u32x4 y = load16(src + 64 * g + 16 * g4 + 8 * w);
+        q[t][2 * g + w] = as_bf16x8(y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sum += __uint_as_float(y[i] << 16) + __uint_as_float(y[i] & 0xffff0000u);
+      }
+      sum += wave_xor(sum, 16);
+      sum += wave_xor(sum, 32);
+      const float part0 = (float)(__bf16)-sum, part1 = (float)(__bf16)(-sum - part0);
+      const float on = g4 == 0 ? 1.f : 0.f;
+      qz[t][g] =
+          to_bf16x8(part0 * on, part1 * on, (-sum - part0 - part1) * on, 0.f, 0.f, 0.f, 0.f, 0.f);
+      st[t].corr[g] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    sum += wave_xor(sum, 16);
-    sum += wave_xor(sum, 32);
-    const float part0 = (float)(__bf16)-sum, part1 = (float)(__bf16)(-sum - part0);
-    const float on = g4 == 0 ? 1.f : 0.f;
-    qz[g] = to_bf16x8(part0 * on, part1 * on, (-sum - part0 - part1) * on, 0.f, 0.f, 0.f, 0.f, 0.f);
-    st.corr[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  st.l = 0.f;
-  st.m = -INFINITY;
+    st[t].l = 0.f;
+    st[t].m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < D / 16; ++i) st[t].o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
   // where the lane's operands stand in a page's codes
   const int at = kG == 2 ? 16 * (4 * l16 + ((g4 + (l16 >> 2)) & 3)) : 8 * (4 * l16 + g4);
@@ -343,7 +358,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
     const int key0 = kQKeys * b;
     const uint32_t* params = r.p;
     // ---- S^T = K Q^T ---------------------------------------------------------------
-    float sc[8];
+    float sc[C][8];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       uint32_t code[2 * kG];
@@ -352,19 +367,25 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
       for (int g = 0; g < kG; ++g) {
         const uint32_t kz = params[kv4_place<D>(j, 0, g) + l16];
         const uint32_t zz = __builtin_amdgcn_perm(kz, kz, 0x01000100u);
-        f32x4 acc = mfma16(kv4_operand(zz, zz, zz, zz), qz[g], f32x4{0.f, 0.f, 0.f, 0.f});
+        f32x4 acc[C];
+#pragma unroll
+        for (int t = 0; t < C; ++t)
+          acc[t] = mfma16(kv4_operand(zz, zz, zz, zz), qz[t][g], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           const uint32_t y = code[2 * g + w];
-          acc = mfma16(kv4_operand(unpack(y, 0), unpack(y, 1), unpack(y, 2), unpack(y, 3)),
-                       q[2 * g + w], acc);
+          const bf16x8 k = kv4_operand(unpack(y, 0), unpack(y, 1), unpack(y, 2), unpack(y, 3));
+#pragma unroll
+          for (int t = 0; t < C; ++t) acc[t] = mfma16(k, q[t][2 * g + w], acc[t]);
         }
         const u32x4 kp = *reinterpret_cast<const u32x4*>(params + kv4_place<D>(j, 0, g) + 4 * g4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float s = kv4_scale(kp[i]);
-          sc[4 * j + i] = g == 0 ? s * acc[i] : fmaf(s, acc[i], sc[4 * j + i]);
-        }
+        for (int t = 0; t < C; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float s = kv4_scale(kp[i]);
+            sc[t][4 * j + i] = g == 0 ? s * acc[t][i] : fmaf(s, acc[t][i], sc[t][4 * j + i]);
+          }
       }
     }
     u32x4 vp[2][kG];
@@ -381,7 +402,9 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = key0 + 16 * (i / 4) + 4 * g4 + i % 4;
-        if (key > last) sc[i] = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < C; ++t)
+          if (key > last[t]) sc[t][i] = -INFINITY;
 #pragma unroll
         for (int g = 0; g < kG; ++g) {     // (zero points alike for all columns: none that is NaN)
           const uint32_t y = key < x.kv_len ? vp[i / 4][g][i % 4] : 0;
@@ -390,38 +413,45 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
       }
     }
     // ---- softmax ------------------------------------------------------------------------
-    float top = sc[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
-    top = column_max(top);
-    if (wave_any(top > st.m + tau)) {
-      const float m = fmaxf(st.m, top);
-      const float alpha = st.m == -INFINITY ? 0.f : fast_exp2((st.m - m) * c);
-      st.l *= alpha;
+    for (int t = 0; t < C; ++t) {
+      float top = sc[t][0];
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) st.o[i] *= alpha;
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[t][i]);
+      top = column_max(top);
+      if (wave_any(top > st[t].m + tau)) {
+        const float m = fmaxf(st[t].m, top);
+        const float alpha = st[t].m == -INFINITY ? 0.f : fast_exp2((st[t].m - m) * c);
+        st[t].l *= alpha;
 #pragma unroll
-      for (int g = 0; g < kG; ++g) st.corr[g] *= alpha;
-      st.m = m;
-    }
-    const float ref = st.m == -INFINITY ? 0.f : -st.m * c;
+        for (int i = 0; i < D / 16; ++i) st[t].o[i] *= alpha;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sc[i] = fast_exp2(fmaf(sc[i], c, ref));
-      st.l += sc[i];
+        for (int g = 0; g < kG; ++g) st[t].corr[g] *= alpha;
+        st[t].m = m;
+      }
+      const float ref = st[t].m == -INFINITY ? 0.f : -st[t].m * c;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sc[t][i] = fast_exp2(fmaf(sc[t][i], c, ref));
+        st[t].l += sc[t][i];
+      }
     }
     // ---- O^T += V^T P^T ---------------------------------------------------------------------
 #pragma unroll
     for (int g = 0; g < kG; ++g) {
-      float y[8];
+      bf16x8 pf[C];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = sc[i] * kv4_scale(vp[i / 4][g][i % 4]);
-      if constexpr (masked) {              // (the scale of a key not seen may be NaN)
+      for (int t = 0; t < C; ++t) {
+        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (key0 + 16 * (i / 4) + 4 * g4 + i % 4 > last) y[i] = 0.f;
+        for (int i = 0; i < 8; ++i) y[i] = sc[t][i] * kv4_scale(vp[i / 4][g][i % 4]);
+        if constexpr (masked) {            // (the scale of a key not seen may be NaN)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (key0 + 16 * (i / 4) + 4 * g4 + i % 4 > last[t]) y[i] = 0.f;
+        }
+        pf[t] = to_bf16x8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
       }
-      const bf16x8 pf = to_bf16x8(y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]);
       uint32_t w[4], zz[4];                // two keys' units of group g, and their zero points
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -433,12 +463,15 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
           w[i] = __builtin_amdgcn_perm(v[i / 2][i % 2 * 2 + 1], v[i / 2][i % 2 * 2],
                                        g == 0 ? 0x05040100u : 0x07060302u);
       }
-      st.corr[g] = mfma16(kv4_operand(zz[0], zz[1], zz[2], zz[3]), pf, st.corr[g]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        st.o[4 * g + e] = mfma16(kv4_operand(unpack(w[0], e), unpack(w[1], e), unpack(w[2], e),
-                                             unpack(w[3], e)),
-                                 pf, st.o[4 * g + e]);
+      for (int t = 0; t < C; ++t)
+        st[t].corr[g] = mfma16(kv4_operand(zz[0], zz[1], zz[2], zz[3]), pf[t], st[t].corr[g]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bf16x8 vv = kv4_operand(unpack(w[0], e), unpack(w[1], e), unpack(w[2], e), unpack(w[3], e));
+#pragma unroll
+        for (int t = 0; t < C; ++t) st[t].o[4 * g + e] = mfma16(vv, pf[t], st[t].o[4 * g + e]);
+      }
     }
   };
   // Blocks base .. base + 3 stand in stage `stage`.  Waits for the wave's own copies (and, where waves
@@ -454,15 +487,13 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
     copy(stage == 0 ? kQStages - 1 : stage - 1);
     find(base + kQStages * kQWaves + wave);
   };
-  const bool active = pair0 < pairs;
   const int open = (x.kv_len - x.rows + 1) / kQKeys;     // blocks that all rows see whole
   auto blocks = [&](int& base, int to, auto masked_t) {
     for (; base < to; base += kQWaves) {
       turn();
       refill(base);
-      if (active)
-        for (int j = wave / side; j < kQWaves && base + j < x.b1; j += kQWaves / side)
-          block(lds.ring[stage][j], base + j, masked_t);
+      for (int j = wave / side; j < kQWaves && base + j < x.b1; j += kQWaves / side)
+        block(lds.ring[stage][j], base + j, masked_t);
       stage = stage == kQStages - 1 ? 0 : stage + 1;
     }
   };
@@ -474,12 +505,15 @@ __device__ __forceinline__ void kv4_wave(const Kv4Args& a, const Kv4Piece& x, in
   kv4_fence();
   __builtin_amdgcn_s_waitcnt(0);           // (copies that nobody waited for)
   kv4_fence();
-  st.l += wave_xor(st.l, 16);
-  st.l += wave_xor(st.l, 32);
 #pragma unroll
-  for (int g = 0; g < kG; ++g)
+  for (int t = 0; t < C; ++t) {
+    st[t].l += wave_xor(st[t].l, 16);
+    st[t].l += wave_xor(st[t].l, 32);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) st.o[4 * g + e] -= st.corr[g];
+    for (int g = 0; g < kG; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st[t].o[4 * g + e] -= st[t].corr[g];
+  }
 }
 
 // x of the lanes 4 (R = 4) or 8 (R = 2, 4) before this one in its 16, around.
@@ -733,110 +767,162 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
         st.o[4 * g + e][r] = kv4_class_sum<R>(st.o[4 * g + e][r] - st.corr[g][r]);
 }
 
-// Join of a cut tile's pieces: piece p's partials are at place 2 (first + p), + 1 for p = 0.
-template <int D>
+// Join of a cut tile's pieces: piece p's partials are at place 2 (first + p), + 1 for p = 0.  A wave has
+// kRows rows' reads on their way at a time, of eight pieces each.
+template <int D, int kRows>
 __device__ __forceinline__ void kv4_join(const Kv4Args& a, const Kv4Piece& x, int h) {
   const int C = a.cols;
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
   const int have = min(kQPairs, x.rows * group - x.tile * kQPairs);
   auto place = [&](int p) { return ((size_t)(2 * (x.first + p) + (p == 0)) * a.hkv + h) * C; };
-  for (int i = threadIdx.x >> 6; i < have; i += kQWaves) {
-    // (eight pieces' rows are requested at a time, the first beside the log-sum-exps)
-    float y[8][kPer];
-    auto request = [&](int p0) {
+  auto request = [&](float (&y)[8][kPer], int i, int p0) {
 #pragma unroll
-      for (int p = 0; p < 8; ++p)
-        load_coherent_vec<kPer>(a.part_o + (place(min(p0 + p, x.n - 1)) + i) * D + lane * kPer, y[p]);
-    };
-    const float lse = lane < x.n ? load_coherent(a.part_lse + place(lane) + i) : -INFINITY;
-    request(0);
-    float top = lse;
+    for (int p = 0; p < 8; ++p)
+      load_coherent_vec<kPer>(a.part_o + (place(min(p0 + p, x.n - 1)) + i) * D + lane * kPer, y[p]);
+  };
+  for (int i0 = wave_id(); i0 < have; i0 += kRows * kQWaves) {
+    float lse[kRows], y[kRows][8][kPer];
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, wave_xor(top, m));
-    const float w = lse == -INFINITY ? 0.f : fast_exp2(lse - top);
-    float sum = w;
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) sum += wave_xor(sum, m);
-    float acc[kPer] = {};
-    for (int p0 = 0; p0 < x.n; p0 += 8) {
-      if (p0 > 0) request(p0);
-#pragma unroll
-      for (int p = 0; p < 8; ++p) {
-        const float wp = __uint_as_float(
-            __builtin_amdgcn_readlane(__float_as_uint(w), min(p0 + p, kWave - 1)));
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] += p0 + p >= x.n || wp == 0.f ? 0.f : wp * y[p][e];
-      }
+    for (int t = 0; t < kRows; ++t) {
+      const int i = min(i0 + t * kQWaves, have - 1);
+      lse[t] = lane < x.n ? load_coherent(a.part_lse + place(lane) + i) : -INFINITY;
+      request(y[t], i, 0);
     }
-    const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
-    const int pair = x.tile * kQPairs + i;
-    bf16_t* o = (bf16_t*)a.o + ((size_t)(x.qb + pair / group) * a.hq + h * group + pair % group) * D;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const __bf16 y = (__bf16)(acc[e] * inv);
-      o[lane * kPer + e] = __builtin_bit_cast(bf16_t, y);
+    for (int t = 0; t < kRows; ++t) {
+      const int i = i0 + t * kQWaves;
+      if (i >= have) break;
+      float top = lse[t];
+#pragma unroll
+      for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, wave_xor(top, m));
+      const float w = lse[t] == -INFINITY ? 0.f : fast_exp2(lse[t] - top);
+      float sum = w;
+#pragma unroll
+      for (int m = 32; m >= 1; m >>= 1) sum += wave_xor(sum, m);
+      float acc[kPer] = {};
+      for (int p0 = 0; p0 < x.n; p0 += 8) {
+        if (p0 > 0) request(y[t], i, p0);
+#pragma unroll
+        for (int p = 0; p < 8; ++p) {
+          const float wp = __uint_as_float(
+              __builtin_amdgcn_readlane(__float_as_uint(w), min(p0 + p, kWave - 1)));
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) acc[e] += p0 + p >= x.n || wp == 0.f ? 0.f : wp * y[t][p][e];
+        }
+      }
+      const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+      const int pair = x.tile * kQPairs + i;
+      bf16_t* o = (bf16_t*)a.o + ((size_t)(x.qb + pair / group) * a.hq + h * group + pair % group) * D;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const __bf16 z = (__bf16)(acc[e] * inv);
+        o[lane * kPer + e] = __builtin_bit_cast(bf16_t, z);
+      }
     }
   }
 }
 
-template <int D, int R>
-__device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, int h, Kv4Lds<D, R>& lds) {
+template <int D, int R, int C>
+__device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, int h, Kv4Lds<D, R, C>& lds) {
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4, wave = wave_id();
   const int group = a.hq / a.hkv, pair0 = x.tile * kQPairs, have = min(x.rows * group - pair0, kQPairs);
-  // the waves: `side` column tiles of 16 pairs beside each other
-  const int side = kv4_side(have), mine = wave % side;
+  // the waves: `side` of them beside each other, of 16 C pairs each
+  const int side = C == 1 ? 1 : kv4_side(have), mine = wave % side;
   const float c = a.scale * kLog2e;
-  {
-    Kv4State<D> st;
-    if constexpr (R == 1)
-      kv4_wave<D>(a, x, h, pair0 + 16 * mine, side, lds, st);
-    else
-      kv4_wave_few<D, R>(a, x, h, lds.four[wave], st);
-    __syncthreads();                       // (the blocks make room for the states)
-    if (16 * mine < have && l16 < 16 / R) {
+  auto keep = [&](const Kv4State<D>& st, int t) {
+    if (l16 < 16 / R) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          lds.o[wave][l16][64 * (i / 4) + 4 * (4 * g4 + r) + i % 4] = st.o[i][r];
+          lds.o[wave][16 * t + l16][64 * (i / 4) + 4 * (4 * g4 + r) + i % 4] = st.o[i][r];
       if (g4 == 0) {
-        lds.m[wave][l16] = st.m;
-        lds.l[wave][l16] = st.l;
+        lds.m[wave][16 * t + l16] = st.m;
+        lds.l[wave][16 * t + l16] = st.l;
       }
     }
+  };
+  // (waves beside each other may differ in their number of tiles; either way they pass the same number of
+  // barriers: one for every kQWaves of the piece's blocks, and one behind them)
+  if (C == 2 && have > 16 * (2 * mine + 1)) {
+    if constexpr (C == 2) {
+      Kv4State<D> st[2];
+      kv4_wave<D, 2>(a, x, h, pair0 + 32 * mine, side, lds, st);
+      __syncthreads();                     // (the blocks make room for the states)
+      keep(st[0], 0);
+      keep(st[1], 1);
+    }
+  } else {
+    Kv4State<D> st[1];
+    if constexpr (R == 1)
+      kv4_wave<D, 1>(a, x, h, pair0 + 32 * mine, side, lds, st);
+    else
+      kv4_wave_few<D, R>(a, x, h, lds.four[wave], st[0]);
+    __syncthreads();
+    keep(st[0], 0);
   }
   __syncthreads();
-  for (int i = wave; i < have; i += kQWaves) {
-    const int pair = pair0 + i, row = i % 16;
-    float top = -INFINITY, sum = 0.f, acc[kPer] = {};
-    for (int w = i / 16; w < kQWaves; w += side) top = fmaxf(top, lds.m[w][row]);
-    for (int w = i / 16; w < kQWaves; w += side) {
-      const float m = lds.m[w][row], f = m == -INFINITY ? 0.f : fast_exp2((m - top) * c);
-      sum += m == -INFINITY ? lds.l[w][row] : f * lds.l[w][row];
+  // (a wave has some rows' reads on their way at a time: one after another a row takes a microsecond)
+  auto join = [&](auto side_t) {
+    constexpr int kSide = decltype(side_t)::value, kStates = kQWaves / kSide;
+    constexpr int kRows = R == 1 ? 4 : 4 / R;
+    for (int i0 = wave; i0 < have; i0 += kRows * kQWaves) {
+      float m[kRows][kStates], l[kRows][kStates], y[kRows][kStates][kPer];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] += f * lds.o[w][row][lane * kPer + e];
-    }
-    // (a sum that is NaN, from keys that are, stays: the row is NaN)
-    const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
-    if (x.n == 1) {
-      bf16_t* o = (bf16_t*)a.o + ((size_t)(x.qb + pair / group) * a.hq + h * group + pair % group) * D;
+      for (int t = 0; t < kRows; ++t) {
+        const int i = min(i0 + t * kQWaves, have - 1), row = i % (16 * C), w0 = i / (16 * C);
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const __bf16 y = (__bf16)(acc[e] * inv);
-        o[lane * kPer + e] = __builtin_bit_cast(bf16_t, y);
+        for (int k = 0; k < kStates; ++k) {
+          const int w = w0 + k * kSide;
+          m[t][k] = lds.m[w][row];
+          l[t][k] = lds.l[w][row];
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) y[t][k][e] = lds.o[w][row][lane * kPer + e];
+        }
       }
-    } else {
-      const size_t at = ((size_t)(2 * (x.first + x.p) + (x.p == 0)) * a.hkv + h) * a.cols + i;
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) store_coherent(a.part_o + at * D + lane * kPer + e, acc[e] * inv);
-      if (lane == 0)
-        store_coherent(a.part_lse + at, sum > 0.f   ? top * c + __log2f(sum)
-                                        : sum == sum ? -INFINITY
-                                                     : sum);
+      for (int t = 0; t < kRows; ++t) {
+        const int i = i0 + t * kQWaves, pair = pair0 + i;
+        if (i >= have) break;
+        float top = m[t][0], sum = 0.f, acc[kPer] = {};
+#pragma unroll
+        for (int k = 1; k < kStates; ++k) top = fmaxf(top, m[t][k]);
+#pragma unroll
+        for (int k = 0; k < kStates; ++k) {
+          const float f = m[t][k] == -INFINITY ? 0.f : fast_exp2((m[t][k] - top) * c);
+          sum += m[t][k] == -INFINITY ? l[t][k] : f * l[t][k];
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) acc[e] += f * y[t][k][e];
+        }
+        // (a sum that is NaN, from keys that are, stays: the row is NaN)
+        const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
+        if (x.n == 1) {
+          bf16_t* o =
+              (bf16_t*)a.o + ((size_t)(x.qb + pair / group) * a.hq + h * group + pair % group) * D;
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) {
+            const __bf16 z = (__bf16)(acc[e] * inv);
+            o[lane * kPer + e] = __builtin_bit_cast(bf16_t, z);
+          }
+        } else {
+          const size_t at = ((size_t)(2 * (x.first + x.p) + (x.p == 0)) * a.hkv + h) * a.cols + i;
+#pragma unroll
+          for (int e = 0; e < kPer; ++e)
+            store_coherent(a.part_o + at * D + lane * kPer + e, acc[e] * inv);
+          if (lane == 0)
+            store_coherent(a.part_lse + at, sum > 0.f   ? top * c + __log2f(sum)
+                                            : sum == sum ? -INFINITY
+                                                         : sum);
+        }
+      }
     }
-  }
+  };
+  if (side == 1)
+    join(std::integral_constant<int, 1>());
+  else
+    join(std::integral_constant<int, 2>());
   if (x.n == 1) return;
   // Every partial has gone out with device-coherent stores; once they have completed one
   // arrival is counted, and the workgroup that counts the last joins and clears the counter.
@@ -847,14 +933,14 @@ __device__ __forceinline__ void kv4_piece(const Kv4Args& a, const Kv4Piece& x, i
     lds.flag = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
   if (lds.flag != x.n - 1) return;
-  kv4_join<D>(a, x, h);
+  kv4_join<D, C == 2 ? 8 : 4 / R>(a, x, h);
   if (threadIdx.x == 0) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// R: 16 / R pairs a sequence at most (R = 1: any number).
-template <int D, int R>
+// Pairs a sequence: up to 16 / R, or, with C = 2, any number.
+template <int D, int R, int C>
 __global__ __launch_bounds__(64 * kQWaves, 2) void kv4_decode_kernel(Kv4Args a) {
-  __shared__ Kv4Lds<D, R> lds;
+  __shared__ Kv4Lds<D, R, C> lds;
   const int h = blockIdx.x % a.hkv, unit = blockIdx.x / a.hkv;
   Kv4Plan plan;
   if (a.units > 0) kv4_plan(a, lds, plan);
@@ -864,6 +950,7 @@ __global__ __launch_bounds__(64 * kQWaves, 2) void kv4_decode_kernel(Kv4Args a) 
       x = kv4_find(a, lds, plan, unit, at);
       if (x.s < 0) return;
       at = x.next;
+      if (x.p < 0) continue;
     } else {                               // a workgroup for each tile
       x.s = unit / a.tiles;
       x.tile = unit % a.tiles;
@@ -873,7 +960,7 @@ __global__ __launch_bounds__(64 * kQWaves, 2) void kv4_decode_kernel(Kv4Args a) 
       x.b1 = kv4_blocks(x.kv_len);
       x.n = 1;
     }
-    kv4_piece<D, R>(a, x, h, lds);
+    kv4_piece<D, R, C>(a, x, h, lds);
     if (a.units == 0) return;
   }
 }
@@ -903,11 +990,13 @@ template <int D>
 void launch_kv4_d(const Kv4Args& a, const Kv4Shape& t, hipStream_t stream) {
   const dim3 grid((unsigned)kv4_grid(t, a.num_seqs, a.hkv)), block(64 * kQWaves);
   if (t.cols <= 4)
-    kv4_decode_kernel<D, 4><<<grid, block, 0, stream>>>(a);
+    kv4_decode_kernel<D, 4, 1><<<grid, block, 0, stream>>>(a);
   else if (t.cols <= 8)
-    kv4_decode_kernel<D, 2><<<grid, block, 0, stream>>>(a);
+    kv4_decode_kernel<D, 2, 1><<<grid, block, 0, stream>>>(a);
+  else if (t.cols <= 16)
+    kv4_decode_kernel<D, 1, 1><<<grid, block, 0, stream>>>(a);
   else
-    kv4_decode_kernel<D, 1><<<grid, block, 0, stream>>>(a);
+    kv4_decode_kernel<D, 1, 2><<<grid, block, 0, stream>>>(a);
 }
 
 }  // namespace
