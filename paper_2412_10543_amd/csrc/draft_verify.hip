@@ -18,6 +18,12 @@
 // each row places the draw in a segment and reads that again; the last row of a sequence to finish
 // walks.  With them: workgroups for the one row a sequence whose next token is drawn find it
 // from the segments' sums, sum max(p - q, 0) in segments, and the last one draws.
+//
+// 16 trees of 24 to 64 nodes, 128,000 tokens in bf16: 72 us, 60 of them in the first launch, whose
+// vector units are busy for 65% (some 20 instructions a logit; rows at T = 0 alone take 36, at 5 TB/s),
+// and 12 in the second, a chain of dependent reads.  48 chains of 3 to 9 nodes with the drafter's
+// probabilities, 128,077 tokens in fp32: 52 us, 33 (4.8 TB/s) and 19.  One chain of five, 32,768
+// tokens: 11, of which the kernels wait for one another's first reads.
 #include "common.h"
 #include "serve.h"
 
@@ -199,11 +205,31 @@ __device__ __forceinline__ const void* logits_row(const VerifyArgs& a, int row) 
 }
 
 // ---- over the wave ----------------------------------------------------------------------
-__device__ __forceinline__ double wave_sum(double x) {
+// (by DPP and readlane: through LDS a sum of 64 bits takes a third of a microsecond)
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double dpp64(double x) {
+  u32x2 b = __builtin_bit_cast(u32x2, x);
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, kWave);
-  return x;
+  for (int i = 0; i < 2; ++i) b[i] = __builtin_amdgcn_update_dpp(0, b[i], kCtrl, kRows, 0xf, false);
+  return __builtin_bit_cast(double, b);
 }
+// x of a lane that is the same for the wave.
+__device__ __forceinline__ double lane_of(double x, int lane) {
+  u32x2 b = __builtin_bit_cast(u32x2, x);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) b[i] = __builtin_amdgcn_readlane(b[i], lane);
+  return __builtin_bit_cast(double, b);
+}
+// Sum of the lanes up to this one: within rows of 16, then over rows 0 and 2, then over row 1's end.
+__device__ __forceinline__ double wave_upto(double x) {
+  x += dpp64<0x111, 0xf>(x);
+  x += dpp64<0x112, 0xf>(x);
+  x += dpp64<0x114, 0xf>(x);
+  x += dpp64<0x118, 0xf>(x);
+  x += dpp64<0x142, 0xa>(x);
+  return x + dpp64<0x143, 0xc>(x);
+}
+__device__ __forceinline__ double wave_sum(double x) { return lane_of(wave_upto(x), kWave - 1); }
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) x = fmaxf(x, wave_xor(x, m));
@@ -216,13 +242,8 @@ __device__ __forceinline__ int wave_min(int x) {
 }
 // Sum of the lanes before this one, and of all.
 __device__ __forceinline__ double wave_before(double x, double& total) {
-  double y = x;
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) {
-    const double z = __shfl_up(y, m, kWave);
-    if ((int)(threadIdx.x & 63) >= m) y += z;
-  }
-  total = __shfl(y, kWave - 1, kWave);
+  const double y = wave_upto(x);
+  total = lane_of(y, kWave - 1);
   return y - x;
 }
 
@@ -313,7 +334,7 @@ __device__ __forceinline__ int segment_of(int segs, double target, F sums, doubl
     if (some != 0) {
       const int l = above != 0 ? __builtin_ctzll(above) : 63 - __builtin_clzll(some);
       last = c0 + l;
-      before = __shfl(b, l, kWave);
+      before = lane_of(b, l);
     }
     if (above != 0) break;
     all += total;
@@ -348,7 +369,7 @@ __device__ __forceinline__ int element_of(int e0, double before, double target, 
     const uint64_t any = __builtin_amdgcn_ballot_w64(some >= 0);
     if (any != 0) {
       const int l = above != 0 ? __builtin_ctzll(above) : 63 - __builtin_clzll(any);
-      last = e0 + v * kVStep + 8 * l + __shfl(above != 0 ? at : some, l, kWave);
+      last = e0 + v * kVStep + 8 * l + __builtin_amdgcn_readlane(above != 0 ? at : some, l);
     }
     if (above != 0) break;
     before += total;
@@ -627,10 +648,10 @@ __global__ __launch_bounds__(kVThreads) void verify_rest_kernel(VerifyArgs a) {
 
 // Loads of a segment of `rows` rows: as many as leave the GPU `fill` waves.
 constexpr int64_t kVFill = 8192;
-// One row a sequence: fewer and longer segments cost fewer arrivals (48 sequences, 128,077 tokens: 60 us
-// the call; with 1024 66, 4096 64, 8192 74).
+// One row a sequence: fewer and longer segments cost fewer arrivals (48 sequences, 128,077 tokens: with
+// 1024 6 us more, 4096 4 more, 8192 14 more).
 constexpr int64_t kVRestFill = 2048;
-// (Rows of eight loads a wave: 57 us against 55, 16 trees 78 against 76; of two 59 and 83.)
+// (Rows of eight loads a wave: both batches above 2 us more; of two 4 and 7 more.)
 constexpr int kVMaxLoads = 4, kVMaxRestLoads = 4;
 
 int verify_loads(int64_t rows, int vocab, int64_t fill, int kv) {
