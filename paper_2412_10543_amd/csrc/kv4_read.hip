@@ -1,10 +1,11 @@
 // Keys and values of sequences in a 4-bit paged cache, back as packed bf16 rows
 // (gfx950): what a prefill over keys that are in the cache already takes.
 //
-// HBM-bound, by the rows written (24,600 keys of 8 heads of 128: 30 us, 4.3 TB/s of codes and rows).  A wave takes one page of a few kv heads, one after another: a
-// lane has 16 bytes of K codes (one key, 16 channels of each group) and 16 of V codes (four keys,
-// four channels of each group), each load in the page's order, and one or two parameters, which
-// reach the lanes that need them by shuffles.
+// HBM-bound, by the rows written (24,600 keys of 8 heads of 128: 30 us, 4.3 TB/s of codes and
+// rows).  A wave takes one page of a few kv heads, one after another: a lane has 16 bytes of K
+// codes (one key, 16 channels of each group) and 16 of V codes (four keys, four channels of each
+// group), each load in the page's order, and one or two parameters, which reach the lanes that
+// need them by shuffles.
 #include "common.h"
 #include "kv4.h"
 #include "serve.h"
