@@ -74,6 +74,20 @@ def test_chains(hq, hkv, d):
         _check(kv, rows, hq, hkv, d, seed=most)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (2, 2, 128), (3, 1, 128)])
+def test_numbers_of_pairs_around_the_tiles_of_16(hq, hkv, d):
+    """Sequences on both sides of every number of tiles, some cut into pieces, in one batch; with those
+    beside them that have no keys to cut."""
+    group = hq // hkv
+    rows = [(p + group - 1) // group for p in (16, 17, 32, 33, 48, 49, 64, 65, 1, 8, 130)] + [0, 1]
+    r = random.Random(hq)
+    kv = [n + r.choice([0, 1, 30, 500, 2500]) for n in rows[:-2]] + [77, 1]
+    _check(kv, rows, hq, hkv, d, seed=31)
+    order = list(range(len(kv)))
+    r.shuffle(order)
+    _check([kv[i] + 600 * (rows[i] > 0) for i in order], [rows[i] for i in order], hq, hkv, d, seed=32)
+
+
 @pytest.mark.parametrize("k_scale", [4.0, 12.0])
 def test_peaked_scores(k_scale):
     _check([900, 40, 3000], [1, 3, 2], 8, 2, 128, 5, k_scale)
