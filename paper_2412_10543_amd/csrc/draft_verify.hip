@@ -19,7 +19,7 @@
 // walks.  With them: workgroups for the one row a sequence whose next token is drawn find it
 // from the segments' sums, sum max(p - q, 0) in segments, and the last one draws.
 //
-// 16 trees of 24 to 64 nodes, 128,000 tokens in bf16: 72 us, 60 of them in the first launch, whose
+// 16 trees of 24 to 64 nodes, 128,000 tokens in bf16: 70 us, 58 of them in the first launch, whose
 // vector units are busy for 65% (some 20 instructions a logit; rows at T = 0 alone take 36, at 5 TB/s),
 // and 12 in the second, a chain of dependent reads.  48 chains of 3 to 9 nodes with the drafter's
 // probabilities, 128,077 tokens in fp32: 52 us, 33 (4.8 TB/s) and 19.  One chain of five, 32,768
