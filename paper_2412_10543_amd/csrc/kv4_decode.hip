@@ -109,9 +109,11 @@ __device__ __forceinline__ int wave_scan(int x) {       // inclusive
   return x;
 }
 
+// (Tiles and partials are laid out for max_rows; more are a broken precondition, of which the first
+// max_rows are attended.)
 __device__ __forceinline__ void kv4_sequence(const Kv4Args& a, int s, int& qb, int& rows, int& kv) {
   qb = a.cu_q != nullptr ? a.cu_q[s] : s;
-  rows = a.cu_q != nullptr ? a.cu_q[s + 1] - qb : 1;
+  rows = a.cu_q != nullptr ? min(a.cu_q[s + 1] - qb, a.max_rows) : 1;
   kv = min(a.kv_lens[s], a.max_blocks * 16);
 }
 

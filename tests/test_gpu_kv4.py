@@ -252,3 +252,30 @@ def test_shapes_are_refused():
                  (kc, vc[..., 8:].contiguous(), table, _cu([40]), k, k.clone())):
         with pytest.raises((ValueError, binding.RagError)):
             binding.rag_kv4_read(*args)
+
+
+@pytest.mark.parametrize("max_rows,hq,hkv,d", [(1, 32, 8, 128), (2, 8, 2, 64), (5, 8, 2, 128), (17, 4, 1, 128)])
+def test_rows_past_the_host_s_bound_stay_inside_the_workspace(max_rows, hq, hkv, d):
+    """A broken precondition (a sequence of more rows than max_seqlen_q), which the call is not
+    told of: it writes neither behind its workspace nor the rows past the bound, and sequences
+    inside it are attended as alone."""
+    rows, kv = [max_rows + 8, max_rows, 1, 3 * max_rows + 40], [5000, 3000, 700, 9000]
+    q, kc, vc, table = _case(kv, rows, hq, hkv, d, 21)
+    size = binding.rag_attn_decode_kv4_workspace_size(4, max_rows, hq, hkv, d, table.shape[1])
+    store = torch.zeros(size + (1 << 20), dtype=torch.uint8, device="cuda")
+    store[size:] = 0x5a
+    o = torch.full_like(q, math.nan)
+    for _ in range(2):
+        binding.rag_attn_decode_paged_kv4(q, kc, vc, o, table, _i32(kv), 1 / math.sqrt(d), _cu(rows), max_rows,
+                                          store[:size])
+        torch.cuda.synchronize()
+        assert (store[size:] == 0x5a).all() and int(store[:4096 * 4].count_nonzero()) == 0
+    want, bound = ss.reference_kv4(q, kc, vc, table.cpu(), kv, rows, 1 / math.sqrt(d))
+    for s in range(4):
+        at = sum(rows[:s])
+        n = min(rows[s], max_rows)
+        if n == rows[s]:
+            within(o[at:at + n], want[at:at + n], bound[at:at + n], f"sequence {s}")
+        else:
+            assert torch.isfinite(o[at:at + n]).all()
+            assert o[at + n:at + rows[s]].isnan().all()
