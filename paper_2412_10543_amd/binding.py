@@ -608,11 +608,17 @@ def rag_attn_decode_kv4_workspace_size(num_seqs, max_seqlen_q, num_q_heads, num_
 
 
 def rag_attn_decode_paged_kv4(q, k_cache, v_cache, o, block_tables, kv_lens, softmax_scale,
-                              cu_seqlens_q=None, max_seqlen_q=1, workspace=None, stream=None) -> None:
+                              cu_seqlens_q=None, max_seqlen_q=None, workspace=None,
+                              stream=None) -> None:
     """q, o [Tq, Hq, d] bf16; caches uint8 [num_blocks, Hkv, 9 * d]; block_tables int32
     [S, max_blocks]; kv_lens int32 [S], the rows counted; cu_seqlens_q int32 [S+1]
-    offsets of the sequences' last rows, or None: one row each; workspace a GPU tensor of
-    rag_attn_decode_kv4_workspace_size bytes, zero-filled once before its first use."""
+    offsets of the sequences' last rows, with max_seqlen_q, the most that one has, or
+    None: one row each; workspace a GPU tensor of rag_attn_decode_kv4_workspace_size
+    bytes, zero-filled once before its first use."""
+    if max_seqlen_q is None:
+        if cu_seqlens_q is not None:
+            raise ValueError("decode kv4: cu_seqlens_q without max_seqlen_q")
+        max_seqlen_q = 1
     t = (q, o, k_cache, v_cache, block_tables, kv_lens, cu_seqlens_q)
     p = _pointers(b"b3b3u3u3i2i1I1", *t)
     if p.__class__ is int:

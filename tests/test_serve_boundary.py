@@ -112,6 +112,16 @@ def test_attention_refusals(kw, status):
 
 
 @needs_lib
+def test_attention_of_chains_is_told_their_length():
+    """A length that the call took for granted would be a bound that longer chains break."""
+    q = torch.zeros((4, 8, 64), dtype=torch.bfloat16)
+    cache, i = torch.zeros((3, 2, 576), dtype=torch.uint8), torch.zeros((2, 1), dtype=torch.int32)
+    args = (q, cache, cache.clone(), q.clone(), i, i[:, 0], 0.1)
+    with pytest.raises(ValueError, match="max_seqlen_q"):
+        binding.rag_attn_decode_paged_kv4(*args, cu_seqlens_q=torch.tensor([0, 1, 4], dtype=torch.int32))
+
+
+@needs_lib
 def test_launches_of_too_many_threads_are_refused():
     """A launch takes less than 2^32 threads: 2^24 workgroups of 256."""
     L = binding.lib()
