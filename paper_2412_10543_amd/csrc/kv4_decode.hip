@@ -975,8 +975,8 @@ Kv4Shape kv4_shape(int num_seqs, int max_rows, int hq, int hkv, int max_blocks) 
   t.cols = (int)std::min<int64_t>(pairs, kQPairs);
   t.tiles = (int)((pairs + kQPairs - 1) / kQPairs);
   t.units = num_seqs <= kKv4PlanSeqs ? std::max(kQWorkgroups / hkv, 1) : 0;
-  // (counters; places among all blocks are counted in 32 bits)
-  if ((int64_t)t.units * hkv > kKv4Counters ||
+  // (counters; places among all blocks are counted in 32 bits; without pages there is nothing to cut)
+  if (max_blocks == 0 || (int64_t)t.units * hkv > kKv4Counters ||
       (double)num_seqs * t.tiles * (max_blocks / 2 + 1 + kQStart) * kQMaxWeight > 1e9)
     t.units = 0;
   return t;

@@ -117,6 +117,21 @@ def test_sequences_without_keys_or_rows():
     assert torch.isfinite(o[:4]).all() and o[4:].isnan().all()
 
 
+@pytest.mark.parametrize("S,rows", [(1, 1), (5, 1), (3, 0)])
+def test_tables_without_pages(S, rows):
+    """The workspace that the library asks for, none, is what the call takes: zeros, or no rows."""
+    hq, hkv, d = 32, 8, 128
+    assert binding.rag_attn_decode_kv4_workspace_size(S, 9, hq, hkv, d, 0) == 0
+    q = torch.randn((S, hq, d)).bfloat16().cuda()
+    kc, vc = (torch.empty((0, hkv, 9 * d), dtype=torch.uint8, device="cuda") for _ in range(2))
+    o, table = torch.full_like(q, math.nan), torch.empty((S, 0), dtype=torch.int32, device="cuda")
+    cu = None if rows else _i32([0] * (S + 1))
+    for _ in range(2):
+        binding.rag_attn_decode_paged_kv4(q, kc, vc, o, table, _i32([0] * S), 0.1, cu, 9)
+        torch.cuda.synchronize()
+        assert (o == 0).all() if rows else o.isnan().all()
+
+
 @pytest.mark.parametrize("S", [200, 1024, 1025])
 def test_many_sequences(S):
     """Up to 1024 sequences share all keys; with one more none is cut."""
