@@ -629,8 +629,10 @@ rag_status rag_kv4_read(const void *k_cache, const void *v_cache,
                         int32_t block_size, hipStream_t stream);
 
 /*
- * Bytes of workspace for rag_attn_decode_paged_kv4 calls of these sizes and of smaller
- * ones (it does not depend on num_seqs and max_blocks_per_seq).  0 for invalid sizes.
+ * Bytes of workspace for rag_attn_decode_paged_kv4 calls of these sizes and, with the same
+ * heads, of smaller ones (it does not depend on num_seqs and max_blocks_per_seq; other
+ * numbers of heads may need more, also where they are fewer).  0 for invalid sizes and for
+ * tables of no pages, which need none.
  * Library-internal layout: 4096 int32 arrival counters, fp32 log-sum-exps and fp32
  * partial outputs of the workgroups.
  */
@@ -659,11 +661,11 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
  *            the sequence's keys again: for pieces of hundreds of rows rag_kv4_read and
  *            rag_attn_prefill_varlen are faster.
  *   workspace, workspace_bytes  device scratch of at least
- *            rag_attn_decode_kv4_workspace_size(...) bytes for the same arguments or for
- *            larger sizes; 256-byte aligned.  It must be zero-filled before its first
- *            use; every completed call leaves its counters zero again, so that calls of
- *            any sizes may follow each other in it.  Calls that may overlap, and graphs
- *            that may be replayed at once, must not share it.
+ *            rag_attn_decode_kv4_workspace_size(...) bytes for the same arguments or, with
+ *            the same heads, for larger sizes; 256-byte aligned.  It must be zero-filled
+ *            before its first use; every completed call leaves its counters zero again, so
+ *            that calls of any sizes that it serves may follow each other in it.  Calls that
+ *            may overlap, and graphs that may be replayed at once, must not share it.
  *
  * Any num_q_heads / num_kv_heads.  Up to 1024 sequences are cut on the GPU from their
  * lengths into even shares for the workgroups that it works on at a time; with more,

@@ -155,6 +155,20 @@ def test_attention_workspace_serves_smaller_calls():
     assert size(1, 1, 32, 8, 128, 10, 32) == 0
 
 
+@needs_lib
+def test_attention_workspace_is_of_its_heads():
+    """Why the promise of smaller calls is one for the same heads: shares per kv head are whole
+    workgroups, and fewer kv heads have more rows of q heads each."""
+    size = binding.rag_attn_decode_kv4_workspace_size
+    assert size(1, 1, 4, 4, 128, 10) > size(1, 1, 5, 5, 128, 10)
+    assert size(1, 1, 256, 256, 128, 10) > size(1, 1, 300, 300, 128, 10)
+    assert size(1, 1, 32, 8, 128, 10) > size(1, 1, 32, 32, 128, 10)
+    header = open(os.path.join(os.path.dirname(binding.__file__), "..", "include", "rag_attn.h")).read()
+    words = " ".join(header.replace("*", " ").split())
+    assert "rag_attn_decode_paged_kv4 calls of these sizes and, with the same heads, of smaller ones" in words
+    assert "for the same arguments or, with the same heads, for larger sizes" in words
+
+
 VERIFY = dict(logits=_at(0), wide=0, ls=1000, draft=None, ds=0, tokens=_at(2), parents=_at(3), cu=_at(4),
               heat=_at(5), u=_at(6), kept=_at(7), n=_at(8), nxt=_at(9), T=20, S=4, V=1000, most=8,
               ws=_at(10), ws_bytes=1 << 30)
