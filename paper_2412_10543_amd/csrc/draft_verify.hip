@@ -302,7 +302,11 @@ __device__ __forceinline__ VRow row_of(const VerifyArgs& a, const VStat* stats, 
   r.total = wave_sum(r.total);
   if (r.total > 0) return r;
   r.total = 0;
-  if (heat > 0.f) {                        // (all masked, or +inf among them)
+  if (r.top == -INFINITY) {                // (all masked: NaN among them is alike, but equals nothing)
+    r.best = 0;
+    return r;
+  }
+  if (heat > 0.f) {                        // (+inf among them)
     const void* x = logits_row<kWide>(a, row);
     for (int e = lane * 8; e < a.vocab; e += kVStep) {
       float y[8];
@@ -313,7 +317,7 @@ __device__ __forceinline__ VRow row_of(const VerifyArgs& a, const VStat* stats, 
     }
   }
   arg = wave_min(arg);
-  r.best = arg < a.vocab ? arg : 0;        // (a row of NaN: 0)
+  r.best = arg < a.vocab ? arg : 0;
   return r;
 }
 

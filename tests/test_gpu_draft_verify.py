@@ -163,6 +163,33 @@ def test_masked_and_unusual_logits():
             assert want is None or got == tuple(want), (u, heat)
 
 
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("vocab", [3, 5000])
+def test_rows_of_nan_and_masks_alone(vocab, wide):
+    """NaN counts as -inf also where nothing else is left: the first index of the maximum is 0,
+    whichever of the two stands there."""
+    inf, nan = math.inf, math.nan
+    rows = [[nan] + [-inf] * (vocab - 1), [-inf] + [nan] * (vocab - 1), [nan] * (vocab - 1) + [-inf],
+            [nan] * vocab, [-inf] * vocab, [nan, -inf] + [nan] * (vocab - 2)]
+    x = torch.tensor(rows)
+    x = x if wide else x.bfloat16()
+    n, u = len(rows), 0.6
+    for heat in (0.0, 1.0):
+        assert _verify(x.cuda(), [0] * n, None, list(range(n + 1)), [heat] * n, [u] * n, None, 1) == \
+            ([[0]] * n, [1] * n, [0] * n)
+        # chains of two: token 0 is what such a row says, 1 is not
+        q = torch.full((2 * n, vocab), 1.0 / vocab).cuda()
+        y = x.repeat_interleave(2, 0).cuda()
+        for token in (0, 1):
+            tokens = [9, token] * n
+            cu, h, us = list(range(0, 2 * n + 1, 2)), [heat] * n, [u] * (2 * n)
+            for draft in (None, q):
+                got = _verify(y, tokens, None, cu, h, us, draft, 2)
+                want = ss.reference_verify(y.float().cpu().numpy(), tokens, cu, h, us, 2,
+                                           draft=None if draft is None else q.cpu().numpy())
+                assert got == tuple(want) and got[1] == [1 if token else 2] * n and got[2] == [0] * n
+
+
 def test_numbers_outside_the_interval_stay_in_the_vocabulary():
     x = torch.randn((4, 5000)).cuda()
     q = torch.softmax(torch.randn((4, 5000)), 1).cuda()
