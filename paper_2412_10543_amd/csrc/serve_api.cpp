@@ -154,9 +154,15 @@ rag_status rope(const char* who, rag::RopeArgs a, bool kv4, int32_t block_size, 
   // (a row is written by the lanes that have read it, so that an output may be its own input)
   const size_t last = (size_t)a.num_tokens - 1;
   const size_t pool = (size_t)num_blocks * a.hkv * (kv4 ? 9 * a.d : kBlock * a.d * 2);
+  const size_t weight = (size_t)a.d * 2;
   const Span in[] = {{"q", a.q, 2 * (last * a.q_stride + wq)},
                      {"k", a.k, 2 * (last * a.k_stride + wk)},
-                     {"v", a.v, 2 * (last * a.v_stride + wk)}};
+                     {"v", a.v, 2 * (last * a.v_stride + wk)},
+                     {"slot_mapping", a.slots, (last + 1) * 4},
+                     {"positions", a.positions, (last + 1) * 4},
+                     {"cos_sin", a.cos_sin, a.cos_sin ? (size_t)a.max_position * a.rot * 4 : 0},
+                     {"q_weight", a.q_weight, weight},
+                     {"k_weight", a.k_weight, weight}};
   const Span out[] = {{"q_out", a.q_out, 2 * (last + 1) * wq},
                       {"k_out", a.k_out, 2 * (last + 1) * wk},
                       {"v_out", a.v_out, 2 * (last + 1) * wk},
@@ -165,7 +171,7 @@ rag_status rope(const char* who, rag::RopeArgs a, bool kv4, int32_t block_size, 
   for (int i = 0; i < 5; ++i) {
     for (int j = i + 1; j < 5; ++j)
       if ((st = check_apart(who, out[i], out[j])) != RAG_OK) return st;
-    for (int j = 0; j < 3; ++j)
+    for (int j = 0; j < 8; ++j)
       if (!(i == j && out[i].at == in[j].at && out[i].bytes == in[j].bytes) &&
           (st = check_apart(who, out[i], in[j])) != RAG_OK)
         return st;

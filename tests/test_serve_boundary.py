@@ -75,6 +75,21 @@ def test_rope_refuses_outputs_that_overlap(a, b, bytes_b):
         assert "overlap" in binding.rag_last_error()
 
 
+@needs_lib
+@pytest.mark.parametrize("b,bytes_b", [("slots", 20), ("pos", 20), ("cs", 1000 * 128 * 4), ("qw", 256),
+                                       ("kw", 256)])
+@pytest.mark.parametrize("a", ["qo", "ko", "vo", "kc", "vc"])
+def test_rope_refuses_outputs_over_its_other_inputs(a, b, bytes_b):
+    """Slots, positions, angles and weights, in part or whole, in either call."""
+    L = binding.lib()
+    for call in (L.rag_qkv_rope_write, L.rag_qkv_rope_write_kv4):
+        for shift in (0, 16 * ((bytes_b - 1) // 16), -16):
+            x = dict(ROPE)
+            x[a] = x[b] + shift
+            _says(call(*x.values(), None), BAD)
+            assert "overlap" in binding.rag_last_error()
+
+
 READ = dict(kc=_at(0), vc=_at(1), table=_at(2), cu=_at(3), k=_at(4), v=_at(5), T=100, S=3, width=10,
             blocks=50, hkv=8, d=128, bs=16)
 
