@@ -613,12 +613,14 @@ rag_status rag_qkv_rope_write_kv4(
  *   cu_seqlens_k  device int32 [num_seqs + 1], as in rag_attn_prefill_varlen: rows
  *            [cu[s], cu[s+1]) get the first cu[s+1] - cu[s] keys of sequence s
  *   k, v     device [num_rows, num_kv_heads, head_dim]; output: s (c - z) rounded to
- *            bf16.  num_rows >= cu[num_seqs]; rows behind those stay as they are.
+ *            bf16.  num_rows >= cu[num_seqs]; rows behind those stay as they are.  Neither
+ *            may overlap the other or anything else.
  * Preconditions (checked when RAG_ATTN_CHECK=1): cu starts at 0 and does not decrease,
  * keys inside the table, pages inside the pool.
  *
  * Returns RAG_OK (no rows, no sequences or a table of no pages is a no-op),
- * RAG_ERR_INVALID_ARG, RAG_ERR_UNSUPPORTED (head_dim, block_size, sizes) or RAG_ERR_HIP.
+ * RAG_ERR_INVALID_ARG (null, misaligned or overlapping pointers, sizes),
+ * RAG_ERR_UNSUPPORTED (head_dim, block_size, sizes) or RAG_ERR_HIP.
  */
 rag_status rag_kv4_read(const void *k_cache, const void *v_cache,
                         const int32_t *block_tables,

@@ -318,8 +318,19 @@ rag_status rag_kv4_read(const void* k_cache, const void* v_cache, const int32_t*
     return fail(RAG_ERR_INVALID_ARG, "kv4 read: pointer not 16-byte aligned");
   const rag::Kv4ReadArgs a{k_cache,  v_cache,  block_tables,       cu_seqlens_k, k,       v,
                            num_rows, num_seqs, max_blocks_per_seq, num_kv_heads, head_dim};
-  if (check_mode() && (st = check_read(a, num_blocks, stream)) != RAG_OK) return st;
   if (rag::kv4_read_grid(a) > kMaxGroups) return fail(RAG_ERR_UNSUPPORTED, "kv4 read: too many rows");
+  const size_t rows = (size_t)num_rows * num_kv_heads * head_dim * 2;
+  const size_t pool = (size_t)num_blocks * num_kv_heads * 9 * head_dim;
+  const Span spans[] = {{"k", k, rows},
+                        {"v", v, rows},
+                        {"k_cache", k_cache, pool},
+                        {"v_cache", v_cache, pool},
+                        {"block_tables", block_tables, (size_t)num_seqs * max_blocks_per_seq * 4},
+                        {"cu_seqlens_k", cu_seqlens_k, ((size_t)num_seqs + 1) * 4}};
+  for (int i = 0; i < 2; ++i)
+    for (int j = i + 1; j < 6; ++j)
+      if ((st = check_apart("kv4 read", spans[i], spans[j])) != RAG_OK) return st;
+  if (check_mode() && (st = check_read(a, num_blocks, stream)) != RAG_OK) return st;
   if (rag::launch_kv4_read(a, stream) != hipSuccess)
     return fail(RAG_ERR_HIP, "kv4 read: kernel launch failed");
   return ok();

@@ -107,6 +107,18 @@ def test_read_refusals(kw, status):
     _says(binding.lib().rag_kv4_read(*dict(READ, **kw).values(), None), status)
 
 
+@needs_lib
+@pytest.mark.parametrize("a,b,bytes_b", [
+    ("k", "v", 100 * 2048), ("k", "kc", 50 * 8 * 1152), ("v", "vc", 50 * 8 * 1152), ("k", "vc", 50 * 8 * 1152),
+    ("v", "table", 120), ("k", "table", 120), ("v", "cu", 16), ("k", "cu", 16)])
+def test_read_refuses_outputs_that_overlap(a, b, bytes_b):
+    for shift in (0, 16 * ((bytes_b - 1) // 16), -16):
+        x = dict(READ)
+        x[a] = x[b] + shift
+        _says(binding.lib().rag_kv4_read(*x.values(), None), BAD)
+        assert "overlap" in binding.rag_last_error()
+
+
 ATTN = dict(q=_at(0), kc=_at(1), vc=_at(2), o=_at(3), table=_at(4), kv=_at(5), cu=_at(6), S=4, rows=3,
             width=20, blocks=100, hq=32, hkv=8, d=128, bs=16, scale=0.088, ws=_at(7), ws_bytes=1 << 30)
 
