@@ -650,7 +650,8 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
  * the rows are in the cache already (rag_qkv_rope_write_kv4).
  *
  *   q, o     device [Tq, num_q_heads, head_dim]; o is output, written up to row
- *            cu[num_seqs]
+ *            cu[num_seqs].  o may be q; otherwise neither it nor the workspace may overlap
+ *            anything else.
  *   k_cache, v_cache  as in rag_qkv_rope_write_kv4
  *   block_tables, num_blocks, block_size  as in rag_attn_decode_paged
  *   kv_lens  device int32 [num_seqs]: keys of sequence s, counting those of its rows
@@ -674,9 +675,10 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
  * none is cut.  Preconditions (checked when RAG_ATTN_CHECK=1): the above, keys inside
  * the table, pages inside the pool.
  *
- * Returns RAG_OK (num_seqs == 0 or max_seqlen_q == 0 is a no-op), RAG_ERR_INVALID_ARG,
- * RAG_ERR_UNSUPPORTED (head_dim, block_size, max_seqlen_q * num_q_heads from 2^24 on,
- * sizes), RAG_ERR_WORKSPACE or RAG_ERR_HIP.
+ * Returns RAG_OK (num_seqs == 0 or max_seqlen_q == 0 is a no-op), RAG_ERR_INVALID_ARG
+ * (null, misaligned or overlapping pointers, sizes, softmax_scale), RAG_ERR_UNSUPPORTED
+ * (head_dim, block_size, max_seqlen_q * num_q_heads from 2^24 on, sizes),
+ * RAG_ERR_WORKSPACE or RAG_ERR_HIP.
  */
 rag_status rag_attn_decode_paged_kv4(
     const void *q, const void *k_cache, const void *v_cache, void *o,

@@ -396,6 +396,24 @@ rag_status rag_attn_decode_paged_kv4(const void* q, const void* k_cache, const v
     a.part_lse = reinterpret_cast<float*>((char*)workspace + ws.lse_off);
     a.part_o = reinterpret_cast<float*>((char*)workspace + ws.o_off);
   }
+  // (o may be q: a tile's rows are written when all its pieces have read them.  How many rows there are
+  // with cu_seqlens_q the host does not know: one at least.)
+  const size_t width = (size_t)num_q_heads * head_dim * 2, seqs = (size_t)num_seqs;
+  const size_t rows = (cu_seqlens_q ? 1 : seqs) * width;
+  const size_t pool = (size_t)num_blocks * num_kv_heads * 9 * head_dim;
+  const Span spans[] = {{"o", o, rows},
+                        {"workspace", ws.bytes > 0 ? workspace : nullptr, ws.bytes},
+                        {"q", q, rows},
+                        {"k_cache", k_cache, pool},
+                        {"v_cache", v_cache, pool},
+                        {"block_tables", block_tables, seqs * max_blocks_per_seq * 4},
+                        {"kv_lens", kv_lens, seqs * 4},
+                        {"cu_seqlens_q", cu_seqlens_q, (seqs + 1) * 4}};
+  for (int i = 0; i < 2; ++i)
+    for (int j = i + 1; j < 8; ++j)
+      if (!(i == 0 && j == 2 && o == q) &&
+          (st = check_apart("decode kv4", spans[i], spans[j])) != RAG_OK)
+        return st;
   if (check_mode() && (st = check_kv4(a, num_blocks, stream)) != RAG_OK) return st;
   if (rag::launch_kv4(a, t, stream) != hipSuccess)
     return fail(RAG_ERR_HIP, "decode kv4: kernel launch failed");

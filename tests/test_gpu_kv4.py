@@ -163,6 +163,20 @@ def test_cuts_do_not_depend_on_the_others():
     within(c, want[index], bound[index])
 
 
+@pytest.mark.parametrize("kv,rows", [([9000, 40], [1, 1]), ([5000, 700, 3, 2500], [9, 17, 1, 33]),
+                                     ([300] * 1030, [1] * 1030)])
+def test_in_place(kv, rows):
+    """o = q: cut sequences, several tiles, and launches that cut none."""
+    hq, hkv, d = (32, 8, 128) if len(kv) < 1000 else (4, 2, 64)
+    q, kc, vc, table = _case(kv, rows, hq, hkv, d, 14)
+    o = _attend(q, kc, vc, table, kv, rows)
+    for _ in range(3):
+        p, ws = q.clone(), _workspace(len(kv), max(rows), hq, hkv, d)
+        binding.rag_attn_decode_paged_kv4(p, kc, vc, p, table, _i32(kv), 1 / math.sqrt(d), _cu(rows),
+                                          max(rows), ws)
+        assert torch.equal(o, p)
+
+
 def test_physical_order_of_pages_changes_nothing():
     kv, hq, hkv, d = [1234, 600], 8, 2, 128
     q, kc, vc, table = _case(kv, [1, 1], hq, hkv, d, 9, poison=False)

@@ -139,6 +139,25 @@ def test_attention_refusals(kw, status):
 
 
 @needs_lib
+@pytest.mark.parametrize("cu", [_at(6), None])
+@pytest.mark.parametrize("a", ["o", "ws"])
+@pytest.mark.parametrize("b,bytes_b", [("q", 4 * 8192), ("kc", 100 * 8 * 1152), ("vc", 100 * 8 * 1152),
+                                       ("table", 320), ("kv", 16), ("cu", 20), ("ws", 4096), ("o", 4 * 8192)])
+def test_attention_refuses_outputs_that_overlap(a, b, bytes_b, cu):
+    if a == b or (b == "cu" and cu is None):
+        return
+    if cu and b in ("q", "o"):
+        bytes_b = 8192                         # (a row at least)
+    step = 256 if a == "ws" else 16
+    for shift in (0, step * ((bytes_b - 1) // step), -step):
+        if (a, b, shift) != ("o", "q", 0):     # (in place)
+            x = dict(ATTN, cu=cu)
+            x[a] = x[b] + shift
+            _says(binding.lib().rag_attn_decode_paged_kv4(*x.values(), None), BAD)
+            assert "overlap" in binding.rag_last_error()
+
+
+@needs_lib
 def test_attention_of_chains_is_told_their_length():
     """A length that the call took for granted would be a bound that longer chains break."""
     q = torch.zeros((4, 8, 64), dtype=torch.bfloat16)
