@@ -677,8 +677,8 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
  *
  * Returns RAG_OK (num_seqs == 0 or max_seqlen_q == 0 is a no-op), RAG_ERR_INVALID_ARG
  * (null, misaligned or overlapping pointers, sizes, softmax_scale), RAG_ERR_UNSUPPORTED
- * (head_dim, block_size, max_seqlen_q * num_q_heads from 2^24 on, sizes),
- * RAG_ERR_WORKSPACE or RAG_ERR_HIP.
+ * (head_dim, block_size, max_seqlen_q * num_q_heads from 2^24 on, tables of more than 2^26
+ * pages, sizes), RAG_ERR_WORKSPACE or RAG_ERR_HIP.
  */
 rag_status rag_attn_decode_paged_kv4(
     const void *q, const void *k_cache, const void *v_cache, void *o,

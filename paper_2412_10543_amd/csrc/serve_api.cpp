@@ -24,6 +24,9 @@ using rag::ok;
 
 // Page ids fit in int32 slots (page * 16 + offset), table widths in int32 keys.
 constexpr int32_t kMaxPages = 1 << 27;
+// Pages of a sequence that is attended: keys behind its last block, and the places where all
+// sequences' shares start (512 of up to 1/62 of the longest, four a block), fit in int32 too.
+constexpr int32_t kMaxAttended = 1 << 26;
 // Workgroups of a launch, of 256 threads at most: it takes less than 2^32 threads.
 constexpr int64_t kMaxGroups = (1 << 24) - 1;
 
@@ -342,7 +345,7 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
                                           int32_t block_size) {
   if (num_seqs <= 0 || max_seqlen_q <= 0 || num_kv_heads <= 0 || num_q_heads <= 0 ||
       num_q_heads % num_kv_heads != 0 || (head_dim != 64 && head_dim != 128) ||
-      max_blocks_per_seq <= 0 || max_blocks_per_seq >= kMaxPages || block_size != kBlock)
+      max_blocks_per_seq <= 0 || max_blocks_per_seq > kMaxAttended || block_size != kBlock)
     return 0;
   // (of one sequence: the same for all numbers of them, and for all table widths)
   return kv4_workspace(rag::kv4_shape(1, max_seqlen_q, num_q_heads, num_kv_heads, 1), num_kv_heads,
@@ -366,6 +369,8 @@ rag_status rag_attn_decode_paged_kv4(const void* q, const void* k_cache, const v
   rag_status st = check_shape("decode kv4", num_q_heads, num_kv_heads, head_dim);
   if (st == RAG_OK) st = check_paging("decode kv4", block_size, max_blocks_per_seq, num_blocks);
   if (st != RAG_OK) return st;
+  if (max_blocks_per_seq > kMaxAttended)
+    return fail(RAG_ERR_UNSUPPORTED, "decode kv4: tables of more than %d pages", kMaxAttended);
   if (cu_seqlens_q == nullptr) max_seqlen_q = 1;
   if ((int64_t)max_seqlen_q * num_q_heads >= 1 << 24)
     return fail(RAG_ERR_UNSUPPORTED, "decode kv4: %d rows of %d heads (2^24 of them)", max_seqlen_q,

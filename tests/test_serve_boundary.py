@@ -186,6 +186,21 @@ def test_launches_of_too_many_threads_are_refused():
 
 
 @needs_lib
+def test_tables_wider_than_the_plan_counts():
+    """Where the plan's places fit in 32 bits at the widest table that is taken, and did not at
+    wider ones: 512 shares, each at least the longest tile's 62nd part, a block counted four times."""
+    widest = 1 << 26
+    longest = (widest // 2 + 24) * 4
+    assert 512 * ((longest + 61) // 62) < 1 << 31 < 512 * (((1 << 26) - 1 + 24) * 4 // 62)
+    assert 16 * (widest + 2 * 64) < 1 << 31              # a key of the last pages requested
+    L = binding.lib()
+    for width, want in ((widest, WS), (widest + 1, NO), ((1 << 27) - 1, NO)):
+        _says(L.rag_attn_decode_paged_kv4(*dict(ATTN, S=1, width=width, ws=None).values(), None), want)
+        n = binding.rag_attn_decode_kv4_workspace_size(1, 3, 32, 8, 128, width)
+        assert (n > 0) == (want == WS)
+
+
+@needs_lib
 def test_attention_workspace_serves_smaller_calls():
     size = binding.rag_attn_decode_kv4_workspace_size
     for hq, hkv, d in ((32, 8, 128), (64, 8, 128), (14, 2, 64), (512, 512, 128)):
