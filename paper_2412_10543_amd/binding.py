@@ -388,7 +388,7 @@ _TYPES = {"i": torch.int32, "l": torch.int64, "u": torch.uint8, "b": torch.bfloa
 
 def _refuse_at(i, spec, names, tensors):
     """Why tensor i was not taken."""
-    first = next(t for t in tensors if isinstance(t, torch.Tensor))
+    first = next((t for t in tensors if isinstance(t, torch.Tensor)), None)   # (None: i's type is why)
     if i == len(tensors):
         raise ValueError(f"tensors on {first.device}, not on the current device")
     t, name, kind = tensors[i], names.split()[i], chr(spec[2 * i]).lower()

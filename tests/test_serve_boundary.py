@@ -158,6 +158,21 @@ def test_attention_refuses_outputs_that_overlap(a, b, bytes_b, cu):
 
 
 @needs_lib
+@pytest.mark.parametrize("x", [None, 3, np.zeros((2, 2), dtype=np.int32)])
+@pytest.mark.parametrize("call,count,first", [
+    ("rag_kv_pages_update", 10, "block_tables"), ("rag_kv_cache_keep", 6, "k_cache"),
+    ("rag_kv4_read", 6, "k_cache"), ("rag_draft_verify", 8, "logits"), ("rag_qkv_rope_write", 6, "k"),
+    ("rag_attn_decode_paged_kv4", 6, "q"), ("rag_attn_decode_paged_tree", 8, "q"),
+    ("rag_attn_prefill_varlen_ranges", 8, "q")])
+def test_arguments_that_are_no_tensors_are_named(call, count, first, x):
+    """No tensor among them: the first is refused by its name, as it is among tensors."""
+    more = {"rag_attn_decode_paged_kv4": (0.1,), "rag_attn_decode_paged_tree": (4, 0.1),
+            "rag_attn_prefill_varlen_ranges": (8, 8, 0.1)}.get(call, ())
+    with pytest.raises(TypeError, match=f"^{first} must be a torch.Tensor"):
+        getattr(binding, call)(*[x] * count, *more)
+
+
+@needs_lib
 def test_attention_of_chains_is_told_their_length():
     """A length that the call took for granted would be a bound that longer chains break."""
     q = torch.zeros((4, 8, 64), dtype=torch.bfloat16)
