@@ -506,7 +506,8 @@ __global__ __launch_bounds__(kWave) void verify_walk_kernel(VerifyArgs a) {
   if (a.num_seqs == 0 || row >= min(a.cu[a.num_seqs], a.num_rows)) return;
   const VWs ws = verify_ws(a.ws, a.num_rows, a.vocab);
   const int segs = verify_segments(a.vocab, kV), s = sequence_of(a, row);
-  const int first = a.cu[s], n = a.cu[s + 1] - first;
+  // (rows behind num_rows are a broken precondition: no arrival of theirs is waited for)
+  const int first = a.cu[s], n = min(a.cu[s + 1], a.num_rows) - first;
   const float heat = a.temperature[s], u = a.uniforms[row];
   const double k = log2e_over(heat);
   const VStat* stats = ws.stats + (size_t)row * segs;

@@ -190,6 +190,21 @@ def test_rows_of_nan_and_masks_alone(vocab, wide):
                 assert got == tuple(want) and got[1] == [1 if token else 2] * n and got[2] == [0] * n
 
 
+@pytest.mark.parametrize("chain,with_draft", [(False, False), (True, False), (True, True)])
+def test_offsets_past_the_rows_leave_the_workspace_as_it_was(chain, with_draft):
+    """A broken precondition (a last sequence that ends behind num_rows), which the call is not told
+    of: the sequence has the rows that there are, and the next call's counters are zero."""
+    lens, vocab = [4, 1, 9], 700
+    logits, tokens, parents, cu, heat, u, draft = ss.verify_case(3, lens, vocab, chain, heats=(1.0,))
+    ws = _workspace(14, 3, vocab)
+    args = (tokens, None if chain else parents)
+    want = ss.reference_verify(logits.numpy(), tokens, cu, heat, u.tolist(), 9, None if chain else parents,
+                               draft.numpy() if with_draft else None)
+    q = draft.cuda() if with_draft else None
+    for end in (14, 23, 1 << 20, 14):                       # (_verify looks at the counters)
+        assert _verify(logits.cuda(), *args, cu[:3] + [end], heat, u, q, 9, ws) == tuple(want)
+
+
 def test_numbers_outside_the_interval_stay_in_the_vocabulary():
     x = torch.randn((4, 5000)).cuda()
     q = torch.softmax(torch.randn((4, 5000)), 1).cuda()
