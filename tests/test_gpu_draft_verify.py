@@ -287,6 +287,45 @@ def test_large_vocabulary_flat_drafts():
     assert got == tuple(want)
 
 
+def _lens(rows, S, seed):
+    """S lengths of at least 1 that have `rows` nodes together."""
+    r = random.Random(seed)
+    lens = [1] * S
+    for _ in range(rows - S):
+        lens[r.randrange(S)] += 1
+    return lens
+
+
+# A wave has one, two or four loads of 512 logits of a row, from 66 and from 131 rows of 128,077 tokens
+# on, and in the draws behind chains from 17 and from 33 sequences on.
+@pytest.mark.parametrize("rows", [40, 70, 131, 300])
+@pytest.mark.parametrize("S", [5, 17, 33])
+@pytest.mark.parametrize("wide", [False, True])
+def test_batches_over_a_large_vocabulary(rows, S, wide):
+    vocab = 128077
+    for chain, with_draft in ((True, True), (True, False), (False, False)):
+        if rows == 300 and (not wide or not chain):
+            continue
+        _check(_lens(rows, S, rows), vocab, chain, with_draft, wide, padded=3, seed=S + rows, near=1.0)
+
+
+def test_flat_logits_and_drafts_in_a_batch_of_chains():
+    """As the flat ones above, at the longest segments: 40 chains, all sums of 128,077 tokens alike."""
+    g = torch.Generator().manual_seed(17)
+    S, n, vocab = 40, 4, 128077
+    x = 0.01 * torch.randn((S * n, vocab), generator=g)
+    q = torch.softmax(0.01 * torch.randn((S * n, vocab), generator=g), 1)
+    u = torch.rand(S * n, generator=g)
+    u[1::n] = torch.where(torch.arange(S) % 2 == 0, u[1::n], 0.9999)          # (half of them: mostly refused)
+    tokens = torch.randint(0, vocab, (S * n,), generator=g).tolist()
+    cu = list(range(0, S * n + 1, n))
+    for draft in (None, q):
+        got = _verify(x.cuda(), tokens, None, cu, [1.0] * S, u, None if draft is None else q.cuda(), n)
+        want = ss.reference_verify(x.numpy(), tokens, cu, [1.0] * S, u.tolist(), n,
+                                   draft=None if draft is None else q.numpy())
+        assert got == tuple(want)
+
+
 def test_one_workspace_for_calls_of_any_sizes():
     ws = _workspace(400, 50, 9000)
     r = random.Random(1)

@@ -141,6 +141,23 @@ def test_many_sequences(S):
     _check(kv, [1] * S, 4, 2, 64, seed=S)
 
 
+@pytest.mark.parametrize("most,group", [(1, 4), (2, 4), (4, 4), (8, 4), (40, 4)])
+def test_many_chains_that_none_is_cut_of(most, group):
+    """More than 1024 sequences, with rows for every form and for several tiles."""
+    r = random.Random(most)
+    rows = [r.choice([0, 1, most]) for _ in range(1030)]
+    kv = [n + r.choice([0, 1, 20, 70]) for n in rows]
+    kv[500] += 1500
+    _check(kv, rows, group, 1, 64, seed=most)
+
+
+@pytest.mark.parametrize("hkv", [300, 600, 4100])
+def test_many_kv_heads(hkv):
+    """One workgroup a kv head for all sequences, and more kv heads than there are counters for."""
+    _check([100, 1, 333], [1, 1, 1], hkv, hkv, 64, seed=hkv)
+    _check([40, 9, 70], [3, 0, 9], hkv, hkv, 64, seed=hkv + 1)
+
+
 def test_cuts_do_not_depend_on_the_others():
     """A sequence alone, among others and in another order: the same numbers up to the
     bound; runs repeat bit by bit, and one workspace serves calls of any sizes."""
@@ -229,6 +246,30 @@ def test_rows_read_back(hkv, d, lens):
         rows, _ = ss.unpack(cache, d, values)
         want = [rows[table[s, :pages_of(n)].long()].reshape(-1, hkv, d)[:n] for s, n in enumerate(lens)]
         assert torch.equal(got.cpu()[:total], torch.cat(want).float().bfloat16())
+        assert (got[total:] == -7).all()
+
+
+# A wave reads one head of a page, then the next, of as many as leave the launch 8192 waves: two, four and
+# eight of 8 (32,768, 65,536 and 131,072 keys), parts of three, six and eight with a shorter last one.
+@pytest.mark.parametrize("hkv,d,pages", [(8, 128, 2100), (8, 128, 4200), (8, 64, 8300), (7, 64, 2800),
+                                         (6, 128, 4200), (3, 64, 8300), (20, 64, 2800), (20, 128, 1700)])
+def test_rows_of_many_keys_read_back(hkv, d, pages):
+    """Over tables that repeat a few pages."""
+    r = random.Random(pages)
+    kc, vc, _ = ss.random_pool([16 * 50], hkv, d, pages)
+    lens = [16 * (pages // 2) + 5, 0, 16 * (pages // 3), 1, 16 * (pages // 6) - 3, 77]
+    width = max(map(pages_of, lens))
+    table = torch.tensor([[r.randrange(kc.shape[0]) for _ in range(width)] for _ in lens], dtype=torch.int32)
+    total = sum(lens)
+    out = [torch.full((total + 3, hkv, d), -7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    binding.rag_kv4_read(kc.cuda(), vc.cuda(), table.cuda(), _cu(lens), *out)
+    for cache, values, got in ((kc, False, out[0]), (vc, True, out[1])):
+        rows = next(iter(ss.unpack(cache, d, values))).float().bfloat16().cuda()
+        at = 0
+        for s, n in enumerate(lens):
+            want = rows[table[s, :pages_of(n)].long().cuda()].reshape(-1, hkv, d)[:n]
+            assert torch.equal(got[at:at + n], want), (s, values)
+            at += n
         assert (got[total:] == -7).all()
 
 

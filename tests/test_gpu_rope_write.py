@@ -215,6 +215,31 @@ def test_norms_of_small_and_large_rows():
     assert (out["q"][2] == 0).all()
 
 
+# Launches whose waves have every second to every eleventh step of a token's heads.
+@pytest.mark.parametrize("T,hq,hkv,d", [(400, 32, 8, 128), (700, 32, 8, 128), (1500, 32, 8, 128),
+                                        (2700, 32, 8, 128), (2300, 14, 2, 64), (1400, 30, 5, 64)])
+def test_tokens_whose_heads_some_waves_share(T, hq, hkv, d):
+    c = _case(T, hq, hkv, d, d // 2, seed=T, pad=0.05)
+    out, four = _run(c, d, False), _run(c, d, True)
+    _check_rows(c, out, False)
+    assert torch.equal(out["q"], four["q"]) and torch.equal(out["k"], four["k"])
+    real = c["slots"] >= 0
+    at = c["slots"][real].long()
+    for cache, before, rows in ((out["kc"], out["before"][0], out["k"]), (out["vc"], out["before"][1], out["v"])):
+        want = before.clone()
+        want[at // 16, :, at % 16] = rows[real]
+        assert torch.equal(cache, want)
+    # the 4-bit pages: those that calls of a few tokens each write
+    kc, vc = (x.cuda() for x in four["before"])
+    qkv = c["qkv"].cuda()
+    for a in range(0, T, 18):
+        part = slice(a, min(a + 18, T))
+        binding.rag_qkv_rope_write_kv4(None, qkv[part, hq:hq + hkv], qkv[part, hq + hkv:], None,
+                                       c["pos"][part].cuda(), c["cs"].cuda(), c["slots"][part].cuda(), kc, vc,
+                                       k_weight=c["kw"].cuda())
+    assert torch.equal(four["kc"], kc.cpu()) and torch.equal(four["vc"], vc.cpu())
+
+
 @pytest.mark.parametrize("T,hq,hkv,d", [(4500, 32, 8, 128), (9001, 4, 2, 64)])
 def test_many_tokens(T, hq, hkv, d):
     """Launches that walk over a token's heads in one wave: the same rows as few tokens."""
