@@ -249,8 +249,6 @@ def test_rows_read_back(hkv, d, lens):
         assert (got[total:] == -7).all()
 
 
-# A wave reads one head of a page, then the next, of as many as leave the launch 8192 waves: two, four and
-# eight of 8 (32,768, 65,536 and 131,072 keys), parts of three, six and eight with a shorter last one.
 @pytest.mark.parametrize("hkv,d,pages", [(8, 128, 2100), (8, 128, 4200), (8, 64, 8300), (7, 64, 2800),
                                          (6, 128, 4200), (3, 64, 8300), (20, 64, 2800), (20, 128, 1700)])
 def test_rows_of_many_keys_read_back(hkv, d, pages):
