@@ -651,13 +651,24 @@ __global__ __launch_bounds__(kVThreads) void verify_rest_kernel(VerifyArgs a) {
   finish(a, s, count, token, kVThreads);
 }
 
-// Loads of a segment of `rows` rows: as many as leave the GPU `fill` waves.
-constexpr int64_t kVFill = 8192;
-// One row a sequence: fewer and longer segments cost fewer arrivals (48 sequences, 128,077 tokens: with
-// 1024 6 us more, 4096 4 more, 8192 14 more).
-constexpr int64_t kVRestFill = 2048;
-// (Rows of eight loads a wave: both batches above 2 us more; of two 4 and 7 more.)
-constexpr int kVMaxLoads = 4, kVMaxRestLoads = 4;
+// Loads of a segment: as many as leave the GPU this many waves.  Microseconds of a call with one, two and
+// four loads of its rows (bf16, no draft probabilities):
+//   128,000 tokens  20 rows 12.6, 11.9, 12.9   40 rows 15.2, 13.3, 13.9   131 rows 24.4, 21.2, 21.3
+//                   700 rows 92, 78, 70
+//   32,768 tokens   66 rows 10.6, 10.6, 11.5   131 rows 13.2, 12.3, 12.7   700 rows 33, 30, 29
+// Over 132 batches of 8 to 384 rows of 20,000 to 256,000 tokens the launch that this chooses is 1.1% above the
+// best of the three on average (with 1024 1.9%, 4096 1.9%, 8192 4.2%).  Eight loads a wave: 2 us more where
+// four are chosen.
+constexpr int64_t kVFill = 2048;
+constexpr int kVMaxLoads = 4;
+// The same of the rows whose next token is drawn from max(p - q, 0), one a sequence: longer segments also cost
+// fewer arrivals.  Chains of six, fp32:
+//   128,077 tokens  8 sequences 22.4, 20.5, 22.5   16 33.6, 27.7, 27.6   48 62, 51, 46
+//   32,768 tokens   8 sequences 12.8, 13.4, 15.3   48 23.1, 22.4, 24.2   96 35.1, 31.0, 32.7
+// Over 132 batches of 2 to 64 sequences 1.9% above the best (with 512 2.1%, 1024 1.5% but up to 12% above
+// 1792 in some, 2048 2.6%, 4096 5.9%).
+constexpr int64_t kVRestFill = 1792;
+constexpr int kVMaxRestLoads = 4;
 
 int verify_loads(int64_t rows, int vocab, int64_t fill, int kv) {
   while (kv > 1 && rows * verify_segments(vocab, kv) < fill) kv /= 2;
