@@ -647,7 +647,9 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
 /*
  * Attention of the last rows of every sequence against a 4-bit paged cache: one decode
  * step, or a chain of drafted tokens judged in one step (rag_draft_verify).  K and V of
- * the rows are in the cache already (rag_qkv_rope_write_kv4).
+ * the rows are in the cache already (rag_qkv_rope_write_kv4).  Trees of drafted tokens
+ * (rag_attn_decode_paged_tree, rag_kv_cache_keep) take the bf16 cache only; a chain's kept
+ * rows are its first ones, so that nothing has to be moved.
  *
  *   q, o     device [Tq, num_q_heads, head_dim]; o is output, written up to row
  *            cu[num_seqs].  o may be q; otherwise neither it nor the workspace may overlap

@@ -19,11 +19,11 @@
 // walks.  With them: workgroups for the one row a sequence whose next token is drawn find it
 // from the segments' sums, sum max(p - q, 0) in segments, and the last one draws.
 //
-// 16 trees of 24 to 64 nodes, 128,000 tokens in bf16: 70 us, 58 of them in the first launch, whose
-// vector units are busy for 65% (some 20 instructions a logit; rows at T = 0 alone take 36, at 5 TB/s),
-// and 12 in the second, a chain of dependent reads.  48 chains of 3 to 9 nodes with the drafter's
-// probabilities, 128,077 tokens in fp32: 52 us, 33 (4.8 TB/s) and 19.  One chain of five, 32,768
-// tokens: 11, of which the kernels wait for one another's first reads.
+// 16 trees of 24 to 64 nodes, 128,000 tokens in bf16: 67 us (under a trace 60 in the first launch, whose
+// vector units are busy for 70%, some 20 instructions a logit; rows at T = 0 alone take 36, at 5 TB/s;
+// and 14 in the second, a chain of dependent reads).  48 chains of 3 to 9 nodes with the drafter's
+// probabilities, 128,077 tokens in fp32: 50 us (33, 4.8 TB/s, and 19).  One chain of five, 32,768
+// tokens: 9.4, of which the kernels wait for one another's first reads.
 #include "common.h"
 #include "serve.h"
 

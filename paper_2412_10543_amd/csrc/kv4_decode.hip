@@ -13,9 +13,10 @@
 // bf16 cache's kernels, and the correction uses the rounded p', so that 128 cancels.
 //
 // HBM-bound where each sequence has few pairs (64 sequences of 2.6k to 10.3k keys, 32 q / 8 kv heads of
-// 128: 88 us, 4.8 TB/s); with 16 to 64 pairs a sequence bound by the chains of product, softmax and
+// 128: 84 us, 5.0 TB/s); with 16 to 64 pairs a sequence bound by the chains of product, softmax and
 // product of the two waves that a SIMD has room for (32 chains of 3 to 9 rows, 700 to 10,304 keys: 61 us,
-// vector units 43% busy, matrix units 11%).
+// vector units 41% busy, matrix units 11%; of its 256 registers the join of up to 64 pairs spills 18, addresses
+// that it loads again for every piece; the loops over blocks spill none).
 //
 // Pages are copied straight into LDS with 16 bytes a lane and lanes in the pages' order, parameters with
 // a load of their lines: a load that finds a line still on its way holds up all behind it (the 64
@@ -45,8 +46,9 @@ namespace {
 constexpr int kQWaves = 4;
 constexpr int kQKeys = 32;                 // keys of a block
 constexpr int kQPairs = 16 * kQWaves;      // pairs of a tile, at most
-// Blocks of a share, at least.  One sequence of 4,782 keys, 32 q / 8 kv heads: 13.6 us; cut down to 4
-// blocks 2.9 more (more partials to join), to 16 0.1 more.
+// Work of a share, at least, as that of blocks of up to 16 pairs (at 17 to 32 pairs it is that of 5 blocks,
+// above of 4; a tile's start counts too).  One sequence of 4,782 keys, 32 q / 8 kv heads: 13.6 us; with 4
+// 2.9 more (more partials to join), with 16 0.1 more.
 constexpr int kQMinBlocks = 8;
 // Blocks that the start of a tile counts for: a workgroup's second piece costs 10 to 20 us more than its
 // blocks (plan, first loads, states, partials; the 32 chains: 61 us; with 18 62.5, 32 63.8).
@@ -641,8 +643,9 @@ __device__ __forceinline__ void kv4_wave_few(const Kv4Args& a, const Kv4Piece& x
           uint32_t code[2];
           kv4_read(code, r.k + 8 * D * pg + at + 8 * g);
           const uint32_t z = r.kp[(pg * kG + g) * 16 + l16], zz = __builtin_amdgcn_perm(z, z, 0x01000100u);
-          // (a product of 16 channels would do, but accumulators that pass from that shape to
-          // the other at once have given wrong sums)
+          // (a product of 16 channels would do, but an accumulator that passes from that shape to the
+          // other needs a wait, which the compiler leaves out: half of such sums were wrong where the
+          // two follow at once, none with 16 cycles between them)
           f32x4 acc = mfma16(kv4_operand(zz, zz, zz, zz), qz[g], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int w = 0; w < 2; ++w) {

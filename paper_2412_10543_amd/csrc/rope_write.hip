@@ -9,8 +9,9 @@
 // Both in fp32, rounded once, to bf16; 4-bit codes (kv4.h) are made of the rounded
 // values, so that they are those of a bf16 cache.
 //
-// HBM-bound: 8,200 tokens of 32 q / 8 kv heads of 128 with packed K and V 46 us, 4.6 TB/s; 7,000 into 4
-// bits 44, 3.5 TB/s, with the vector units busy for 68% (minima, codes and their places).  A wave
+// HBM-bound: 8,200 tokens of 32 q / 8 kv heads of 128 with packed K and V 46 us, 4.6 TB/s; 6,665 into 4
+// bits 44, 3.3 TB/s, with the vector units busy for 69% (minima, codes and their places).  64 tokens take
+// 4.0 us in bf16 and 4.6 in 4 bits, one launch's latencies.  A wave
 // holds 64 / (D/8) head rows at a time, 16 bytes a lane, and walks over the heads of one token with its
 // angles in registers, so that neither the rows nor the angles are read twice and a head's sum of
 // squares stays in DPP rows of 8 or 16 lanes.
