@@ -672,6 +672,8 @@ size_t rag_attn_decode_kv4_workspace_size(int32_t num_seqs, int32_t max_seqlen_q
  *            that calls of any sizes that it serves may follow each other in it.  Calls that
  *            may overlap, and graphs that may be replayed at once, must not share it.
  *
+ * As over the bf16 cache, a row's weighted sums are divided by their weights at the end,
+ * in fp32: with values beyond 1e30 they may overflow.
  * Any num_q_heads / num_kv_heads.  Up to 1024 sequences are cut on the GPU from their
  * lengths into even shares for the workgroups that it works on at a time; with more,
  * none is cut.  Preconditions (checked when RAG_ATTN_CHECK=1): the above, keys inside

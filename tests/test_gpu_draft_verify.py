@@ -3,6 +3,7 @@ every kept node, count and token is the same."""
 import math
 import random
 
+import numpy as np
 import pytest
 import torch
 
@@ -161,6 +162,33 @@ def test_masked_and_unusual_logits():
             # (with u = 0 the first token that has any weight, here e^-400)
             assert token[8] == 3000 or heat == inf or u == 0.0
             assert want is None or got == tuple(want), (u, heat)
+
+
+@pytest.mark.parametrize("heat", [1e-45, 1e-30, 0.01, 1e30, math.inf])
+def test_draws_at_the_ends_of_the_temperatures(heat):
+    """Masked, constant and far-apart rows against weights by hand: where T is infinite every finite
+    logit weighs 1, where it is least the largest ones do."""
+    vocab, inf = 5000, math.inf
+    g = torch.Generator().manual_seed(12)
+    x = torch.randn((6, vocab), generator=g)
+    x[1, :4990] = -inf
+    x[2] = 1e30
+    x[3] = -3e38
+    x[3, 5::7] = -inf
+    x[4, ::2] = 3e38
+    x[4, 1::2] = -3e38
+    x[5, 17:] = math.nan
+    heat = float(torch.tensor(heat))
+    for u in (0.0, 0.25, 0.77, 1 - 2.0 ** -24):
+        u, want = float(torch.tensor(u)), []
+        for row in x.double().numpy():
+            some = np.isfinite(row)
+            far = np.where(some, row - row[some].max(), 0)
+            w = np.where(some, 1.0 if heat == inf else np.exp(np.maximum(far / heat, -1e4)), 0.0)
+            want.append(ss._pick(w, u))
+        got = _verify(x.cuda(), [0] * 6, None, list(range(7)), [heat] * 6, [u] * 6, None, 1)
+        # (with u = 0 a weight that is 0 for one and e^-700 for the other would count)
+        assert u == 0.0 and heat == float(torch.tensor(0.01)) or got[2] == want, (u, heat)
 
 
 @pytest.mark.parametrize("wide", [False, True])
